@@ -437,6 +437,98 @@ mdnn_status_t mdnn_cast(int64_t n, const void* src, mdnn_dtype_t src_type, void*
                         mdnn_dtype_t dst_type, mdnn_stream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * 8-bit serving of trained fully connected layers (section 3.2's lower
+ * precisions taken one step on): quantisers, the product of 8-bit codes, and
+ * the root-mean-square norm that hands rows to it.
+ *
+ * Codes are whole numbers -127..127 with one fp32 scale per row (activations)
+ * or per output channel (weights); a code's value is code * scale.  For a row
+ * t: a = max(max |t|, 2^-100), code = t * fl(127 / a) (rounded to fp32)
+ * rounded to the nearest whole number, ties to even, and scale = fl(a / 127).
+ * A row of zeros has codes 0 and the scale 2^-100 / 127.  A row that holds Inf
+ * or NaN has codes 0 and the scale NaN, which makes its products NaN.
+ *
+ * mdnn_quantize_i8: x [rows][ldx >= cols] of x_type -> q [rows][ldq >= cols],
+ *   scale fp32 [rows].
+ * mdnn_quantize_i8_t: codes with a scale for each column of x, stored
+ *   transposed: q [cols][ldq >= rows], scale fp32 [cols].  For a layer's
+ *   weights W[in, out] this is the product's operand B with a scale for each
+ *   output.  workspace: mdnn_quantize_i8_t_workspace(rows, cols) bytes,
+ *   16-byte aligned (may be NULL when that size is 0).
+ * q may start at any byte and have any ldq; ldq a multiple of 16 with a
+ * 16-byte aligned q lets mdnn_gemm_i8 take its fastest kernels.  Bytes of q
+ * between a row's width and ldq are left as they are.  cols <= 2^29.
+ * Deterministic.  Errors: MDNN_ERR_SHAPE, _DTYPE, _NULL, _LAYOUT (a leading
+ * dimension below the width), _MISALIGNED, _WORKSPACE, _LAUNCH.
+ * ------------------------------------------------------------------------- */
+mdnn_status_t mdnn_quantize_i8(int64_t rows, int64_t cols, const void* x, int64_t ldx, mdnn_dtype_t x_type,
+                               int8_t* q, int64_t ldq, float* scale, mdnn_stream_t stream);
+size_t mdnn_quantize_i8_t_workspace(int64_t rows, int64_t cols);
+mdnn_status_t mdnn_quantize_i8_t(int64_t rows, int64_t cols, const void* x, int64_t ldx, mdnn_dtype_t x_type,
+                                 int8_t* q, int64_t ldq, float* scale, void* workspace, size_t ws_bytes,
+                                 mdnn_stream_t stream);
+
+/* D[m][n] = act( float(sum_k A[m][k] * B[n][k]) * a_scale[m] * b_scale[n] + bias[n] )
+ * A [M][lda >= K] and B [N][ldb >= K] are 8-bit codes (any value -128..127),
+ * a_scale fp32 [M], b_scale fp32 [N], bias NULL or fp32 [N], D [M][ldd >= N]
+ * of d_type (fp32, fp16 or bf16), computed in fp32 from the exact int32 sum
+ * and rounded once.  K <= 131071, so that no sum leaves 32 bits
+ * (MDNN_ERR_SHAPE above).  Any M, N, K >= 0 (M or N == 0: no-op; K == 0: the
+ * sums are 0), any strides and byte addresses of A and B; 16-byte aligned A
+ * and B with lda, ldb multiples of 16 are fastest.  Bytes of A and B past K
+ * in a row are never used.  D must not overlap an input.
+ * workspace: NULL, or 16-byte aligned device memory; with at least
+ * mdnn_gemm_i8_workspace(M, N, K) bytes a product of few output tiles over a
+ * long K splits K across workgroups (the same result: the sums are exact).
+ * It is scratch, overwritten; calls that share one must be ordered on one
+ * stream.  Deterministic.  Errors as above. */
+size_t mdnn_gemm_i8_workspace(int64_t M, int64_t N, int64_t K);
+mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t* A, int64_t lda, const float* a_scale,
+                           const int8_t* B, int64_t ldb, const float* b_scale, const float* bias, mdnn_act_t act,
+                           void* D, int64_t ldd, mdnn_dtype_t d_type, void* workspace, size_t ws_bytes,
+                           mdnn_stream_t stream);
+
+/* Root-mean-square norm with the residual's addition, of rows of `dtype`:
+ *   h = x + residual          (fp32; residual NULL: h = x)
+ *   y = h * gamma / sqrt(mean(h^2) + eps)
+ * gamma NULL (ones) or fp32 [cols]; eps > 0.  h_out (NULL allowed) receives
+ * h rounded to dtype; y is computed from the unrounded h and rounded once.
+ *   mdnn_rmsnorm_fwd     y of dtype;
+ *   mdnn_rmsnorm_i8_fwd  codes and a scale for each row, as defined above for
+ *     t = fl(h * gamma), with scale = fl(a / 127) / sqrt(mean(h^2) + eps): the
+ *     root is common to a row's elements, so the codes do not depend on it.
+ * Sums are fp32 in a fixed order (deterministic).  A row that holds Inf or
+ * NaN, or whose sum of squares passes fp32's range, gives NaN in all of y
+ * (codes 0 and scale NaN; also where h * gamma overflows).
+ * cols >= 1 and <= 2^29, any rows >= 0, leading dimensions >= cols; buffers
+ * need their element alignment.  h_out and y may lie exactly in place of x or
+ * residual (same address and leading dimension); otherwise outputs must not
+ * overlap inputs or each other.  Errors as above (MDNN_ERR_SHAPE for eps). */
+mdnn_status_t mdnn_rmsnorm_fwd(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual,
+                               int64_t ldr, const float* gamma, float eps, void* h_out, int64_t ldh, void* y,
+                               int64_t ldy, mdnn_dtype_t dtype, mdnn_stream_t stream);
+mdnn_status_t mdnn_rmsnorm_i8_fwd(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual,
+                                  int64_t ldr, const float* gamma, float eps, void* h_out, int64_t ldh, int8_t* q,
+                                  int64_t ldq, float* scale, mdnn_dtype_t dtype, mdnn_stream_t stream);
+
+/* Gradients of y with respect to h (hence to x and to residual alike) and
+ * gamma, at the stored h [rows][ldh] (x itself where there was no residual):
+ *   r = 1 / sqrt(mean(h^2) + eps), g = dy * gamma, xh = h * r
+ *   dx = r * (g - xh * mean(g * xh)) + dres      (dres NULL: without it; it
+ *        is the gradient that reaches h along the residual)
+ *   dgamma[c] = sum over rows of dy * xh         (fp32, overwritten)
+ * dy, h, dres, dx are `dtype`; dx and dgamma may each be NULL.  dx may lie
+ * exactly in place of dy, h or dres.  workspace: at least
+ * mdnn_rmsnorm_bwd_workspace(rows, cols) bytes, 256-byte aligned, when dgamma
+ * is asked for (otherwise NULL is allowed); scratch.  Sums in a fixed order
+ * (deterministic).  rows == 0: dgamma = 0.  Errors as above. */
+size_t mdnn_rmsnorm_bwd_workspace(int64_t rows, int64_t cols);
+mdnn_status_t mdnn_rmsnorm_bwd(int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* h, int64_t ldh,
+                               const float* gamma, float eps, const void* dres, int64_t lddr, void* dx, int64_t lddx,
+                               float* dgamma, mdnn_dtype_t dtype, void* workspace, size_t ws_bytes,
+                               mdnn_stream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Train step of a fixed layer chain (section 2.1 compute graph, fixed here;
  * section 3.1 minibatch SGD).  One call = forward, loss, backpropagation and
  * update of one minibatch, all enqueued on one stream with no host sync.

@@ -99,6 +99,13 @@ _SIGS = {
     "mdnn_net_bind": [_vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp],
     "mdnn_net_sync_lowp": [_vp, _vp],
     "mdnn_train_step": [_vp, _vp, _vp, _vp, _vp],
+    "mdnn_quantize_i8": [_i64, _i64, _vp, _i64, _i, _vp, _i64, _vp, _vp],
+    "mdnn_quantize_i8_t": [_i64, _i64, _vp, _i64, _i, _vp, _i64, _vp, _vp, C.c_size_t, _vp],
+    "mdnn_gemm_i8": [_i64, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i, _vp, _i64, _i, _vp, C.c_size_t, _vp],
+    "mdnn_rmsnorm_fwd": [_i64, _i64, _vp, _i64, _vp, _i64, _vp, _f, _vp, _i64, _vp, _i64, _i, _vp],
+    "mdnn_rmsnorm_i8_fwd": [_i64, _i64, _vp, _i64, _vp, _i64, _vp, _f, _vp, _i64, _vp, _i64, _vp, _i, _vp],
+    "mdnn_rmsnorm_bwd": [_i64, _i64, _vp, _i64, _vp, _i64, _vp, _f, _vp, _i64, _vp, _i64, _vp, _i, _vp, C.c_size_t,
+                         _vp],
     "mdnn_train_graph_create": [_vp, _vp, _vp, _vp, _vp],
     "mdnn_graph_launch": [_vp, _vp],
 }
@@ -122,6 +129,12 @@ _lib.mdnn_gemm_split3_workspace.argtypes = [_i64, _i64, _i64]
 _lib.mdnn_gemm_split3_workspace.restype = C.c_size_t
 _lib.mdnn_bias_act_bwd_workspace.argtypes = [_i64, _i64]
 _lib.mdnn_bias_act_bwd_workspace.restype = C.c_size_t
+_lib.mdnn_quantize_i8_t_workspace.argtypes = [_i64, _i64]
+_lib.mdnn_quantize_i8_t_workspace.restype = C.c_size_t
+_lib.mdnn_gemm_i8_workspace.argtypes = [_i64, _i64, _i64]
+_lib.mdnn_gemm_i8_workspace.restype = C.c_size_t
+_lib.mdnn_rmsnorm_bwd_workspace.argtypes = [_i64, _i64]
+_lib.mdnn_rmsnorm_bwd_workspace.restype = C.c_size_t
 _lib.mdnn_last_error.restype = C.c_char_p
 _lib.mdnn_version.restype = C.c_char_p
 _lib.mdnn_net_activation.argtypes = [_vp, C.c_int32]
@@ -183,7 +196,8 @@ def exported_symbols():
                                  "mdnn_conv2d_bwd_filter_noalloc_max_workspace",
                                  "mdnn_gemm_split3_workspace", "mdnn_gemm_workspace",
                                  "mdnn_conv2d_fwd_winograd_workspace", "mdnn_conv2d_fwd_algo_workspace",
-                                 "mdnn_conv2d_fwd_choose",
+                                 "mdnn_conv2d_fwd_choose", "mdnn_quantize_i8_t_workspace",
+                                 "mdnn_gemm_i8_workspace", "mdnn_rmsnorm_bwd_workspace",
                                  "mdnn_last_error",
                                  "mdnn_version", "mdnn_net_activation", "mdnn_net_output_grad", "mdnn_net_destroy",
                                  "mdnn_graph_destroy", "mdnn_set_gemm_tile"])
@@ -338,6 +352,49 @@ def mdnn_gemm_split3(layout, M, N, K, alpha, A, lda, a_scale, B, ldb, b_scale, b
                      workspace, ws_bytes, stream=None):
     return _call("mdnn_gemm_split3", layout, M, N, K, alpha, _p(A), lda, a_scale, _p(B), ldb, b_scale,
                  beta, _p(Cm), ldc, _p(D), ldd, _p(workspace), ws_bytes, _s(stream))
+
+
+def mdnn_quantize_i8(rows, cols, x, ldx, x_type, q, ldq, scale, stream=None):
+    return _call("mdnn_quantize_i8", rows, cols, _p(x), ldx, x_type, _p(q), ldq, _p(scale), _s(stream))
+
+
+def mdnn_quantize_i8_t_workspace(rows, cols) -> int:
+    return _lib.mdnn_quantize_i8_t_workspace(rows, cols)
+
+
+def mdnn_quantize_i8_t(rows, cols, x, ldx, x_type, q, ldq, scale, workspace=None, ws_bytes=0, stream=None):
+    return _call("mdnn_quantize_i8_t", rows, cols, _p(x), ldx, x_type, _p(q), ldq, _p(scale), _p(workspace), ws_bytes,
+                 _s(stream))
+
+
+def mdnn_gemm_i8_workspace(M, N, K) -> int:
+    return _lib.mdnn_gemm_i8_workspace(M, N, K)
+
+
+def mdnn_gemm_i8(M, N, K, A, lda, a_scale, B, ldb, b_scale, bias, act, D, ldd, d_type, workspace=None, ws_bytes=0,
+                 stream=None):
+    return _call("mdnn_gemm_i8", M, N, K, _p(A), lda, _p(a_scale), _p(B), ldb, _p(b_scale), _p(bias), act, _p(D), ldd,
+                 d_type, _p(workspace), ws_bytes, _s(stream))
+
+
+def mdnn_rmsnorm_fwd(rows, cols, x, ldx, residual, ldr, gamma, eps, h_out, ldh, y, ldy, dtype, stream=None):
+    return _call("mdnn_rmsnorm_fwd", rows, cols, _p(x), ldx, _p(residual), ldr, _p(gamma), eps, _p(h_out), ldh, _p(y),
+                 ldy, dtype, _s(stream))
+
+
+def mdnn_rmsnorm_i8_fwd(rows, cols, x, ldx, residual, ldr, gamma, eps, h_out, ldh, q, ldq, scale, dtype, stream=None):
+    return _call("mdnn_rmsnorm_i8_fwd", rows, cols, _p(x), ldx, _p(residual), ldr, _p(gamma), eps, _p(h_out), ldh,
+                 _p(q), ldq, _p(scale), dtype, _s(stream))
+
+
+def mdnn_rmsnorm_bwd_workspace(rows, cols) -> int:
+    return _lib.mdnn_rmsnorm_bwd_workspace(rows, cols)
+
+
+def mdnn_rmsnorm_bwd(rows, cols, dy, lddy, h, ldh, gamma, eps, dres, lddr, dx, lddx, dgamma, dtype, workspace=None,
+                     ws_bytes=0, stream=None):
+    return _call("mdnn_rmsnorm_bwd", rows, cols, _p(dy), lddy, _p(h), ldh, _p(gamma), eps, _p(dres), lddr, _p(dx), lddx,
+                 _p(dgamma), dtype, _p(workspace), ws_bytes, _s(stream))
 
 
 def mdnn_net_create(layers, batch: int, cfg: TrainCfg) -> int:

@@ -15,10 +15,14 @@ from . import (ACT_NONE, BF16, F16, F32, LAYER_CONV, LAYER_FC, LAYER_MAXPOOL2, L
                mdnn_gemm_split3_workspace, mdnn_net_activation, mdnn_net_output_grad, mdnn_net_bind, mdnn_net_create, mdnn_net_destroy, mdnn_net_sizes, mdnn_net_sync_lowp,
                mdnn_split_f16, mdnn_train_step, mdnn_train_step_async, mdnn_train_graph_create,
                mdnn_graph_launch, mdnn_graph_destroy, mdnn_conv2d_fwd_winograd,
-               mdnn_conv2d_fwd_winograd_workspace, mdnn_conv2d_fwd_algo, mdnn_conv2d_fwd_algo_workspace)
+               mdnn_conv2d_fwd_winograd_workspace, mdnn_conv2d_fwd_algo, mdnn_conv2d_fwd_algo_workspace,
+               mdnn_quantize_i8, mdnn_quantize_i8_t, mdnn_quantize_i8_t_workspace, mdnn_gemm_i8,
+               mdnn_gemm_i8_workspace, mdnn_rmsnorm_fwd, mdnn_rmsnorm_i8_fwd, mdnn_rmsnorm_bwd,
+               mdnn_rmsnorm_bwd_workspace)
 
 __all__ = ["torch_dtype", "gemm", "split_f16", "gemm_split3", "conv_shape", "conv2d_fwd",
-           "conv2d_fwd_winograd", "conv2d_fwd_algo", "conv2d_bwd_data", "conv2d_bwd_filter", "make_scaler", "read_scaler", "Net", "StepGraph"]
+           "conv2d_fwd_winograd", "conv2d_fwd_algo", "conv2d_bwd_data", "conv2d_bwd_filter", "make_scaler", "read_scaler", "Net", "StepGraph",
+           "quantize_i8", "gemm_i8", "rmsnorm", "rmsnorm_i8", "rmsnorm_bwd"]
 
 
 def torch_dtype(code: int):
@@ -158,6 +162,147 @@ def conv2d_bwd_filter(x, dy, r: int, s: int, pad: int, with_db: bool = True, str
     ws = torch.empty((max(ws_bytes, 16),), dtype=torch.uint8, device=x.device)
     mdnn_conv2d_bwd_filter(sh, x, dy, dtype_of(x), dw, db, ws, ws_bytes, stream)
     return dw, db
+
+
+def _rows_of(t, name: str):
+    """(rows, cols, leading dimension) of a 2-D device tensor whose rows are
+    contiguous, on the current device (whose stream the call runs on)."""
+    import torch
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be 2-D with contiguous rows")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is not on the current GPU")
+    rows, cols = t.shape
+    return rows, cols, max(t.stride(0), cols) if rows <= 1 else t.stride(0)
+
+
+def _vector_of(t, n: int, name: str):
+    """A contiguous fp32 vector of n elements on the current device."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous fp32 values")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is not on the current GPU")
+    return t
+
+
+def _like(t, x, name: str):
+    """(tensor, leading dimension) of an operand with x's shape and type."""
+    if t is None:
+        return None, x.shape[1]
+    if t.shape != x.shape or t.dtype != x.dtype:
+        raise ValueError(f"{name} must have the shape and type of the first operand")
+    return t, _rows_of(t, name)[2]
+
+
+def _codes_like(q, rows: int, cols: int, device):
+    """Room for [rows, cols] codes; allocated rows start on 16 bytes."""
+    import torch
+    if q is None:
+        q = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
+    elif q.dtype != torch.int8 or tuple(q.shape) != (rows, cols):
+        raise ValueError(f"q must be int8 [{rows}, {cols}]")
+    return q, _rows_of(q, "q")[2]
+
+
+def quantize_i8(x, transpose: bool = False, q=None, scale=None, workspace=None, stream=None):
+    """(codes, scales) of a 2-D tensor: int8 codes with an fp32 scale for each
+    row, or with transpose for each column, the codes stored [cols, rows] (a
+    layer's weights W[in, out] as gemm_i8's operand B)."""
+    import torch
+    rows, cols, ldx = _rows_of(x, "x")
+    n = cols if transpose else rows
+    q, ldq = _codes_like(q, n, rows if transpose else cols, x.device)
+    scale = torch.empty((n,), dtype=torch.float32, device=x.device) if scale is None else _vector_of(scale, n, "scale")
+    if not transpose:
+        mdnn_quantize_i8(rows, cols, x, ldx, dtype_of(x), q, ldq, scale, stream)
+        return q, scale
+    if workspace is None:
+        workspace = torch.empty((max(mdnn_quantize_i8_t_workspace(rows, cols), 16),), dtype=torch.uint8,
+                                device=x.device)
+    mdnn_quantize_i8_t(rows, cols, x, ldx, dtype_of(x), q, ldq, scale, workspace, workspace.numel(), stream)
+    return q, scale
+
+
+def gemm_i8(A, a_scale, B, b_scale, bias=None, act: int = ACT_NONE, out_dtype=None, out=None, workspace=None,
+            stream=None):
+    """D = act((A B^T) * a_scale[:, None] * b_scale + bias) of int8 codes A [M, K],
+    B [N, K].  workspace: None, True (allocate what mdnn_gemm_i8_workspace
+    asks for) or a device byte tensor."""
+    import torch
+    M, K, lda = _rows_of(A, "A")
+    N, KB, ldb = _rows_of(B, "B")
+    if A.dtype != torch.int8 or B.dtype != torch.int8 or KB != K:
+        raise ValueError("A and B must be int8 codes of one depth")
+    _vector_of(a_scale, M, "a_scale"), _vector_of(b_scale, N, "b_scale"), _vector_of(bias, N, "bias")
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype or torch.float32, device=A.device)
+    elif tuple(out.shape) != (M, N):
+        raise ValueError(f"out must be [{M}, {N}]")
+    if workspace is True:
+        workspace = torch.empty((max(mdnn_gemm_i8_workspace(M, N, K), 16),), dtype=torch.uint8, device=A.device)
+    mdnn_gemm_i8(M, N, K, A, lda, a_scale, B, ldb, b_scale, bias, act, out, _rows_of(out, "out")[2], dtype_of(out),
+                 workspace, workspace.numel() if workspace is not None else 0, stream)
+    return out
+
+
+def rmsnorm(x, gamma=None, residual=None, eps: float = 1e-6, h_out=None, out=None, stream=None):
+    """y = h * gamma / sqrt(mean(h^2) + eps) of the rows of h = x + residual.
+    Returns y, or (y, h) with a residual (h_out is allocated then)."""
+    import torch
+    rows, cols, ldx = _rows_of(x, "x")
+    residual, ldr = _like(residual, x, "residual")
+    if residual is not None and h_out is None:
+        h_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    h_out, ldh = _like(h_out, x, "h_out")
+    out, ldy = _like(torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out, x, "out")
+    mdnn_rmsnorm_fwd(rows, cols, x, ldx, residual, ldr, _vector_of(gamma, cols, "gamma"), eps, h_out, ldh, out, ldy,
+                     dtype_of(x), stream)
+    return (out, h_out) if h_out is not None else out
+
+
+def rmsnorm_i8(x, gamma=None, residual=None, eps: float = 1e-6, h_out=None, q=None, scale=None, stream=None):
+    """rmsnorm with its result as int8 codes and an fp32 scale for each row.
+    Returns (q, scale), or (q, scale, h) with a residual."""
+    import torch
+    rows, cols, ldx = _rows_of(x, "x")
+    residual, ldr = _like(residual, x, "residual")
+    if residual is not None and h_out is None:
+        h_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    h_out, ldh = _like(h_out, x, "h_out")
+    q, ldq = _codes_like(q, rows, cols, x.device)
+    scale = (torch.empty((rows,), dtype=torch.float32, device=x.device) if scale is None
+             else _vector_of(scale, rows, "scale"))
+    mdnn_rmsnorm_i8_fwd(rows, cols, x, ldx, residual, ldr, _vector_of(gamma, cols, "gamma"), eps, h_out, ldh, q, ldq,
+                        scale, dtype_of(x), stream)
+    return (q, scale, h_out) if h_out is not None else (q, scale)
+
+
+def rmsnorm_bwd(dy, h, gamma=None, eps: float = 1e-6, dres=None, dx=None, with_dgamma: bool = True, dgamma=None,
+                workspace=None, stream=None):
+    """(dx, dgamma) of rmsnorm at the stored h; dres is the gradient that
+    reaches h along the residual.  dgamma is None without with_dgamma."""
+    import torch
+    rows, cols, lddy = _rows_of(dy, "dy")
+    if h is None:
+        raise ValueError("h is required")
+    h, ldh = _like(h, dy, "h")
+    dres, lddr = _like(dres, dy, "dres")
+    dx, lddx = _like(torch.empty((rows, cols), dtype=dy.dtype, device=dy.device) if dx is None else dx, dy, "dx")
+    if not with_dgamma:
+        dgamma = None
+    elif dgamma is None:
+        dgamma = torch.empty((cols,), dtype=torch.float32, device=dy.device)
+    else:
+        _vector_of(dgamma, cols, "dgamma")
+    if with_dgamma and workspace is None:
+        workspace = torch.empty((max(mdnn_rmsnorm_bwd_workspace(rows, cols), 256),), dtype=torch.uint8,
+                                device=dy.device)
+    mdnn_rmsnorm_bwd(rows, cols, dy, lddy, h, ldh, _vector_of(gamma, cols, "gamma"), eps, dres, lddr, dx, lddx, dgamma,
+                     dtype_of(dy), workspace, workspace.numel() if workspace is not None else 0, stream)
+    return dx, dgamma
 
 
 def make_scaler(scale: float, growth_interval: int = 2000, growth: float = 2.0,

@@ -1,0 +1,875 @@
+// Row-wise operators around the 8-bit product: root-mean-square norm with the
+// residual's addition (16-bit / fp32 or 8-bit output), its gradients, and the
+// quantisers of rows and of columns.
+//
+//   h = x + res                                  (fp32; stored rounded once)
+//   y = h * rstd * gamma,  rstd = 1 / sqrt(mean(h^2) + eps)
+//   codes of a row t: a = max(max|t|, 2^-100), q = rint(fl(t * fl(127 / a))),
+//   scale = fl(a / 127); for the norm t = fl(h * gamma) and the scale is
+//   multiplied by rstd: rstd is common to the row, so it cancels from the
+//   codes, and the sum of squares and the maximum need one pass over the row
+//   and one reduction together.
+//
+// Bound: memory.  A row is read once, kept in registers (chunks of eight
+// consecutive elements, TPR threads per row, NCH chunks per thread), reduced
+// and written once.  Chunks are read and written at element alignment (one
+// unaligned access each); a row's last, partial chunk is read from the row's
+// last eight elements and the ones that belong to its neighbour are cleared,
+// so every load is unconditional and lies inside the row.  Rows longer than
+// the registers hold, or below eight elements, take the two-pass kernels.
+#include <cmath>
+
+#include "common.h"
+#include "internal.h"
+
+namespace mdnn {
+namespace {
+
+constexpr float A_MIN = 0x1p-100f;  // smallest row maximum the codes resolve (127 / a stays finite)
+
+// Eight consecutive elements at any element address.
+typedef uint32_t u4v_a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u4v_a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u2v_a1 __attribute__((ext_vector_type(2), aligned(1)));
+#define MDNN_GLOBAL __attribute__((address_space(1)))
+
+template <class T>
+struct Chunk {
+  static constexpr bool H = sizeof(typename T::storage) == 2;
+  typedef typename T::storage S;
+  uint32_t w[H ? 4 : 8];
+  __device__ __forceinline__ void load(const S* p) {
+    if constexpr (H) {
+      const u4v_a2 v = *(const MDNN_GLOBAL u4v_a2*)p;
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else {
+      const u4v_a4 v = *(const MDNN_GLOBAL u4v_a4*)p, u = *(const MDNN_GLOBAL u4v_a4*)(p + 4);
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w, w[4] = u.x, w[5] = u.y, w[6] = u.z, w[7] = u.w;
+    }
+  }
+  __device__ __forceinline__ float get(int e) const {
+    if constexpr (H)
+      return to_f<T>((uint16_t)(w[e >> 1] >> ((e & 1) * 16)));
+    else
+      return __builtin_bit_cast(float, w[e]);
+  }
+  // clears elements 0 .. lo - 1
+  __device__ __forceinline__ void clear(int lo) {
+    asm("" : "+v"(lo));  // (the tests of lo stay here: hoisted out of a loop over rows they fill the scalar registers)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < lo) w[H ? e >> 1 : e] &= H && !(e & 1) ? 0xffff0000u : 0u;
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    if constexpr (H) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = (uint32_t)from_f<T>(v[2 * e]) | ((uint32_t)from_f<T>(v[2 * e + 1]) << 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = __builtin_bit_cast(uint32_t, v[e]);
+    }
+  }
+  // elements lo .. 7 (lo = 0: one vector store)
+  __device__ __forceinline__ void store(S* p, int lo) const {
+    if (lo == 0) {
+      if constexpr (H) {
+        *(MDNN_GLOBAL u4v_a2*)p = (u4v_a2){w[0], w[1], w[2], w[3]};
+      } else {
+        *(MDNN_GLOBAL u4v_a4*)p = (u4v_a4){w[0], w[1], w[2], w[3]};
+        *(MDNN_GLOBAL u4v_a4*)(p + 4) = (u4v_a4){w[4], w[5], w[6], w[7]};
+      }
+    } else {
+      asm("" : "+v"(lo));
+#pragma unroll
+      for (int e = 1; e < 8; ++e)
+        if (e >= lo) {
+          if constexpr (H)
+            p[e] = (uint16_t)(w[e >> 1] >> ((e & 1) * 16));
+          else
+            p[e] = __builtin_bit_cast(float, w[e]);
+        }
+    }
+  }
+};
+
+// Codes of four values: fl(t * inv) rounded to the nearest even integer (by
+// adding 1.5 * 2^23, whose last place is 1), the low bytes packed.  The
+// product is rounded before the addition: no contraction.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+#pragma clang fp contract(off)
+  constexpr float MAGIC = 12582912.0f;
+  const float pa = a * inv, pb = b * inv, pc = c * inv, pd = d * inv;
+  const uint32_t ua = __float_as_uint(pa + MAGIC), ub = __float_as_uint(pb + MAGIC);
+  const uint32_t uc = __float_as_uint(pc + MAGIC), ud = __float_as_uint(pd + MAGIC);
+  const uint32_t lo = __builtin_amdgcn_perm(ub, ua, 0x0c0c0400u), hi = __builtin_amdgcn_perm(ud, uc, 0x0c0c0400u);
+  return lo | (hi << 16);
+}
+__device__ __forceinline__ float mul_rn(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+__device__ __forceinline__ float add_rn(float a, float b) {
+#pragma clang fp contract(off)
+  return a + b;
+}
+__device__ __forceinline__ void store_codes(int8_t* p, uint32_t lo4, uint32_t hi4, int lo) {
+  if (lo == 0) {
+    *(MDNN_GLOBAL u2v_a1*)p = (u2v_a1){lo4, hi4};
+  } else {
+    asm("" : "+v"(lo));
+#pragma unroll
+    for (int e = 1; e < 8; ++e)
+      if (e >= lo) p[e] = (int8_t)((e < 4 ? lo4 : hi4) >> (8 * (e & 3)));
+  }
+}
+
+// From a row's largest magnitude (as bits: NaN above Inf above the rest) the
+// factor of the codes and the scale; not finite: scale NaN, all codes 0.
+struct RowScale {
+  float inv, scale;
+  uint32_t mask;  // 0: the codes are 0
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t bits, bool bad) {
+  RowScale r;
+  if (bad || bits >= 0x7f800000u) {
+    r.inv = 0.0f, r.scale = __builtin_nanf(""), r.mask = 0u;
+  } else {
+    const float f = __uint_as_float(bits), a = f > A_MIN ? f : A_MIN;
+    r.inv = 127.0f / a, r.scale = a / 127.0f, r.mask = 0xffffffffu;
+  }
+  return r;
+}
+
+// 1 / sqrt(mean + eps); a sum that is not finite (the row holds Inf or NaN,
+// or its squares pass fp32's range) makes the whole row NaN.
+__device__ __forceinline__ float row_rstd(float ssq, float cols, float eps) {
+  return isfinite(ssq) ? 1.0f / sqrtf(ssq / cols + eps) : __builtin_nanf("");
+}
+
+// Two sums, or a sum and a maximum of bit patterns, over a row's TPR threads,
+// in a fixed order.  Rows of more than a wave combine their waves through one
+// of two LDS buffers in turn (`flip`), so a loop over rows has one barrier.
+struct SumMax {
+  float s;
+  uint32_t m;
+};
+template <int TPR>
+__device__ __forceinline__ SumMax row_reduce(SumMax v, SumMax (*buf)[TPR / 64 + 1], int flip) {
+  constexpr int W = TPR < 64 ? TPR : 64;
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) {
+    v.s += __shfl_xor(v.s, o, W);
+    const uint32_t u = (uint32_t)__shfl_xor((int)v.m, o, W);
+    v.m = u > v.m ? u : v.m;
+  }
+  if constexpr (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) buf[flip][threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = buf[flip][0];
+#pragma unroll
+    for (int w = 1; w < TPR / 64; ++w) {
+      const SumMax u = buf[flip][w];
+      v.s += u.s;
+      v.m = u.m > v.m ? u.m : v.m;
+    }
+  }
+  return v;
+}
+struct Sum2 {
+  float a, b;
+};
+template <int TPR>
+__device__ __forceinline__ Sum2 row_reduce(Sum2 v, Sum2 (*buf)[TPR / 64 + 1], int flip) {
+  constexpr int W = TPR < 64 ? TPR : 64;
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) {
+    v.a += __shfl_xor(v.a, o, W);
+    v.b += __shfl_xor(v.b, o, W);
+  }
+  if constexpr (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) buf[flip][threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = buf[flip][0];
+#pragma unroll
+    for (int w = 1; w < TPR / 64; ++w) v.a += buf[flip][w].a, v.b += buf[flip][w].b;
+  }
+  return v;
+}
+
+enum RowMode { QUANT = 0, NORM = 1, NORM_I8 = 2 };
+
+struct RowArgs {
+  const void *x, *res;  // res: or null
+  const float* gamma;   // or null (ones)
+  void *h, *y;          // h: or null
+  int8_t* q;
+  float* scale;
+  int64_t rows, ldx, ldr, ldh, ldy, ldq;
+  int32_t cols;
+  float eps;
+};
+
+// Where this thread's chunk c of a row lies: its first element, and how many
+// of its leading elements are not its own (8: none is).
+struct ChunkPos {
+  int start, lo;
+};
+__device__ __forceinline__ ChunkPos chunk_pos(int c, int cols) {
+  const int at = c * 8, last = cols - 8;
+  return {at < last ? at : last, at <= last ? 0 : at < cols ? at - last : 8};
+}
+
+template <class T, int MODE, int TPR, int NCH>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_kernel(RowArgs a) {
+  typedef typename T::storage S;
+  constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
+  __shared__ SumMax buf[2][TPR / 64 + 1];
+  const int t = threadIdx.x % TPR;
+  ChunkPos pos[NCH];
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) pos[i] = chunk_pos(t + i * TPR, a.cols);
+  int flip = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB, flip ^= 1) {
+    // (a thread group past the last row repeats it and stores nothing)
+    const int64_t rw = r0 + threadIdx.x / TPR;
+    const bool live = rw < a.rows;
+    const int64_t row = live ? rw : a.rows - 1;
+    Chunk<T> cx[NCH], cr[NCH];
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) cx[i].load((const S*)a.x + row * a.ldx + pos[i].start);
+    if (MODE != QUANT && a.res) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) cr[i].load((const S*)a.res + row * a.ldr + pos[i].start);
+    }
+    float h[NCH][8];
+    SumMax v = {0.0f, 0u};
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      if (pos[i].lo > 0) cx[i].clear(pos[i].lo);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] = cx[i].get(e);
+      if (MODE != QUANT && a.res) {
+        if (pos[i].lo > 0) cr[i].clear(pos[i].lo);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[i][e] = add_rn(h[i][e], cr[i].get(e));
+      }
+      if (MODE != QUANT) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.s = fmaf(h[i][e], h[i][e], v.s);
+        if (a.h && live && pos[i].lo < 8) {
+          Chunk<T> c;
+          c.set(h[i]);
+          c.store((S*)a.h + row * a.ldh + pos[i].start, pos[i].lo);
+        }
+        if (a.gamma) {
+          Chunk<F32> g;
+          g.load(a.gamma + pos[i].start);
+          if (MODE == NORM_I8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[i][e] = mul_rn(h[i][e], g.get(e));
+          }
+        }
+      }
+      if (MODE != NORM) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t u = __float_as_uint(h[i][e]) & 0x7fffffffu;
+          v.m = u > v.m ? u : v.m;
+        }
+      }
+    }
+    v = row_reduce<TPR>(v, buf, flip);
+    const float rstd = MODE == QUANT ? 1.0f : row_rstd(v.s, (float)a.cols, a.eps);
+    if (MODE == NORM) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        if (!live || pos[i].lo == 8) continue;
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = h[i][e] * rstd;
+        if (a.gamma) {
+          Chunk<F32> g;
+          g.load(a.gamma + pos[i].start);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] *= g.get(e);
+        }
+        Chunk<T> c;
+        c.set(y);
+        c.store((S*)a.y + row * a.ldy + pos[i].start, pos[i].lo);
+      }
+    } else {
+      const RowScale k = row_scale(v.m, MODE == NORM_I8 && !isfinite(v.s));
+      if (live && t == 0) a.scale[row] = MODE == QUANT ? k.scale : k.scale * rstd;
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        if (!live || pos[i].lo == 8) continue;
+        const uint32_t q0 = codes4(h[i][0], h[i][1], h[i][2], h[i][3], k.inv) & k.mask;
+        const uint32_t q1 = codes4(h[i][4], h[i][5], h[i][6], h[i][7], k.inv) & k.mask;
+        store_codes(a.q + row * a.ldq + pos[i].start, q0, q1, pos[i].lo);
+      }
+    }
+  }
+}
+
+// Rows of any length, element by element, read again for each use.  A thread
+// reads an element for the last time before it writes that element, so
+// outputs may lie in place of the inputs as in the kernel above.
+template <class T, int MODE>
+__global__ void __launch_bounds__(1024) row_long_kernel(RowArgs a) {
+  typedef typename T::storage S;
+  __shared__ SumMax buf[2][17];
+  int flip = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
+    const S* x = (const S*)a.x + row * a.ldx;
+    const S* res = MODE != QUANT && a.res ? (const S*)a.res + row * a.ldr : nullptr;
+    auto value = [&](int c) {
+      float h = to_f<T>(x[c]);
+      if (res) h = add_rn(h, to_f<T>(res[c]));
+      return h;
+    };
+    SumMax v = {0.0f, 0u};
+    for (int c = threadIdx.x; c < a.cols; c += 1024) {
+      float h = value(c);
+      if (MODE != QUANT) v.s = fmaf(h, h, v.s);
+      if (MODE == NORM_I8 && a.gamma) h = mul_rn(h, a.gamma[c]);
+      const uint32_t u = __float_as_uint(h) & 0x7fffffffu;
+      v.m = u > v.m ? u : v.m;
+    }
+    v = row_reduce<1024>(v, buf, flip);
+    const float rstd = MODE == QUANT ? 1.0f : row_rstd(v.s, (float)a.cols, a.eps);
+    const RowScale k = row_scale(v.m, MODE == NORM_I8 && !isfinite(v.s));
+    if (MODE != NORM && threadIdx.x == 0) a.scale[row] = MODE == QUANT ? k.scale : k.scale * rstd;
+    for (int c = threadIdx.x; c < a.cols; c += 1024) {
+      const float h = value(c);
+      if (MODE != QUANT && a.h) ((S*)a.h + row * a.ldh)[c] = from_f<T>(h);
+      if (MODE == NORM) {
+        float y = h * rstd;
+        if (a.gamma) y *= a.gamma[c];
+        ((S*)a.y + row * a.ldy)[c] = from_f<T>(y);
+      } else {
+        const float s = MODE == NORM_I8 && a.gamma ? mul_rn(h, a.gamma[c]) : h;
+        a.q[row * a.ldq + c] = (int8_t)(codes4(s, 0.0f, 0.0f, 0.0f, k.inv) & k.mask);
+      }
+    }
+  }
+}
+
+// One launch holds fewer than 2^32 threads: blocks beyond this many rows loop.
+constexpr int64_t MAX_BLOCKS = 1 << 20;
+
+template <class T, int MODE, int TPR, int NCH>
+void launch_rows(const RowArgs& a, hipStream_t st) {
+  constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
+  const int64_t blocks = ceil_div(a.rows, RPB);
+  hipLaunchKernelGGL((row_kernel<T, MODE, TPR, NCH>), dim3((unsigned)(blocks < MAX_BLOCKS ? blocks : MAX_BLOCKS)),
+                     dim3(NT), 0, st, a);
+}
+
+template <class T, int MODE>
+mdnn_status_t run_rows_t(const RowArgs& a, hipStream_t st) {
+  const int64_t nch = ceil_div(a.cols, 8);
+  if (a.cols < 8 || nch > 4096) {
+    const int64_t blocks = a.rows < MAX_BLOCKS ? a.rows : MAX_BLOCKS;
+    hipLaunchKernelGGL((row_long_kernel<T, MODE>), dim3((unsigned)blocks), dim3(1024), 0, st, a);
+  } else if (nch <= 16) {
+    launch_rows<T, MODE, 16, 1>(a, st);
+  } else if (nch <= 64) {
+    launch_rows<T, MODE, 64, 1>(a, st);
+  } else if (nch <= 256) {
+    launch_rows<T, MODE, 256, 1>(a, st);
+  } else if (nch <= 512) {
+    launch_rows<T, MODE, 256, 2>(a, st);
+  } else if (nch <= 1024) {
+    launch_rows<T, MODE, 256, 4>(a, st);
+  } else if (nch <= 2048) {
+    launch_rows<T, MODE, 1024, 2>(a, st);
+  } else {
+    launch_rows<T, MODE, 1024, 4>(a, st);
+  }
+  return check_launch("row_kernel");
+}
+
+template <int MODE>
+mdnn_status_t run_rows(const RowArgs& a, mdnn_dtype_t t, hipStream_t st) {
+  clear_error();
+  switch (t) {
+    case MDNN_F32: return run_rows_t<F32, MODE>(a, st);
+    case MDNN_F16: return run_rows_t<F16, MODE>(a, st);
+    default: return run_rows_t<BF16, MODE>(a, st);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// gradients of the norm
+//   g = dy * gamma, xh = h * rstd, c = mean(g * xh)
+//   dx = rstd * (g - xh * c) + dres,  dgamma = sum over rows of dy * xh
+// One reduction per row for sum h^2 and sum g * h together.  Each block walks
+// its rows and keeps the dgamma sums of its threads' columns in registers;
+// it writes them once, and the blocks' sums are added in a fixed order.
+// ---------------------------------------------------------------------------
+struct BwdArgs {
+  const void *dy, *h, *dres;  // dres: or null
+  const float* gamma;         // or null
+  void* dx;                   // or null
+  float* partial;             // [blocks][cols], or null
+  int64_t rows, lddy, ldh, lddr, lddx;
+  int32_t cols;
+  float eps;
+};
+
+template <class T, int TPR, int NCH>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_bwd_kernel(BwdArgs a) {
+  typedef typename T::storage S;
+  constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
+  __shared__ Sum2 buf[2][TPR / 64 + 1];
+  __shared__ float part[RPB > 1 ? RPB * TPR * NCH * 8 : 1];
+  const int t = threadIdx.x % TPR;
+  ChunkPos pos[NCH];
+  float dg[NCH][8];
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    pos[i] = chunk_pos(t + i * TPR, a.cols);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dg[i][e] = 0.0f;
+  }
+  int flip = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB, flip ^= 1) {
+    const int64_t rw = r0 + threadIdx.x / TPR;
+    const bool live = rw < a.rows;
+    const int64_t row = live ? rw : a.rows - 1;
+    Chunk<T> cd[NCH], ch[NCH], cr[NCH];
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      cd[i].load((const S*)a.dy + row * a.lddy + pos[i].start);
+      ch[i].load((const S*)a.h + row * a.ldh + pos[i].start);
+    }
+    if (a.dres) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) cr[i].load((const S*)a.dres + row * a.lddr + pos[i].start);
+    }
+    Sum2 v = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      Chunk<F32> g;
+      if (a.gamma) g.load(a.gamma + pos[i].start);
+      if (pos[i].lo > 0) ch[i].clear(pos[i].lo), cd[i].clear(pos[i].lo);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float h = ch[i].get(e), d = cd[i].get(e);
+        v.a = fmaf(h, h, v.a);
+        v.b = fmaf(a.gamma ? d * g.get(e) : d, h, v.b);
+      }
+    }
+    v = row_reduce<TPR>(v, buf, flip);
+    const float rstd = row_rstd(v.a, (float)a.cols, a.eps), c = rstd * v.b / (float)a.cols;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      if (!live || pos[i].lo == 8) continue;
+      Chunk<F32> g;
+      if (a.gamma) g.load(a.gamma + pos[i].start);
+      float o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float xh = ch[i].get(e) * rstd, d = cd[i].get(e);
+        o[e] = rstd * ((a.gamma ? d * g.get(e) : d) - xh * c);
+        if (a.dres) o[e] += cr[i].get(e);
+        dg[i][e] = fmaf(d, xh, dg[i][e]);
+      }
+      if (a.dx) {
+        Chunk<T> w;
+        w.set(o);
+        w.store((S*)a.dx + row * a.lddx + pos[i].start, pos[i].lo);
+      }
+    }
+  }
+  if (!a.partial) return;
+  float* out = a.partial + (int64_t)blockIdx.x * a.cols;
+  if constexpr (RPB > 1) {
+    // the block's row groups, added in their order
+#pragma unroll
+    for (int i = 0; i < NCH; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        part[(threadIdx.x / TPR) * (TPR * NCH * 8) + (t + i * TPR) * 8 + e] = dg[i][e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.cols; c += NT) {
+      // where column c lies: its chunk's slot, counted from the row's end in the last, partial chunk
+      const int k = c / 8, start = chunk_pos(k, a.cols).start;
+      float s = 0.0f;
+#pragma unroll
+      for (int r = 0; r < RPB; ++r) s += part[r * (TPR * NCH * 8) + k * 8 + (c - start)];
+      out[c] = s;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      if (pos[i].lo == 8) continue;
+      Chunk<F32> w;
+      w.set(dg[i]);
+      w.store(out + pos[i].start, pos[i].lo);
+    }
+  }
+}
+
+// Rows of any length: read twice, dgamma's sums kept in the block's own row
+// of the partials.
+template <class T>
+__global__ void __launch_bounds__(1024) norm_bwd_long_kernel(BwdArgs a) {
+  typedef typename T::storage S;
+  __shared__ Sum2 buf[2][17];
+  int flip = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
+    const S *dy = (const S*)a.dy + row * a.lddy, *hp = (const S*)a.h + row * a.ldh;
+    Sum2 v = {0.0f, 0.0f};
+    for (int c = threadIdx.x; c < a.cols; c += 1024) {
+      const float h = to_f<T>(hp[c]), d = to_f<T>(dy[c]);
+      v.a = fmaf(h, h, v.a);
+      v.b = fmaf(a.gamma ? d * a.gamma[c] : d, h, v.b);
+    }
+    v = row_reduce<1024>(v, buf, flip);
+    const float rstd = row_rstd(v.a, (float)a.cols, a.eps), k = rstd * v.b / (float)a.cols;
+    for (int c = threadIdx.x; c < a.cols; c += 1024) {
+      const float xh = to_f<T>(hp[c]) * rstd, d = to_f<T>(dy[c]);
+      float o = rstd * ((a.gamma ? d * a.gamma[c] : d) - xh * k);
+      if (a.dres) o += to_f<T>(((const S*)a.dres + row * a.lddr)[c]);
+      if (a.partial) {
+        float* p = a.partial + (int64_t)blockIdx.x * a.cols + c;
+        *p = row == (int64_t)blockIdx.x ? d * xh : fmaf(d, xh, *p);
+      }
+      if (a.dx) ((S*)a.dx + row * a.lddx)[c] = from_f<T>(o);
+    }
+  }
+}
+
+int bwd_rows_per_block(int64_t cols) {
+  const int64_t nch = ceil_div(cols, 8);
+  return cols < 8 || nch > 64 ? 1 : nch <= 16 ? 16 : 4;
+}
+// Blocks of the backward pass: by the sizes alone, so that the workspace and
+// the order of dgamma's sums are the same everywhere.
+int64_t bwd_blocks(int64_t rows, int64_t cols) {
+  const int64_t b = ceil_div(rows, bwd_rows_per_block(cols));
+  return b < 512 ? b : 512;
+}
+
+template <class T, int TPR, int NCH>
+void launch_bwd(const BwdArgs& a, int64_t blocks, hipStream_t st) {
+  hipLaunchKernelGGL((norm_bwd_kernel<T, TPR, NCH>), dim3((unsigned)blocks), dim3(TPR < 256 ? 256 : TPR), 0, st, a);
+}
+
+template <class T>
+mdnn_status_t run_bwd(const BwdArgs& a, hipStream_t st) {
+  const int64_t nch = ceil_div(a.cols, 8), blocks = bwd_blocks(a.rows, a.cols);
+  if (a.cols < 8 || nch > 2048)
+    hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3((unsigned)blocks), dim3(1024), 0, st, a);
+  else if (nch <= 16)
+    launch_bwd<T, 16, 1>(a, blocks, st);
+  else if (nch <= 64)
+    launch_bwd<T, 64, 1>(a, blocks, st);
+  else if (nch <= 256)
+    launch_bwd<T, 256, 1>(a, blocks, st);
+  else if (nch <= 512)
+    launch_bwd<T, 256, 2>(a, blocks, st);
+  else if (nch <= 1024)
+    launch_bwd<T, 512, 2>(a, blocks, st);
+  else
+    launch_bwd<T, 1024, 2>(a, blocks, st);
+  return check_launch("norm_bwd_kernel");
+}
+
+// ---------------------------------------------------------------------------
+// columns: codes of x[rows][cols] with a scale for each column, stored
+// transposed, q[cols][rows].  Pass 1: column maxima of row slabs; pass 2:
+// every tile takes its columns' maxima over the slabs, quantises and turns
+// the tile round in LDS (its second read of x is 64 KB of a matrix that the
+// last-level cache still holds).
+// ---------------------------------------------------------------------------
+constexpr int SLABS = 64;  // at most
+int64_t slab_rows(int64_t rows) {
+  const int64_t s = ceil_div(rows, SLABS);
+  return s < 32 ? 32 : s;
+}
+int64_t slab_count(int64_t rows) { return rows > 0 ? ceil_div(rows, slab_rows(rows)) : 0; }
+
+// Four consecutive elements of a row from column c, zero past the row.
+template <class T>
+__device__ __forceinline__ void load_quad(const typename T::storage* p, int64_t c, int64_t cols, float (&v)[4]) {
+  typedef uint32_t u2v_a2 __attribute__((ext_vector_type(2), aligned(2)));
+  if (c + 4 <= cols) {
+    if constexpr (sizeof(typename T::storage) == 2) {
+      const u2v_a2 w = *(const MDNN_GLOBAL u2v_a2*)(p + c);
+      v[0] = to_f<T>((uint16_t)w.x), v[1] = to_f<T>((uint16_t)(w.x >> 16));
+      v[2] = to_f<T>((uint16_t)w.y), v[3] = to_f<T>((uint16_t)(w.y >> 16));
+    } else {
+      const u4v_a4 w = *(const MDNN_GLOBAL u4v_a4*)(p + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(w[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? to_f<T>(p[c + e]) : 0.0f;
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256)
+colmax_kernel(const typename T::storage* x, int64_t ldx, int64_t rows, int64_t cols, int64_t per, uint32_t* partial) {
+  __shared__ uint32_t red[4][256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 256 + lane * 4;
+  const int64_t r0 = (int64_t)blockIdx.y * per, r1 = r0 + per < rows ? r0 + per : rows;
+  uint32_t m[4] = {0u, 0u, 0u, 0u};
+  if (c < cols)
+    for (int64_t r = r0 + wave; r < r1; r += 4) {
+      float v[4];
+      load_quad<T>(x + r * ldx, c, cols, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t u = __float_as_uint(v[e]) & 0x7fffffffu;
+        m[e] = u > m[e] ? u : m[e];
+      }
+    }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) red[wave][lane * 4 + e] = m[e];
+  __syncthreads();
+  const int64_t co = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (co >= cols) return;
+  uint32_t v = red[0][threadIdx.x];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) v = red[w][threadIdx.x] > v ? red[w][threadIdx.x] : v;
+  partial[(int64_t)blockIdx.y * cols + co] = v;
+}
+
+constexpr int QT_C = 64, QT_R = 128;  // tile: columns, rows
+template <class T>
+__global__ void __launch_bounds__(256)
+quant_t_kernel(const typename T::storage* x, int64_t ldx, int64_t rows, int64_t cols, const uint32_t* partial,
+               int slabs, int8_t* q, int64_t ldq, float* scale) {
+  __shared__ uint32_t top[4][QT_C];
+  __shared__ float inv[QT_C];
+  __shared__ uint32_t mask[QT_C];
+  __shared__ uint32_t tile[QT_C][QT_R / 4 + 1];
+  const int tid = threadIdx.x;
+  const int64_t c0 = (int64_t)blockIdx.x * QT_C;
+  {
+    const int c = tid & 63, part = tid >> 6;
+    uint32_t m = 0u;
+    if (c0 + c < cols)
+      for (int s = part; s < slabs; s += 4) {
+        const uint32_t u = partial[(int64_t)s * cols + c0 + c];
+        m = u > m ? u : m;
+      }
+    top[part][c] = m;
+  }
+  __syncthreads();
+  if (tid < QT_C) {
+    uint32_t m = top[0][tid];
+#pragma unroll
+    for (int p = 1; p < 4; ++p) m = top[p][tid] > m ? top[p][tid] : m;
+    const RowScale k = row_scale(m, false);
+    inv[tid] = k.inv;
+    mask[tid] = k.mask;
+    if (blockIdx.y == 0 && c0 + tid < cols) scale[c0 + tid] = k.scale;
+  }
+  __syncthreads();
+  for (int64_t r0 = (int64_t)blockIdx.y * QT_R; r0 < rows; r0 += (int64_t)gridDim.y * QT_R) {
+    // 4 x 4 blocks: four rows' quads become one word of four rows per column
+    const int cq = (tid & 15) * 4;
+#pragma unroll
+    for (int p = 0; p < QT_R / 64; ++p) {
+      const int rq = (tid >> 4) + p * 16;  // row quad
+      float v[4][4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t r = r0 + rq * 4 + e;
+        if (r < rows) {
+          load_quad<T>(x + r * ldx, c0 + cq, cols, v[e]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[e][j] = 0.0f;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        tile[cq + j][rq] = codes4(v[0][j], v[1][j], v[2][j], v[3][j], inv[cq + j]) & mask[cq + j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < QT_C * (QT_R / 4) / 256; ++p) {
+      const int idx = tid + p * 256, c = idx / (QT_R / 4), w = idx % (QT_R / 4);
+      const int64_t r = r0 + w * 4;
+      if (c0 + c >= cols || r >= rows) continue;
+      typedef uint32_t u1_a1 __attribute__((aligned(1)));
+      int8_t* o = q + (c0 + c) * ldq + r;
+      const uint32_t v = tile[c][w];
+      if (r + 4 <= rows) {
+        *(MDNN_GLOBAL u1_a1*)o = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (r + e < rows) o[e] = (int8_t)(v >> (8 * e));
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <class T>
+mdnn_status_t run_quant_t(int64_t rows, int64_t cols, const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale,
+                          uint32_t* partial, hipStream_t st) {
+  typedef typename T::storage S;
+  const int64_t slabs = slab_count(rows);
+  if (slabs > 0) {
+    hipLaunchKernelGGL(colmax_kernel<T>, dim3((unsigned)ceil_div(cols, 256), (unsigned)slabs), dim3(256), 0, st,
+                       (const S*)x, ldx, rows, cols, slab_rows(rows), partial);
+    MDNN_TRY(check_launch("colmax_kernel"));
+  }
+  int64_t gy = ceil_div(rows, QT_R);
+  gy = gy < 1 ? 1 : gy > 4096 ? 4096 : gy;
+  hipLaunchKernelGGL(quant_t_kernel<T>, dim3((unsigned)ceil_div(cols, QT_C), (unsigned)gy), dim3(256), 0, st,
+                     (const S*)x, ldx, rows, cols, partial, (int)slabs, q, ldq, scale);
+  return check_launch("quant_t_kernel");
+}
+
+constexpr int64_t MAX_COLS = (int64_t)1 << 29;  // 32-bit column indices; a launch holds fewer than 2^32 threads a dimension
+
+bool eps_ok(float eps) { return eps > 0.0f && std::isfinite(eps); }
+
+}  // namespace
+}  // namespace mdnn
+
+using namespace mdnn;
+
+extern "C" mdnn_status_t mdnn_quantize_i8(int64_t rows, int64_t cols, const void* x, int64_t ldx, mdnn_dtype_t x_type,
+                                          int8_t* q, int64_t ldq, float* scale, mdnn_stream_t stream) {
+  if (rows < 0 || cols < 0 || cols > MAX_COLS) return fail(MDNN_ERR_SHAPE, "quantize_i8: bad size");
+  if (!dtype_ok(x_type)) return fail(MDNN_ERR_DTYPE, "quantize_i8: unknown dtype");
+  if (rows == 0) return MDNN_SUCCESS;
+  if (!scale || (cols > 0 && (!x || !q))) return fail(MDNN_ERR_NULL, "quantize_i8: NULL buffer");
+  if (ldx < cols || ldq < cols) return fail(MDNN_ERR_LAYOUT, "quantize_i8: leading dimension below the width");
+  if (!aligned(x, dtype_size(x_type)) || !aligned(scale, 4))
+    return fail(MDNN_ERR_MISALIGNED, "quantize_i8: misaligned buffer");
+  RowArgs a = {};
+  a.x = x, a.q = q, a.scale = scale, a.rows = rows, a.cols = (int32_t)cols, a.ldx = ldx, a.ldq = ldq;
+  return run_rows<QUANT>(a, x_type, as_stream(stream));
+}
+
+extern "C" size_t mdnn_quantize_i8_t_workspace(int64_t rows, int64_t cols) {
+  if (rows < 0 || cols < 0 || cols > MAX_COLS) return 0;
+  return (size_t)slab_count(rows) * (size_t)cols * 4;
+}
+
+extern "C" mdnn_status_t mdnn_quantize_i8_t(int64_t rows, int64_t cols, const void* x, int64_t ldx,
+                                            mdnn_dtype_t x_type, int8_t* q, int64_t ldq, float* scale, void* workspace,
+                                            size_t ws_bytes, mdnn_stream_t stream) {
+  if (rows < 0 || cols < 0 || cols > MAX_COLS) return fail(MDNN_ERR_SHAPE, "quantize_i8_t: bad size");
+  if (!dtype_ok(x_type)) return fail(MDNN_ERR_DTYPE, "quantize_i8_t: unknown dtype");
+  if (cols == 0) return MDNN_SUCCESS;
+  if (!scale || (rows > 0 && (!x || !q))) return fail(MDNN_ERR_NULL, "quantize_i8_t: NULL buffer");
+  if (ldx < cols || ldq < rows) return fail(MDNN_ERR_LAYOUT, "quantize_i8_t: leading dimension below the width");
+  if (!aligned(x, dtype_size(x_type)) || !aligned(scale, 4))
+    return fail(MDNN_ERR_MISALIGNED, "quantize_i8_t: misaligned buffer");
+  const size_t need = mdnn_quantize_i8_t_workspace(rows, cols);
+  if (need > 0 && (!workspace || ws_bytes < need || !aligned(workspace, 16)))
+    return fail(MDNN_ERR_WORKSPACE, "quantize_i8_t: workspace of %zu bytes (16-byte aligned) required", need);
+  clear_error();
+  const hipStream_t st = as_stream(stream);
+  switch (x_type) {
+    case MDNN_F32: return run_quant_t<F32>(rows, cols, x, ldx, q, ldq, scale, (uint32_t*)workspace, st);
+    case MDNN_F16: return run_quant_t<F16>(rows, cols, x, ldx, q, ldq, scale, (uint32_t*)workspace, st);
+    default: return run_quant_t<BF16>(rows, cols, x, ldx, q, ldq, scale, (uint32_t*)workspace, st);
+  }
+}
+
+// Checks and arguments that both forward norms share.
+static mdnn_status_t norm_args(const char* who, RowArgs& a, int64_t rows, int64_t cols, const void* x, int64_t ldx,
+                               const void* residual, int64_t ldr, const float* gamma, float eps, void* h, int64_t ldh,
+                               mdnn_dtype_t dtype) {
+  if (rows < 0 || cols < 1 || cols > MAX_COLS) return fail(MDNN_ERR_SHAPE, "%s: bad size", who);
+  if (!eps_ok(eps)) return fail(MDNN_ERR_SHAPE, "%s: eps must be positive and finite", who);
+  if (!dtype_ok(dtype)) return fail(MDNN_ERR_DTYPE, "%s: unknown dtype", who);
+  if (rows == 0) return MDNN_SUCCESS;
+  if (!x) return fail(MDNN_ERR_NULL, "%s: x is NULL", who);
+  if (ldx < cols || (residual && ldr < cols) || (h && ldh < cols))
+    return fail(MDNN_ERR_LAYOUT, "%s: leading dimension below the width", who);
+  const size_t es = dtype_size(dtype);
+  if (!aligned(x, es) || !aligned(residual, es) || !aligned(h, es) || !aligned(gamma, 4))
+    return fail(MDNN_ERR_MISALIGNED, "%s: misaligned buffer", who);
+  a = {};
+  a.x = x, a.res = residual, a.gamma = gamma, a.h = h, a.rows = rows, a.cols = (int32_t)cols;
+  a.ldx = ldx, a.ldr = ldr, a.ldh = ldh, a.eps = eps;
+  return MDNN_SUCCESS;
+}
+
+extern "C" mdnn_status_t mdnn_rmsnorm_fwd(int64_t rows, int64_t cols, const void* x, int64_t ldx,
+                                          const void* residual, int64_t ldr, const float* gamma, float eps, void* h,
+                                          int64_t ldh, void* y, int64_t ldy, mdnn_dtype_t dtype,
+                                          mdnn_stream_t stream) {
+  RowArgs a;
+  MDNN_TRY(norm_args("rmsnorm_fwd", a, rows, cols, x, ldx, residual, ldr, gamma, eps, h, ldh, dtype));
+  if (rows == 0) return MDNN_SUCCESS;
+  if (!y) return fail(MDNN_ERR_NULL, "rmsnorm_fwd: y is NULL");
+  if (ldy < cols) return fail(MDNN_ERR_LAYOUT, "rmsnorm_fwd: leading dimension below the width");
+  if (!aligned(y, dtype_size(dtype))) return fail(MDNN_ERR_MISALIGNED, "rmsnorm_fwd: misaligned buffer");
+  a.y = y, a.ldy = ldy;
+  return run_rows<NORM>(a, dtype, as_stream(stream));
+}
+
+extern "C" mdnn_status_t mdnn_rmsnorm_i8_fwd(int64_t rows, int64_t cols, const void* x, int64_t ldx,
+                                             const void* residual, int64_t ldr, const float* gamma, float eps, void* h,
+                                             int64_t ldh, int8_t* q, int64_t ldq, float* scale, mdnn_dtype_t dtype,
+                                             mdnn_stream_t stream) {
+  RowArgs a;
+  MDNN_TRY(norm_args("rmsnorm_i8_fwd", a, rows, cols, x, ldx, residual, ldr, gamma, eps, h, ldh, dtype));
+  if (rows == 0) return MDNN_SUCCESS;
+  if (!q || !scale) return fail(MDNN_ERR_NULL, "rmsnorm_i8_fwd: q or scale is NULL");
+  if (ldq < cols) return fail(MDNN_ERR_LAYOUT, "rmsnorm_i8_fwd: leading dimension below the width");
+  if (!aligned(scale, 4)) return fail(MDNN_ERR_MISALIGNED, "rmsnorm_i8_fwd: misaligned buffer");
+  a.q = q, a.ldq = ldq, a.scale = scale;
+  return run_rows<NORM_I8>(a, dtype, as_stream(stream));
+}
+
+extern "C" size_t mdnn_rmsnorm_bwd_workspace(int64_t rows, int64_t cols) {
+  if (rows <= 0 || cols < 1 || cols > MAX_COLS) return 0;
+  // the blocks' sums, then the column sums' own workspace
+  const int64_t b = bwd_blocks(rows, cols);
+  return (((size_t)b * (size_t)cols * 4 + 255) & ~(size_t)255) + column_sums_ws_bytes(b, cols);
+}
+
+extern "C" mdnn_status_t mdnn_rmsnorm_bwd(int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* h,
+                                          int64_t ldh, const float* gamma, float eps, const void* dres, int64_t lddr,
+                                          void* dx, int64_t lddx, float* dgamma, mdnn_dtype_t dtype, void* workspace,
+                                          size_t ws_bytes, mdnn_stream_t stream) {
+  if (rows < 0 || cols < 1 || cols > MAX_COLS) return fail(MDNN_ERR_SHAPE, "rmsnorm_bwd: bad size");
+  if (!eps_ok(eps)) return fail(MDNN_ERR_SHAPE, "rmsnorm_bwd: eps must be positive and finite");
+  if (!dtype_ok(dtype)) return fail(MDNN_ERR_DTYPE, "rmsnorm_bwd: unknown dtype");
+  if (dgamma && !aligned(dgamma, 4)) return fail(MDNN_ERR_MISALIGNED, "rmsnorm_bwd: misaligned buffer");
+  const hipStream_t st = as_stream(stream);
+  if (rows == 0) {
+    clear_error();
+    return dgamma ? fill_zero(dgamma, (size_t)cols * 4, st) : MDNN_SUCCESS;
+  }
+  if (!dx && !dgamma) return MDNN_SUCCESS;
+  if (!dy || !h) return fail(MDNN_ERR_NULL, "rmsnorm_bwd: dy or h is NULL");
+  if (lddy < cols || ldh < cols || (dres && lddr < cols) || (dx && lddx < cols))
+    return fail(MDNN_ERR_LAYOUT, "rmsnorm_bwd: leading dimension below the width");
+  const size_t es = dtype_size(dtype);
+  if (!aligned(dy, es) || !aligned(h, es) || !aligned(dres, es) || !aligned(dx, es) || !aligned(gamma, 4))
+    return fail(MDNN_ERR_MISALIGNED, "rmsnorm_bwd: misaligned buffer");
+  const size_t need = dgamma ? mdnn_rmsnorm_bwd_workspace(rows, cols) : 0;
+  if (need > 0 && (!workspace || ws_bytes < need || !aligned(workspace, 256)))
+    return fail(MDNN_ERR_WORKSPACE, "rmsnorm_bwd: workspace of %zu bytes (256-byte aligned) required", need);
+  clear_error();
+  BwdArgs a = {};
+  a.dy = dy, a.h = h, a.dres = dres, a.gamma = gamma, a.dx = dx, a.partial = dgamma ? (float*)workspace : nullptr;
+  a.rows = rows, a.lddy = lddy, a.ldh = ldh, a.lddr = lddr, a.lddx = lddx, a.cols = (int32_t)cols, a.eps = eps;
+  switch (dtype) {
+    case MDNN_F32: MDNN_TRY(run_bwd<F32>(a, st)); break;
+    case MDNN_F16: MDNN_TRY(run_bwd<F16>(a, st)); break;
+    default: MDNN_TRY(run_bwd<BF16>(a, st)); break;
+  }
+  if (!dgamma) return MDNN_SUCCESS;
+  const int64_t b = bwd_blocks(rows, cols);
+  const size_t used = ((size_t)b * (size_t)cols * 4 + 255) & ~(size_t)255;
+  return column_sums(workspace, nullptr, MDNN_F32, b, cols, dgamma, (char*)workspace + used, need - used, st);
+}

@@ -1,0 +1,303 @@
+"""Root-mean-square norm, its 8-bit output and its gradients against the oracle
+in 64 bits.
+
+Tolerances, with u = 2^-24: a sum of a row's n terms is taken by at most 1024
+threads, each adding ceil(n / 1024) + 32 terms at most, and combined in a tree
+and a chain of at most 22 more; with the roundings of the terms themselves
+every sum is within S(n) = (64 + n / 1024) u of the sum of its terms'
+magnitudes.  1 / rms is then within S / 2 + 6 u (mean, eps, root, quotient),
+and each product rounds once."""
+import numpy as np
+import pytest
+
+from oracle import rowwise as R
+from tests.helpers import dev, host64
+from tests.test_gpu_int8 import COLS, GUARD, HALF, TINY, U, _code_room, _special, _t, _untouched, _values
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+
+
+def _sum_bound(n):
+    return (64 + n / 1024) * U
+
+
+def _gamma(cols, seed=1):
+    return (1 + 0.2 * np.random.default_rng(seed).standard_normal(cols)).astype(np.float32)
+
+
+def _room(rows, cols, dtype, pad, offset):
+    import torch
+    base = torch.full((offset + rows * (cols + pad),), 1e3, dtype=_t(dtype), device="cuda")
+    return base, base[offset:].view(rows, cols + pad)[:, :cols]
+
+
+def _kept(base, view):
+    keep = base.clone()
+    keep.as_strided(view.shape, view.stride(), view.storage_offset()).fill_(1e3)
+    return bool((keep == 1e3).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("cols", COLS)
+def test_norm(mdnn, cols, dtype):
+    gamma = _gamma(cols)
+    for rows, pad, offset, with_res, with_gamma in ((1, 0, 0, True, True), (5, 3, 1, True, True), (35, 0, 0, False, True),
+                                                    (18, 8, 0, True, False)):
+        x, xv = _values(rows, cols, cols + rows, dtype, pad, offset)
+        res, rv = _values(rows, cols, cols + rows + 1, dtype, pad, offset)
+        xv[rows // 2], rv[rows // 2] = 0, 0
+        x[rows // 2], res[rows // 2] = 0, 0
+        g = gamma if with_gamma else np.ones(cols, np.float32)
+        base, y = _room(rows, cols, dtype, pad, offset)
+        hbase, h = _room(rows, cols, dtype, pad, offset)
+        mdnn.rmsnorm(x, dev(gamma, "f32") if with_gamma else None, res if with_res else None, EPS,
+                     h_out=h if with_res else None, out=y)
+        hv = xv.astype(np.float64) + (rv.astype(np.float64) if with_res else 0.0)
+        want = R.rmsnorm(hv, g, EPS)
+        k = _sum_bound(cols) / 2 + 9 * U
+        assert (np.abs(host64(y) - want) <= (k + 1.001 * HALF[dtype]) * np.abs(want) + TINY[dtype]).all()
+        assert _kept(base, y)
+        if with_res:
+            assert (np.abs(host64(h) - hv) <= (1.001 * HALF[dtype] + U) * np.abs(hv) + TINY[dtype]).all()
+            assert _kept(hbase, h)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("cols", COLS)
+def test_norm_codes(mdnn, cols, dtype):
+    gamma = _gamma(cols)
+    for rows, pad, offset, with_res, with_gamma in ((1, 0, 0, True, True), (5, 3, 1, True, True), (35, 0, 0, False, True),
+                                                    (18, 8, 0, True, False)):
+        x, xv = _values(rows, cols, cols + rows, dtype, pad, offset)
+        res, rv = _values(rows, cols, cols + rows + 1, dtype, pad, offset)
+        base, q = _code_room(rows, cols, cols + pad, offset)
+        hbase, h = _room(rows, cols, dtype, pad, offset)
+        out = mdnn.rmsnorm_i8(x, dev(gamma, "f32") if with_gamma else None, res if with_res else None, EPS,
+                              h_out=h if with_res else None, q=q)
+        rq, rs = R.rmsnorm_codes(xv, rv if with_res else None, gamma if with_gamma else None, EPS)
+        assert (q.cpu().numpy() == rq).all()
+        assert (np.abs(host64(out[1]) - rs) <= (_sum_bound(cols) / 2 + 8 * U) * rs).all()
+        assert _untouched(base, q)
+        if with_res:
+            hv = xv.astype(np.float64) + rv
+            assert (np.abs(host64(h) - hv) <= (1.001 * HALF[dtype] + U) * np.abs(hv) + TINY[dtype]).all()
+            assert _kept(hbase, h)
+
+
+@pytest.mark.parametrize("cols", [5, 9, 130, 1000, 3000, 40000])
+def test_norm_special_rows(mdnn, cols):
+    """Rows with Inf or NaN, or whose squares overflow: all NaN, codes 0 and scale NaN; rows of nothing: zeros."""
+    import torch
+    v = _special(cols)
+    x, gamma = torch.from_numpy(v).cuda(), torch.ones(cols, device="cuda")
+    y = mdnn.rmsnorm(x, gamma, eps=EPS).cpu().numpy()
+    q, s = (t.cpu().numpy() for t in mdnn.rmsnorm_i8(x, gamma, eps=EPS))
+    bad = [0, 1, 2, 6, 10]
+    for r in range(12):
+        assert np.isnan(y[r]).all() == (r in bad) and np.isnan(y[r]).any() == (r in bad)
+        assert np.isnan(s[r]) == (r in bad)
+    assert (q[bad] == 0).all() and (q[3] == 0).all() and (q[8] == 0).all()
+    assert (y[3] == 0).all() and (y[8] == 0).all()
+    ok = [r for r in range(12) if r not in bad]
+    rq, _ = R.codes(v[ok])
+    assert (q[ok] == rq).all()
+    # h * gamma overflows though h does not: the codes have no scale
+    x = torch.full((2, cols), 1e10, device="cuda")
+    gamma[cols - 1] = 1e30
+    q, s = mdnn.rmsnorm_i8(x, gamma, eps=EPS)
+    assert bool(s.isnan().all()) and bool((q == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("cols", COLS)
+def test_gradients(mdnn, cols, dtype):
+    import torch
+    gamma = _gamma(cols)
+    for rows, pad, offset, with_res, with_gamma in ((1, 0, 0, True, True), (5, 3, 1, True, True), (35, 0, 0, False, True),
+                                                    (18, 8, 0, True, False), (1100, 0, 0, True, True)):
+        if rows * cols > 1 << 22:
+            continue
+        h, hv = _values(rows, cols, cols + rows, dtype, pad, offset)
+        dy, dv = _values(rows, cols, cols + rows + 1, dtype, pad, offset)
+        dr, rv = _values(rows, cols, cols + rows + 2, dtype, pad, offset)
+        hv[rows // 2] = 0
+        h[rows // 2] = 0
+        g = gamma if with_gamma else np.ones(cols, np.float32)
+        base, dx = _room(rows, cols, dtype, pad, offset)
+        _, dg = mdnn.rmsnorm_bwd(dy, h, dev(gamma, "f32") if with_gamma else None, EPS, dr if with_res else None, dx=dx)
+        want, want_g = R.rmsnorm_bwd(dv, hv, g, EPS, rv if with_res else None)
+        hv, dv, g = hv.astype(np.float64), dv.astype(np.float64), g.astype(np.float64)
+        r = 1 / np.sqrt(np.mean(hv * hv, axis=1, keepdims=True) + EPS)
+        # the terms' magnitudes, each within two sums' error (rms and mean) and a few roundings
+        size = r * (np.abs(g * dv) + np.abs(hv * r) * np.mean(np.abs(g * dv * hv * r), axis=1, keepdims=True))
+        size = size + (np.abs(rv) if with_res else 0.0)
+        tol = (2 * _sum_bound(cols) + 12 * U) * size + 1.01 * HALF[dtype] * np.abs(want) + TINY[dtype]
+        assert (np.abs(host64(dx) - want) <= tol).all()
+        assert _kept(base, dx)
+        # a sum of `rows` terms in any order, each term within the rms' error
+        tol = ((rows + 8) * U + _sum_bound(cols) / 2 + 8 * U) * np.sum(np.abs(dv * hv * r), axis=0) + TINY["f32"]
+        assert (np.abs(host64(dg) - want_g) <= tol).all()
+
+
+def test_gradients_one_at_a_time(mdnn):
+    import torch
+    for rows, cols in ((700, 200), (33, 4096), (3, 20000)):
+        h, _ = _values(rows, cols, 1, "bf16")
+        dy, _ = _values(rows, cols, 2, "bf16")
+        dx, dg = mdnn.rmsnorm_bwd(dy, h)
+        only_x, none = mdnn.rmsnorm_bwd(dy, h, with_dgamma=False)
+        assert none is None and torch.equal(only_x, dx)
+        ws = torch.empty(mdnn.mdnn_rmsnorm_bwd_workspace(rows, cols), dtype=torch.uint8, device="cuda")
+        only_g = torch.empty_like(dg)
+        mdnn.mdnn_rmsnorm_bwd(rows, cols, dy, cols, h, cols, None, 1e-6, None, 0, None, 0, only_g, mdnn.BF16, ws,
+                              ws.numel())
+        assert torch.equal(only_g, dg)
+    dg = torch.ones(77, device="cuda")
+    mdnn.rmsnorm_bwd(torch.empty((0, 77), device="cuda"), torch.empty((0, 77), device="cuda"), dgamma=dg)
+    assert bool((dg == 0).all())
+
+
+def test_gradients_by_differences(mdnn):
+    """dx and dgamma against differences of the forward pass itself."""
+    import torch
+    rows, cols = 3, 19
+    g = torch.Generator(device="cuda").manual_seed(4)
+    h = torch.randn(rows, cols, generator=g, device="cuda")
+    dy = torch.randn(rows, cols, generator=g, device="cuda")
+    gamma = 1 + 0.2 * torch.randn(cols, generator=g, device="cuda")
+    dx, dg = mdnn.rmsnorm_bwd(dy, h, gamma, 1e-3)
+    # step 2^-7: the quotient's error is e^2 / 6 times third derivatives (of order 10 / r^3 with r about 1, times
+    # |dy| sums of order 10) plus rounding 2^-24 * sum |dy y| / e: below 0.02
+    e = 2.0 ** -7
+    loss = lambda a, b: float((dy.double() * mdnn.rmsnorm(a, b, eps=1e-3).double()).sum())
+    for i in range(rows):
+        for j in range(0, cols, 5):
+            d = torch.zeros_like(h)
+            d[i, j] = e
+            assert abs((loss(h + d, gamma) - loss(h - d, gamma)) / (2 * e) - float(dx[i, j])) <= 0.02
+    for j in range(cols):
+        d = torch.zeros_like(gamma)
+        d[j] = e
+        assert abs((loss(h, gamma + d) - loss(h, gamma - d)) / (2 * e) - float(dg[j])) <= 0.02
+
+
+@pytest.mark.parametrize("cols", [5, 100, 1000, 1531, 4096, 9000, 16392, 40000])
+def test_in_place(mdnn, cols):
+    """Outputs exactly in place of inputs give what separate ones do."""
+    import torch
+    for dtype in ("f32", "bf16"):
+        x, _ = _values(37, cols, 1, dtype)
+        res, _ = _values(37, cols, 2, dtype)
+        gamma = dev(_gamma(cols), "f32")
+        y, h = mdnn.rmsnorm(x, gamma, res, EPS)
+        q, s, h2 = mdnn.rmsnorm_i8(x, gamma, res, EPS)
+        dx, dg = mdnn.rmsnorm_bwd(x, res, gamma, EPS, y)
+        assert torch.equal(h, h2)
+        a, b = x.clone(), res.clone()
+        mdnn.rmsnorm(a, gamma, b, EPS, h_out=b, out=a)
+        assert torch.equal(a, y) and torch.equal(b, h)
+        a, b = x.clone(), res.clone()
+        mdnn.rmsnorm(a, gamma, b, EPS, h_out=a, out=b)
+        assert torch.equal(a, h) and torch.equal(b, y)
+        b = res.clone()
+        q2, s2, _ = mdnn.rmsnorm_i8(x, gamma, b, EPS, h_out=b)
+        assert torch.equal(q2, q) and torch.equal(s2, s) and torch.equal(b, h)
+        for k in range(3):
+            t = [x.clone(), res.clone(), y.clone()]
+            _, dg2 = mdnn.rmsnorm_bwd(t[0], t[1], gamma, EPS, t[2], dx=t[k])
+            assert torch.equal(t[k], dx) and torch.equal(dg2, dg)
+
+
+def test_deterministic_and_captured(mdnn):
+    """A training step's forward and backward norm, captured and replayed on new data."""
+    import torch
+    rows, cols = 700, 1531
+    x = torch.randn(rows, cols, device="cuda").bfloat16()
+    res, dy = torch.randn_like(x), torch.randn_like(x)
+    gamma = torch.rand(cols, device="cuda") + 0.5
+    y, h, dx = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    dg = torch.empty(cols, device="cuda")
+    ws = torch.empty(mdnn.mdnn_rmsnorm_bwd_workspace(rows, cols), dtype=torch.uint8, device="cuda")
+
+    def step():
+        mdnn.rmsnorm(x, gamma, res, EPS, h_out=h, out=y)
+        mdnn.rmsnorm_bwd(dy, h, gamma, EPS, y, dx=dx, dgamma=dg, workspace=ws)
+
+    step()
+    first = [t.clone() for t in (y, h, dx, dg)]
+    for _ in range(3):
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(first, (y, h, dx, dg)))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        x.copy_(torch.randn(rows, cols, device="cuda").bfloat16())
+        dy.copy_(torch.randn(rows, cols, device="cuda").bfloat16())
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (y, h, dx, dg)]
+        for t in (y, h, dx, dg):
+            t.zero_()
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(got, (y, h, dx, dg)))
+
+
+def test_many_rows(mdnn):
+    """More rows than one launch has blocks for."""
+    import torch
+    rows, cols = (1 << 20) * 16 + 5, 9
+    x = torch.randn(rows, cols, device="cuda").half()
+    y = mdnn.rmsnorm(x, None, eps=EPS)
+    q, s = mdnn.quantize_i8(x)
+    xf = x.double()
+    # in pieces, with the definition in 64 bits on the GPU
+    for lo in range(0, rows, 1 << 22):
+        p = xf[lo:lo + (1 << 22)]
+        want = p / torch.sqrt((p * p).mean(1, keepdim=True) + EPS)
+        err = (y[lo:lo + (1 << 22)].double() - want).abs()
+        assert bool((err <= (1.001 * HALF["f16"] + 80 * U) * want.abs() + TINY["f16"]).all())
+        a = p.abs().amax(1, keepdim=True).clamp(min=2.0 ** -100)
+        inv = (torch.full_like(a, 127.0) / a).float().double()
+        assert torch.equal(q[lo:lo + (1 << 22)], (p * inv).float().round().to(torch.int8))
+        assert torch.equal(s[lo:lo + (1 << 22)], (a / torch.full_like(a, 127.0)).float()[:, 0])
+
+
+def test_far_rows(mdnn):
+    """Rows whose offsets pass 2^32 bytes."""
+    import torch
+    cols, far = 700, 2 ** 31 + 24
+    base = torch.zeros(2 * far + cols, dtype=torch.bfloat16, device="cuda")
+    x = base.as_strided((3, cols), (far, 1))
+    v, vals = _values(3, cols, 3, "bf16")
+    x.copy_(v)
+    gamma = dev(_gamma(cols), "f32")
+    y, h = mdnn.rmsnorm(v, gamma, v, EPS)
+    q, s, _ = mdnn.rmsnorm_i8(v, gamma, v, EPS)
+    dx, dg = mdnn.rmsnorm_bwd(v, v, gamma, EPS, v)
+    y2, _ = mdnn.rmsnorm(x, gamma, x, EPS)
+    q2, s2, _ = mdnn.rmsnorm_i8(x, gamma, x, EPS)
+    dx2, dg2 = mdnn.rmsnorm_bwd(x, x, gamma, EPS, x)
+    for a, b in ((y, y2), (q, q2), (s, s2), (dx, dx2), (dg, dg2)):
+        assert torch.equal(a, b)
+    assert torch.equal(mdnn.quantize_i8(x)[0], mdnn.quantize_i8(v)[0])
+    assert torch.equal(mdnn.quantize_i8(x, transpose=True)[0], mdnn.quantize_i8(v, transpose=True)[0])
+    out = base.as_strided((3, cols), (far, 1))
+    mdnn.rmsnorm(x, gamma, x, EPS, h_out=out)
+    assert torch.equal(out, h)
+
+
+def test_api_refuses(mdnn):
+    import torch
+    x = torch.zeros((4, 32), device="cuda")
+    g = torch.ones(32, device="cuda")
+    for bad in (lambda: mdnn.rmsnorm(x.t(), g), lambda: mdnn.rmsnorm(x, g[:8]), lambda: mdnn.rmsnorm(x, g, x[:, :8]),
+                lambda: mdnn.rmsnorm(x, g, x.half()), lambda: mdnn.rmsnorm(x, g.half()), lambda: mdnn.rmsnorm(x.cpu(), g),
+                lambda: mdnn.rmsnorm_bwd(x, x[:2], g), lambda: mdnn.rmsnorm_bwd(x, None, g),
+                lambda: mdnn.rmsnorm_i8(x, g, q=torch.zeros((4, 32), device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(mdnn.MdnnError):
+        mdnn.rmsnorm(x, g, eps=0.0)
