@@ -165,6 +165,9 @@ def _p(x) -> Optional[int]:
 def _s(stream) -> Optional[int]:
     if stream is None:
         import torch
+        # (the same handle without a Stream object: 0.2 us a call instead of 2.8)
+        if torch.cuda.is_initialized():
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
