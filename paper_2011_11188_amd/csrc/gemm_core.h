@@ -656,12 +656,14 @@ __device__ __forceinline__ void epilogue_any(const Epilogue& ep, int64_t M, int6
 // ---------------------------------------------------------------------------
 template <class T> struct Mfma;
 template <> struct Mfma<F16> {
+  typedef float4_t Acc;
   static __device__ __forceinline__ float4_t run(uint4 a, uint4 b, float4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a),
                                                   __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
   }
 };
 template <> struct Mfma<BF16> {
+  typedef float4_t Acc;
   static __device__ __forceinline__ float4_t run(uint4 a, uint4 b, float4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8_t, a),
                                                    __builtin_bit_cast(bhalf8_t, b), c, 0, 0, 0);

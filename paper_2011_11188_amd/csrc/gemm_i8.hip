@@ -13,23 +13,32 @@
 #include "internal.h"
 
 namespace mdnn {
-namespace {
 
 typedef int int4v __attribute__((ext_vector_type(4)));
+struct I8 {
+  typedef int8_t storage;
+};
+template <> struct Mfma<I8> {
+  typedef int4v Acc;
+  static __device__ __forceinline__ int4v run(uint4 a, uint4 b, int4v c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(int4v, a), __builtin_bit_cast(int4v, b), c, 0, 0,
+                                                 0);
+  }
+};
+
+namespace {
 
 constexpr int BKB = 128;           // bytes of k per step
 constexpr int64_t I8_MAX_K = 131071;
-
-__device__ __forceinline__ int4v mfma_i8(uint4 a, uint4 b, int4v c) {
-  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(int4v, a), __builtin_bit_cast(int4v, b), c, 0, 0, 0);
-}
 
 struct I8Args {
   const int8_t *a, *b;
   const float *a_scale, *b_scale, *bias;  // bias: or null
   void* d;
   int64_t M, N, K, lda, ldb, ldd;
-  int32_t act;
+  int32_t act, d_type;
+  int32_t* partial;     // split K: sums [splits][M][N]; or null
+  int64_t k_per_split;  // a multiple of the step
 };
 
 // ------------------------------------------------------------- epilogue
@@ -79,7 +88,7 @@ __device__ __forceinline__ void store_i8(const I8Args& g, int64_t m, int64_t n, 
 
 // A wave's FM x FN fragments; mb, nb: this lane's first row and column.
 template <class OutT, int FM, int FN>
-__device__ __forceinline__ void epilogue_i8(const I8Args& g, int64_t mb, int64_t nb, const int4v (&acc)[FM][FN]) {
+__device__ __forceinline__ void epilogue_i8_t(const I8Args& g, int64_t mb, int64_t nb, const int4v (&acc)[FM][FN]) {
   float sa[FM], sb[FN][4], bias[FN][4];
 #pragma unroll
   for (int i = 0; i < FM; ++i) sa[i] = g.a_scale[mb + i * 16 < g.M ? mb + i * 16 : g.M - 1];
@@ -93,6 +102,36 @@ __device__ __forceinline__ void epilogue_i8(const I8Args& g, int64_t mb, int64_t
 #pragma unroll
     for (int j = 0; j < FN; ++j)
       if (mb + i * 16 < g.M && nb + j * 16 < g.N) store_i8<OutT>(g, mb + i * 16, nb + j * 16, acc[i][j], sa[i], sb[j], bias[j]);
+}
+
+template <int FM, int FN>
+__device__ __forceinline__ void epilogue_i8(const I8Args& g, int split, int64_t mb, int64_t nb,
+                                            const int4v (&acc)[FM][FN]) {
+  if (g.partial) {
+    int32_t* p = g.partial + (int64_t)split * g.M * g.N;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const int64_t m = mb + i * 16, n = nb + j * 16;
+        if (m >= g.M || n >= g.N) continue;
+        int32_t* o = p + m * g.N + n;
+        if (n + 4 <= g.N) {
+          typedef int int4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+          *(__attribute__((address_space(1))) int4_a4*)o = (int4_a4){acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (n + e < g.N) o[e] = acc[i][j][e];
+        }
+      }
+    return;
+  }
+  switch (g.d_type) {
+    case MDNN_F32: epilogue_i8_t<F32, FM, FN>(g, mb, nb, acc); break;
+    case MDNN_F16: epilogue_i8_t<F16, FM, FN>(g, mb, nb, acc); break;
+    default: epilogue_i8_t<BF16, FM, FN>(g, mb, nb, acc); break;
+  }
 }
 
 // ------------------------------------------------- register-staged kernel
@@ -120,7 +159,7 @@ __device__ __forceinline__ uint4 row_chunk(const int8_t* row, int64_t k, int64_t
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <class OutT, class TL>
+template <class TL>
 __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_any_kernel(I8Args g) {
   __shared__ __attribute__((aligned(1024))) char lds_a[2][TL::A_BYTES];
   __shared__ __attribute__((aligned(1024))) char lds_b[2][TL::B_BYTES];
@@ -186,19 +225,392 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_any_kernel(I8Args g) 
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mfma_i8(fb[j], fa[i], acc[i][j]);
+        for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa[i], acc[i][j]);
     }
   }
-  epilogue_i8<OutT, FM, FN>(g, m0 + wm * TL::WTM + (lane & 15), n0 + wn * TL::WTN + 4 * (lane >> 4), acc);
+  epilogue_i8<FM, FN>(g, 0, m0 + wm * TL::WTM + (lane & 15), n0 + wn * TL::WTN + 4 * (lane >> 4), acc);
 }
 
-typedef lds::Tile<64, 64, 2, 2, 4> TileI64;
+// ------------------------------------------------- direct-to-LDS kernel
+// 16-byte aligned rows (gemm_lds.h's pipeline): every lane's 16 bytes go
+// straight from memory to LDS.  A K that is no multiple of the step reads
+// through a range-checked buffer, whole 16-byte chunks past K as zeros; its
+// last K % 16 bytes are one more fragment step from registers.
+struct I8Operand {
+  const int8_t* p;
+  int64_t ld, MN, K;
+};
+template <int W, int L, bool RAGGED>
+struct I8Loader {
+  static constexpr bool KC = true, SPLIT_ISSUE = true;
+  static constexpr int P = L >= 2 ? 2 : 1;  // (a lane's k within a step depends on its load's parity)
+  const char* base;
+  lds::int4_t rsrc;
+  int32_t left[P];
+  uint32_t off[L];
 
-template <class OutT>
+  __device__ __forceinline__ void init(const I8Operand& a, int64_t mn0, int64_t kbeg, int wave, int lane) {
+    base = (const char*)a.p + mn0 * a.ld + kbeg;
+    const int32_t rows = a.MN - mn0 < W ? (int32_t)(a.MN - mn0) : W, ld = (int32_t)a.ld;
+    if constexpr (RAGGED) rsrc = lds::make_rsrc(base, (uint32_t)((rows - 1) * ld + (int32_t)(a.K - kbeg)));
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const lds::LoadPos q = lds::load_pos<true, W, L>(wave, lane, i);
+      const int32_t r = q.r < rows ? q.r : rows - 1;
+      off[i] = (uint32_t)(r * ld + q.c * 2);
+      if (i < P) left[i] = (int32_t)((a.K & ~(int64_t)15) - kbeg) - q.c * 2;
+    }
+  }
+  // a whole step (any but a ragged last one)
+  __device__ __forceinline__ void issue_one(int t, uint32_t dst, int i) {
+    lds::dma_global(base + (int64_t)t * BKB, off[i], dst + (uint32_t)i * 1024u);
+  }
+  __device__ __forceinline__ void issue(int t, uint32_t dst) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      if constexpr (RAGGED)
+        lds::dma_buffer(rsrc, t * BKB < left[i % P] ? off[i] + (uint32_t)t * BKB : lds::OOB, dst + (uint32_t)i * 1024u);
+      else
+        issue_one(t, dst, i);
+    }
+  }
+};
+// A tile's rows reach below 2^31 bytes: offsets of every lane and load.
+constexpr int64_t I8_MAX_LD = ((int64_t)1 << 31) / 256 - BKB;
+
+template <class TL, int NS, bool RAGGED>
+__global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_kernel(I8Args g) {
+  typedef I8Loader<TL::BM, TL::LA, RAGGED> LA;
+  typedef I8Loader<TL::BN, TL::LB, RAGGED> LB;
+  static_assert(NS >= 2 && NS <= 4, "2 to 4 stages");
+  static_assert(NS * (TL::A_BYTES + TL::B_BYTES) + 2 * (4 - NS) <= 160 * 1024, "LDS budget");
+  // (a stage an object: see gemm_lds_kernel)
+  __shared__ __attribute__((aligned(1024))) char lds_a0[TL::A_BYTES];
+  __shared__ __attribute__((aligned(1024))) char lds_b0[TL::B_BYTES];
+  __shared__ __attribute__((aligned(1024))) char lds_a1[TL::A_BYTES];
+  __shared__ __attribute__((aligned(1024))) char lds_b1[TL::B_BYTES];
+  __shared__ __attribute__((aligned(NS > 2 ? 1024 : 1))) char lds_a2[NS > 2 ? TL::A_BYTES : 1];
+  __shared__ __attribute__((aligned(NS > 2 ? 1024 : 1))) char lds_b2[NS > 2 ? TL::B_BYTES : 1];
+  __shared__ __attribute__((aligned(NS > 3 ? 1024 : 1))) char lds_a3[NS > 3 ? TL::A_BYTES : 1];
+  __shared__ __attribute__((aligned(NS > 3 ? 1024 : 1))) char lds_b3[NS > 3 ? TL::B_BYTES : 1];
+  char* const all_a[4] = {lds_a0, lds_a1, lds_a2, lds_a3};
+  char* const all_b[4] = {lds_b0, lds_b1, lds_b2, lds_b3};
+  lds::Stages<NS> st;
+#pragma unroll
+  for (int s = 0; s < NS; ++s) st.a[s] = all_a[s], st.b[s] = all_b[s];
+  constexpr int FM = TL::FM, FN = TL::FN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / TL::WN, wn = wave % TL::WN;
+  int tm, tn, split;
+  split_tile_coords(ceil_div(g.M, TL::BM), ceil_div(g.N, TL::BN), tm, tn, split);
+  const int64_t m0 = (int64_t)tm * TL::BM, n0 = (int64_t)tn * TL::BN;
+  int64_t kbeg = 0, kend = g.K;
+  if (g.partial) {
+    kbeg = (int64_t)split * g.k_per_split;
+    kend = kbeg + g.k_per_split < g.K ? kbeg + g.k_per_split : g.K;
+  }
+  // steps that hold a whole 16-byte chunk
+  const int nk = (int)ceil_div((kend & ~(int64_t)15) - kbeg, (int64_t)BKB);
+
+  LA la;
+  LB lb;
+  la.init(I8Operand{g.a, g.lda, g.M, g.K}, m0, kbeg, wave, lane);
+  lb.init(I8Operand{g.b, g.ldb, g.N, g.K}, n0, kbeg, wave, lane);
+  const uint32_t wa = (uint32_t)(wave * TL::LA) * 1024u, wb = (uint32_t)(wave * TL::LB) * 1024u;
+  int4v acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
+  lds::Frags<TL> f0, f1;
+  const lds::LaneFrag fa_l = lds::lane_frag<true, TL::BM>(lane), fb_l = lds::lane_frag<true, TL::BN>(lane);
+  if (nk > 0) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      if (s < nk) {
+        la.issue(s, lds::lds_address(st.a[s]) + wa);
+        lb.issue(s, lds::lds_address(st.b[s]) + wb);
+      }
+  }
+  const int64_t mb = m0 + wm * TL::WTM + (lane & 15), nr = n0 + wn * TL::WTN + (lane & 15);
+  if constexpr (RAGGED) {
+    if ((kend & 15) != 0) {  // the last bytes, as k 0 .. 15 of a step in the first 16 lanes, while the first tiles arrive
+      const int64_t k = kend & ~(int64_t)15;
+      uint4 fb[FN];
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const int64_t n = nr + j * 16 < g.N ? nr + j * 16 : g.N - 1;
+        fb[j] = lane < 16 ? row_chunk(g.b + n * g.ldb, k, g.K) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int64_t m = mb + i * 16 < g.M ? mb + i * 16 : g.M - 1;
+        const uint4 fa = lane < 16 ? row_chunk(g.a + m * g.lda, k, g.K) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa, acc[i][j]);
+      }
+    }
+  }
+  if (nk > 0) {
+    lds::wait_tiles<NS - 1, TL::LA + TL::LB>((nk < NS ? nk : NS) - 1);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < FM; ++i) f0.a[i] = lds::fragment<true, TL::BM>(st.a[0], wm * TL::WTM + i * 16, 0, fa_l);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) f0.b[j] = lds::fragment<true, TL::BN>(st.b[0], wn * TL::WTN + j * 16, 0, fb_l);
+  }
+  constexpr int U = NS % 2 == 0 ? NS : 2 * NS;
+  int t = 0;
+  for (; t + U - 1 + NS < nk - (RAGGED ? 1 : 0); t += U)  // (the last step is issued with its test)
+    lds::pipeline_round<I8, TL, NS, LA, LB, 0, U, false>(t, nk, st, wave, fa_l, fb_l, wm, wn, la, lb, f0, f1, acc);
+  for (; t < nk; t += U)
+    lds::pipeline_round<I8, TL, NS, LA, LB, 0, U, true>(t, nk, st, wave, fa_l, fb_l, wm, wn, la, lb, f0, f1, acc);
+
+  epilogue_i8<FM, FN>(g, split, mb, n0 + wn * TL::WTN + 4 * (lane >> 4), acc);
+}
+
+// ------------------------------------------------------- few rows kernel
+// At most 64 rows (one to a few samples): the time is B's read.  A block owns
+// FN * 16 columns and its eight waves share K; each wave reads its piece of
+// the operands straight into MFMA fragments (16 bytes of one row a lane, any
+// address), UN steps of 64 k in flight, and the waves' sums are added in LDS.
+constexpr int FEW_WAVES = 8;
+template <int FM, int FN, int UN>
+__global__ void __launch_bounds__(FEW_WAVES * 64) gemm_i8_few_kernel(I8Args g) {
+  static_assert(FM * FN <= FEW_WAVES, "a wave per fragment of the result");
+  __shared__ int4v part[FEW_WAVES][FM * FN][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = (int64_t)blockIdx.x * (FN * 16);
+  const int8_t *ra[FM], *rb[FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int64_t m = i * 16 + (lane & 15);
+    ra[i] = g.a + (m < g.M ? m : g.M - 1) * g.lda + 16 * (lane >> 4);
+  }
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
+    const int64_t n = n0 + j * 16 + (lane & 15);
+    rb[j] = g.b + (n < g.N ? n : g.N - 1) * g.ldb + 16 * (lane >> 4);
+  }
+  // this wave's steps of 64 k
+  const int steps = (int)ceil_div(g.K, 64), per = (int)ceil_div(steps, FEW_WAVES);
+  const int s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps, full = (int)(g.K / 64);
+  int4v acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
+  int s = s0;
+  for (; s + UN <= s1 && s + UN <= full; s += UN) {
+    uint4 fb[UN][FN], fa[UN][FM];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[u][j] = load_bytes(rb[j] + (int64_t)(s + u) * 64);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[u][i] = load_bytes(ra[i] + (int64_t)(s + u) * 64);
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[u][j], fa[u][i], acc[i][j]);
+  }
+  for (; s < s1; ++s) {  // (row_chunk counts k from the row's start)
+    const int64_t k = (int64_t)s * 64 + 16 * (lane >> 4);
+    uint4 fa[FM], fb[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fb[j] = row_chunk(rb[j] - 16 * (lane >> 4), k, g.K);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) fa[i] = row_chunk(ra[i] - 16 * (lane >> 4), k, g.K);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa[i], acc[i][j]);
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) part[wave][i * FN + j][lane] = acc[i][j];
+  __syncthreads();
+  if (wave >= FM * FN) return;
+  int4v sum[1][1] = {{part[0][wave][lane]}};
+#pragma unroll
+  for (int w = 1; w < FEW_WAVES; ++w) sum[0][0] += part[w][wave][lane];
+  epilogue_i8<1, 1>(g, 0, wave / FN * 16 + (lane & 15), n0 + wave % FN * 16 + 4 * (lane >> 4), sum);
+}
+
+// The same for 16-byte aligned rows: a wave's pieces go straight to LDS of its
+// own (whole 128-byte lines of a row per eight lanes; fragments read from
+// memory touch four rows in every four lanes, which the cache answers a line
+// at a time), NS steps of 128 k in flight and no barrier before the sums.
+template <int FM, int FN, int W, int NS>
+__global__ void __launch_bounds__(W * 64) gemm_i8_few_lds_kernel(I8Args g) {
+  constexpr int A_BYTES = FM * 2048, B_BYTES = FN * 2048, STAGE = A_BYTES + B_BYTES, LPT = 2 * (FM + FN);
+  constexpr int ALL = W * NS * STAGE, SUMS = W * FM * FN * 1024;
+  static_assert(ALL <= 160 * 1024 && SUMS <= 160 * 1024, "LDS budget");
+  __shared__ __attribute__((aligned(1024))) char mem[ALL > SUMS ? ALL : SUMS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = (int64_t)blockIdx.x * (FN * 16), m0 = (int64_t)blockIdx.y * (FM * 16);
+  const int steps = (int)ceil_div(g.K & ~(int64_t)15, (int64_t)BKB), per = (int)ceil_div(steps, W);
+  const int s0 = wave * per < steps ? wave * per : steps, nk = (s0 + per < steps ? s0 + per : steps) - s0;
+  const int64_t kbeg = (int64_t)s0 * BKB;
+  I8Loader<FM * 16, 2 * FM, true> la;
+  I8Loader<FN * 16, 2 * FN, true> lb;
+  la.init(I8Operand{g.a, g.lda, g.M, g.K}, m0, kbeg, 0, lane);
+  lb.init(I8Operand{g.b, g.ldb, g.N, g.K}, n0, kbeg, 0, lane);
+  char* const own = mem + wave * (NS * STAGE);
+  const uint32_t at = lds::lds_address(own);
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+    if (s < nk) {
+      lb.issue(s, at + s * STAGE + A_BYTES);
+      la.issue(s, at + s * STAGE);
+    }
+  int4v acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
+  if (wave == W - 1 && (g.K & 15) != 0) {  // the last bytes (see gemm_i8_kernel)
+    const int64_t k = g.K & ~(int64_t)15;
+    uint4 fb[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const int64_t n = n0 + j * 16 + lane < g.N ? n0 + j * 16 + lane : g.N - 1;
+      fb[j] = lane < 16 ? row_chunk(g.b + n * g.ldb, k, g.K) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int64_t m = m0 + i * 16 + lane < g.M ? m0 + i * 16 + lane : g.M - 1;
+      const uint4 fa = lane < 16 ? row_chunk(g.a + m * g.lda, k, g.K) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa, acc[i][j]);
+    }
+  }
+  const lds::LaneFrag fl = lds::lane_frag<true, 64>(lane);
+  for (int t = 0; t < nk; ++t) {
+    lds::wait_tiles<NS - 1, LPT>(nk - 1 - t < NS - 1 ? nk - 1 - t : NS - 1);  // this wave's step t has landed
+    asm volatile("" ::: "memory");
+    const char* sa = own + (t % NS) * STAGE;
+    uint4 fa[2][FM], fb[2][FN];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[kk][j] = lds::fragment<true, FN * 16>(sa + A_BYTES, j * 16, kk, fl);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[kk][i] = lds::fragment<true, FM * 16>(sa, i * 16, kk, fl);
+    }
+    if (t + NS < nk) {
+      // the fragments are in registers before their stage is filled again
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      lb.issue(t + NS, at + (t % NS) * STAGE + A_BYTES);
+      la.issue(t + NS, at + (t % NS) * STAGE);
+    }
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[kk][j], fa[kk][i], acc[i][j]);
+  }
+  __syncthreads();  // every wave is done with its stages
+  int4v* part = (int4v*)mem;  // [W][FM * FN][64]
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) part[(wave * FM * FN + i * FN + j) * 64 + lane] = acc[i][j];
+  __syncthreads();
+  for (int f = wave; f < FM * FN; f += W) {
+    int4v sum[1][1] = {{part[f * 64 + lane]}};
+#pragma unroll
+    for (int w = 1; w < W; ++w) sum[0][0] += part[(w * FM * FN + f) * 64 + lane];
+    epilogue_i8<1, 1>(g, 0, m0 + f / FN * 16 + (lane & 15), n0 + f % FN * 16 + 4 * (lane >> 4), sum);
+  }
+}
+
+typedef lds::Tile<64, 64, 2, 2, 2> TileI64;
+// 128 x 128 with three stages (96 KB), 256 x 128 with eight waves of 64 x 64
+// and three stages (144 KB): one workgroup per CU each
+typedef lds::Tile<128, 128, 2, 2, 1> TileI128;
+typedef lds::Tile<256, 128, 4, 2, 2> TileI256x128;
+
+// 16-byte aligned rows that the direct-to-LDS kernel takes.
+bool i8_aligned(const I8Args& g) {
+  return g.K >= 16 && aligned(g.a, 16) && aligned(g.b, 16) && g.lda % 16 == 0 && g.ldb % 16 == 0 &&
+         g.lda <= I8_MAX_LD && g.ldb <= I8_MAX_LD;
+}
+
+template <class TL, int NS>
+void launch_i8(const I8Args& g, int splits, hipStream_t st) {
+  const dim3 grid((unsigned)(ceil_div(g.M, TL::BM) * ceil_div(g.N, TL::BN)), (unsigned)splits);
+  if (g.K % BKB != 0)
+    hipLaunchKernelGGL((gemm_i8_kernel<TL, NS, true>), grid, dim3(TL::NT), 0, st, g);
+  else
+    hipLaunchKernelGGL((gemm_i8_kernel<TL, NS, false>), grid, dim3(TL::NT), 0, st, g);
+}
+
+template <int FM, int FN, int UN>
+mdnn_status_t launch_few(const I8Args& g, hipStream_t st) {
+  hipLaunchKernelGGL((gemm_i8_few_kernel<FM, FN, UN>), dim3((unsigned)ceil_div(g.N, FN * 16)), dim3(FEW_WAVES * 64), 0,
+                     st, g);
+  return check_launch("gemm_i8_few_kernel");
+}
+
+template <int FM, int FN, int W, int NS>
+mdnn_status_t launch_few_lds(const I8Args& g, hipStream_t st) {
+  hipLaunchKernelGGL((gemm_i8_few_lds_kernel<FM, FN, W, NS>), dim3((unsigned)ceil_div(g.N, FN * 16), (unsigned)ceil_div(g.M, FM * 16)), dim3(W * 64), 0,
+                     st, g);
+  return check_launch("gemm_i8_few_lds_kernel");
+}
+
+// Few rows: FM fragments of rows; FN columns of 16 as the caller chose.
+template <int FN>
+mdnn_status_t run_few(const I8Args& g, hipStream_t st) {
+  if (g.M <= 16) return launch_few_lds<1, FN, 8, 2>(g, st);
+  if (g.M <= 32) return launch_few_lds<2, FN, 4, 3>(g, st);
+  if (g.M <= 48) return launch_few_lds<3, FN, 4, FN == 1 ? 3 : 2>(g, st);
+  return launch_few_lds<4, FN, 4, FN == 1 ? 3 : 2>(g, st);
+}
+
 mdnn_status_t run_i8(const I8Args& g, hipStream_t st) {
-  const int64_t tiles = ceil_div(g.M, TileI64::BM) * ceil_div(g.N, TileI64::BN);
-  hipLaunchKernelGGL((gemm_i8_any_kernel<OutT, TileI64>), dim3((unsigned)tiles), dim3(TileI64::NT), 0, st, g);
-  return check_launch("gemm_i8_any_kernel");
+  if (!i8_aligned(g)) {
+    if (g.M <= 16) return launch_few<1, 1, 8>(g, st);
+    if (g.M <= 64) return launch_few<4, 1, 4>(g, st);
+    const int64_t tiles = ceil_div(g.M, TileI64::BM) * ceil_div(g.N, TileI64::BN);
+    hipLaunchKernelGGL((gemm_i8_any_kernel<TileI64>), dim3((unsigned)tiles), dim3(TileI64::NT), 0, st, g);
+    return check_launch("gemm_i8_any_kernel");
+  }
+  auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(g.M, bm) * ceil_div(g.N, bn); };
+  // Up to one workgroup per CU, the few-rows kernel's waves that share K beat
+  // a 64 x 64 tile's serial loop over it: 64 x 16 tiles (64 x 4096 x 4096 6.6
+  // us, 64 x 32 tiles 7.7, 64 x 64 tiles 9.5), then 64 x 32 (128 x 4096 x
+  // 4096: 11.6, 7.3 and 9.6 us); from two workgroups per CU on it is behind
+  // (192 x 4096 x 4096: 16.9, 14.4, 9.9 us).  Rows of at most 64 and columns
+  // of at most 32 stay on it, their tiles being mostly padding elsewhere
+  // (64 x 8192 x 8192 14.8 us, 64 x 64 tiles 16.3; 16384 x 32 x 4096 13.4,
+  // 18.6).  64 x 16 tiles read A once per 16 columns: not where A is the
+  // larger operand (4096 x 64 x 4096: 12.2 us, 64 x 32 tiles 8.0).
+  if (g.M <= 16 || g.N <= 16 || (tiles(g.M <= 32 ? 32 : 64, 16) <= 256 && g.M <= g.N)) return run_few<1>(g, st);
+  if (g.M <= 64 || g.N <= 32 || tiles(64, 32) <= 256) return run_few<2>(g, st);
+  // 256 x 256 tiles from more than 256 tiles of 256 x 128 on (4096^3 61 us,
+  // 256 x 128 tiles 73; 3000 x 3008 x 2000, 144 tiles, 35 and 44), unless
+  // their padding takes the gain; 256 x 128 while they fill one workgroup per
+  // CU (2048 x 4096 x 4096 36 us; 256 x 256 51, 128 x 128 38; 1536 x 4096 x
+  // 4096 32, 48, 33); below 160 of them 128 x 128 (1024 x 4096 x 4096 24 us,
+  // 256 x 128 29), and 64 x 64 up to 128 of those (1024 x 2048 x 4096 16.3
+  // us, 128 x 128 20.9)
+  if (tiles(256, 128) > 256 && 5 * tiles(256, 256) <= 3 * tiles(256, 128))
+    launch_i8<lds::Tile256, 2>(g, 1, st);
+  else if (tiles(256, 128) > 160)
+    launch_i8<TileI256x128, 3>(g, 1, st);
+  else if (tiles(128, 128) > 128)
+    launch_i8<TileI128, 3>(g, 1, st);
+  else
+    launch_i8<TileI64, 4>(g, 1, st);
+  return check_launch("gemm_i8_kernel");
 }
 
 }  // namespace
@@ -232,11 +644,7 @@ extern "C" mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int
   I8Args g = {};
   g.a = A, g.b = B, g.a_scale = a_scale, g.b_scale = b_scale, g.bias = bias, g.d = D;
   g.M = M, g.N = N, g.K = K, g.lda = lda, g.ldb = ldb, g.ldd = ldd, g.act = act;
+  g.d_type = d_type;
   clear_error();
-  const hipStream_t st = as_stream(stream);
-  switch (d_type) {
-    case MDNN_F32: return run_i8<F32>(g, st);
-    case MDNN_F16: return run_i8<F16>(g, st);
-    default: return run_i8<BF16>(g, st);
-  }
+  return run_i8(g, as_stream(stream));
 }

@@ -671,7 +671,7 @@ __device__ __forceinline__ void wait_tiles(int ahead) {
 template <class T, class TL, class LA, class LB, int C>
 __device__ __forceinline__ void spread_chunk(int tn, uint32_t dst_a, uint32_t dst_b, const char* sa, const char* sb,
                                              int wm, int wn, const LaneFrag& fa_l, const LaneFrag& fb_l, LA& la, LB& lb,
-                                             Frags<TL>& f0, const Frags<TL>& f1, float4_t (&acc)[TL::FM][TL::FN]);
+                                             Frags<TL>& f0, const Frags<TL>& f1, typename Mfma<T>::Acc (&acc)[TL::FM][TL::FN]);
 
 // One K step of the pipeline: tile t in stage S = t % NS (see the kernel).
 // f0 holds k-step 0 of tile t on entry and k-step 0 of tile t+1 on exit.
@@ -680,7 +680,7 @@ __device__ __forceinline__ void spread_chunk(int tn, uint32_t dst_a, uint32_t ds
 template <class T, class TL, int NS, class LA, class LB, int S, bool CHECK>
 __device__ __forceinline__ void pipeline_step(int t, int nk, const Stages<NS>& st, int wave, LaneFrag fa_l,
                                               LaneFrag fb_l, int wm, int wn, LA& la, LB& lb, Frags<TL>& f0,
-                                              Frags<TL>& f1, float4_t (&acc)[TL::FM][TL::FN]) {
+                                              Frags<TL>& f1, typename Mfma<T>::Acc (&acc)[TL::FM][TL::FN]) {
   constexpr int FM = TL::FM, FN = TL::FN;
   constexpr int READS = FM * (LA::KC ? 1 : 2) + FN * (LB::KC ? 1 : 2);
   constexpr int S1 = (S + 1) % NS;
@@ -734,7 +734,7 @@ __device__ __forceinline__ void pipeline_step(int t, int nk, const Stages<NS>& s
 template <class T, class TL, class LA, class LB, int C>
 __device__ __forceinline__ void spread_chunk(int tn, uint32_t dst_a, uint32_t dst_b, const char* sa, const char* sb,
                                              int wm, int wn, const LaneFrag& fa_l, const LaneFrag& fb_l, LA& la, LB& lb,
-                                             Frags<TL>& f0, const Frags<TL>& f1, float4_t (&acc)[TL::FM][TL::FN]) {
+                                             Frags<TL>& f0, const Frags<TL>& f1, typename Mfma<T>::Acc (&acc)[TL::FM][TL::FN]) {
   constexpr int FM = TL::FM, FN = TL::FN, NL = TL::LA + TL::LB;
   if constexpr (C < NL) {
     if constexpr (C < TL::LA)
@@ -770,7 +770,7 @@ __device__ __forceinline__ void spread_chunk(int tn, uint32_t dst_a, uint32_t ds
 template <class T, class TL, int NS, class LA, class LB, int J, int U, bool CHECK>
 __device__ __forceinline__ void pipeline_round(int t, int nk, const Stages<NS>& st, int wave, LaneFrag fa_l,
                                                LaneFrag fb_l, int wm, int wn, LA& la, LB& lb, Frags<TL>& f0,
-                                               Frags<TL>& f1, float4_t (&acc)[TL::FM][TL::FN]) {
+                                               Frags<TL>& f1, typename Mfma<T>::Acc (&acc)[TL::FM][TL::FN]) {
   if constexpr (J < U) {
     if (CHECK && t + J >= nk) return;
     pipeline_step<T, TL, NS, LA, LB, J % NS, CHECK>(t + J, nk, st, wave, fa_l, fb_l, wm, wn, la, lb, f0, f1, acc);
