@@ -18,8 +18,9 @@
 // so every load is unconditional and lies inside the row.  Rows longer than
 // the registers hold, or below eight elements, take the two-pass kernels.
 #include <cmath>
+#include <type_traits>
 
-#include "common.h"
+#include "gemm_core.h"
 #include "internal.h"
 
 namespace mdnn {
@@ -62,8 +63,13 @@ struct Chunk {
   }
   __device__ __forceinline__ void set(const float (&v)[8]) {
     if constexpr (H) {
+      // (a vector conversion is one instruction for two elements)
+      typedef float f2 __attribute__((ext_vector_type(2)));
+      typedef std::conditional_t<T::id == MDNN_F16, _Float16, __bf16> E;
+      typedef E e2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = (uint32_t)from_f<T>(v[2 * e]) | ((uint32_t)from_f<T>(v[2 * e + 1]) << 16);
+      for (int e = 0; e < 4; ++e)
+        w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[2 * e], v[2 * e + 1]}, e2));
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[e] = __builtin_bit_cast(uint32_t, v[e]);
@@ -178,8 +184,8 @@ __device__ __forceinline__ SumMax row_reduce(SumMax v, SumMax (*buf)[TPR / 64 + 
 struct Sum2 {
   float a, b;
 };
-template <int TPR>
-__device__ __forceinline__ Sum2 row_reduce(Sum2 v, Sum2 (*buf)[TPR / 64 + 1], int flip) {
+template <int TPR, int RPB>
+__device__ __forceinline__ Sum2 row_reduce(Sum2 v, Sum2 (*buf)[RPB][TPR / 64 + 1], int flip) {
   constexpr int W = TPR < 64 ? TPR : 64;
 #pragma unroll
   for (int o = W / 2; o > 0; o >>= 1) {
@@ -187,11 +193,12 @@ __device__ __forceinline__ Sum2 row_reduce(Sum2 v, Sum2 (*buf)[TPR / 64 + 1], in
     v.b += __shfl_xor(v.b, o, W);
   }
   if constexpr (TPR > 64) {
-    if ((threadIdx.x & 63) == 0) buf[flip][threadIdx.x >> 6] = v;
+    const int r = threadIdx.x / TPR;
+    if ((threadIdx.x & 63) == 0) buf[flip][r][threadIdx.x % TPR >> 6] = v;
     __syncthreads();
-    v = buf[flip][0];
+    v = buf[flip][r][0];
 #pragma unroll
-    for (int w = 1; w < TPR / 64; ++w) v.a += buf[flip][w].a, v.b += buf[flip][w].b;
+    for (int w = 1; w < TPR / 64; ++w) v.a += buf[flip][r][w].a, v.b += buf[flip][r][w].b;
   }
   return v;
 }
@@ -365,6 +372,11 @@ void launch_rows(const RowArgs& a, hipStream_t st) {
                      dim3(NT), 0, st, a);
 }
 
+// One or two chunks a thread, as few threads of a row idle as that allows
+// (8192 x 1024 bf16, 128 chunks, with codes: 64 threads x 2 chunks 11.4 us,
+// 256 x 1 15.5; 4096 x 4096: 256 x 2 19.4 us, 512 x 1 21.6, 64 x 8 25.0;
+// 8192 x 8192: 512 x 2 83.9 us, 256 x 4 90.6): the chunks' conversions, not the
+// loads in flight, tell the shapes apart.
 template <class T, int MODE>
 mdnn_status_t run_rows_t(const RowArgs& a, hipStream_t st) {
   const int64_t nch = ceil_div(a.cols, 8);
@@ -373,16 +385,20 @@ mdnn_status_t run_rows_t(const RowArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((row_long_kernel<T, MODE>), dim3((unsigned)blocks), dim3(1024), 0, st, a);
   } else if (nch <= 16) {
     launch_rows<T, MODE, 16, 1>(a, st);
+  } else if (nch <= 32) {
+    launch_rows<T, MODE, 16, 2>(a, st);
   } else if (nch <= 64) {
     launch_rows<T, MODE, 64, 1>(a, st);
+  } else if (nch <= 128) {
+    launch_rows<T, MODE, 64, 2>(a, st);
   } else if (nch <= 256) {
     launch_rows<T, MODE, 256, 1>(a, st);
   } else if (nch <= 512) {
     launch_rows<T, MODE, 256, 2>(a, st);
   } else if (nch <= 1024) {
-    launch_rows<T, MODE, 256, 4>(a, st);
+    launch_rows<T, MODE, 512, 2>(a, st);
   } else if (nch <= 2048) {
-    launch_rows<T, MODE, 1024, 2>(a, st);
+    launch_rows<T, MODE, 512, 4>(a, st);
   } else {
     launch_rows<T, MODE, 1024, 4>(a, st);
   }
@@ -403,10 +419,14 @@ mdnn_status_t run_rows(const RowArgs& a, mdnn_dtype_t t, hipStream_t st) {
 // gradients of the norm
 //   g = dy * gamma, xh = h * rstd, c = mean(g * xh)
 //   dx = rstd * (g - xh * c) + dres,  dgamma = sum over rows of dy * xh
-// One reduction per row for sum h^2 and sum g * h together.  Each block walks
-// its rows and keeps the dgamma sums of its threads' columns in registers;
-// it writes them once, and the blocks' sums are added in a fixed order.
+// One reduction per row for sum h^2 and sum g * h together.  Blocks of 512
+// threads, two to a CU, walk their rows and keep the dgamma sums of their
+// threads' columns in registers; a block writes them once, and the blocks'
+// sums are added in a fixed order.  Loading the next row ahead gained nothing
+// (4096 x 4096 bf16: 28.4 us against 28.1: the other block's loads fill the gap),
+// blocks of 1024 threads wait for each other (28.6; 8192 x 8192 114 against 109).
 // ---------------------------------------------------------------------------
+constexpr int BWD_NT(int tpr) { return tpr <= 512 ? 512 : 1024; }
 struct BwdArgs {
   const void *dy, *h, *dres;  // dres: or null
   const float* gamma;         // or null
@@ -418,12 +438,12 @@ struct BwdArgs {
 };
 
 template <class T, int TPR, int NCH>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_bwd_kernel(BwdArgs a) {
+__global__ void __launch_bounds__(BWD_NT(TPR)) norm_bwd_kernel(BwdArgs a) {
   typedef typename T::storage S;
-  constexpr int NT = TPR < 256 ? 256 : TPR, RPB = NT / TPR;
-  __shared__ Sum2 buf[2][TPR / 64 + 1];
-  __shared__ float part[RPB > 1 ? RPB * TPR * NCH * 8 : 1];
-  const int t = threadIdx.x % TPR;
+  constexpr int NT = BWD_NT(TPR), RPB = NT / TPR, WIDE = TPR * NCH * 8;
+  __shared__ Sum2 buf[2][RPB][TPR / 64 + 1];
+  __shared__ float part[RPB > 1 ? RPB * WIDE : 1];
+  const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
   ChunkPos pos[NCH];
   float dg[NCH][8];
 #pragma unroll
@@ -432,18 +452,21 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_bwd_kernel(BwdArgs
 #pragma unroll
     for (int e = 0; e < 8; ++e) dg[i][e] = 0.0f;
   }
+  // (fp32 rows over 1024 threads fill the registers: gamma and the residual's gradient are read late)
+  constexpr bool LATE = TPR == 1024 && !Chunk<T>::H;
   int flip = 0;
   for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB, flip ^= 1) {
-    const int64_t rw = r0 + threadIdx.x / TPR;
-    const bool live = rw < a.rows;
-    const int64_t row = live ? rw : a.rows - 1;
+    const float* gamma = a.gamma;
+    if (LATE) asm("" : "+s"(gamma));  // (read again for every row)
+    const bool live = r0 + grp < a.rows;
+    const int64_t row = live ? r0 + grp : a.rows - 1;  // (past the last row: repeated, nothing stored)
     Chunk<T> cd[NCH], ch[NCH], cr[NCH];
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       cd[i].load((const S*)a.dy + row * a.lddy + pos[i].start);
       ch[i].load((const S*)a.h + row * a.ldh + pos[i].start);
     }
-    if (a.dres) {
+    if (a.dres && !LATE) {
 #pragma unroll
       for (int i = 0; i < NCH; ++i) cr[i].load((const S*)a.dres + row * a.lddr + pos[i].start);
     }
@@ -451,27 +474,28 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_bwd_kernel(BwdArgs
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       Chunk<F32> g;
-      if (a.gamma) g.load(a.gamma + pos[i].start);
+      if (gamma) g.load(gamma + pos[i].start);
       if (pos[i].lo > 0) ch[i].clear(pos[i].lo), cd[i].clear(pos[i].lo);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float h = ch[i].get(e), d = cd[i].get(e);
         v.a = fmaf(h, h, v.a);
-        v.b = fmaf(a.gamma ? d * g.get(e) : d, h, v.b);
+        v.b = fmaf(gamma ? d * g.get(e) : d, h, v.b);
       }
     }
-    v = row_reduce<TPR>(v, buf, flip);
+    v = row_reduce<TPR, RPB>(v, buf, flip);
     const float rstd = row_rstd(v.a, (float)a.cols, a.eps), c = rstd * v.b / (float)a.cols;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       if (!live || pos[i].lo == 8) continue;
       Chunk<F32> g;
-      if (a.gamma) g.load(a.gamma + pos[i].start);
+      if (gamma) g.load(gamma + pos[i].start);
+      if (a.dres && LATE) cr[i].load((const S*)a.dres + row * a.lddr + pos[i].start);
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float xh = ch[i].get(e) * rstd, d = cd[i].get(e);
-        o[e] = rstd * ((a.gamma ? d * g.get(e) : d) - xh * c);
+        o[e] = rstd * ((gamma ? d * g.get(e) : d) - xh * c);
         if (a.dres) o[e] += cr[i].get(e);
         dg[i][e] = fmaf(d, xh, dg[i][e]);
       }
@@ -489,15 +513,15 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_bwd_kernel(BwdArgs
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        part[(threadIdx.x / TPR) * (TPR * NCH * 8) + (t + i * TPR) * 8 + e] = dg[i][e];
+      for (int e = 0; e < 8; e += 4)
+        *(float4*)&part[grp * WIDE + (t + i * TPR) * 8 + e] = make_float4(dg[i][e], dg[i][e + 1], dg[i][e + 2], dg[i][e + 3]);
     __syncthreads();
     for (int c = threadIdx.x; c < a.cols; c += NT) {
-      // where column c lies: its chunk's slot, counted from the row's end in the last, partial chunk
-      const int k = c / 8, start = chunk_pos(k, a.cols).start;
-      float s = 0.0f;
+      // column c's place: its chunk's slot, counted from the row's end in the last, partial chunk
+      const int k = c / 8, at = k * 8 + (c - chunk_pos(k, a.cols).start);
+      float s = part[at];
 #pragma unroll
-      for (int r = 0; r < RPB; ++r) s += part[r * (TPR * NCH * 8) + k * 8 + (c - start)];
+      for (int r = 1; r < RPB; ++r) s += part[r * WIDE + at];
       out[c] = s;
     }
   } else {
@@ -511,12 +535,35 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_bwd_kernel(BwdArgs
   }
 }
 
+// dgamma from the blocks' sums: 32 columns a block, 32 rows of threads, each
+// adding every 32nd block's sums (sixteen loads in flight), then those in order.
+__global__ void __launch_bounds__(1024) dgamma_kernel(const float* partial, int blocks, int64_t cols, float* dgamma) {
+  __shared__ float part[32][32];
+  const int cx = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 32 + cx;
+  const float* p = partial + (c < cols ? c : cols - 1);
+  float s = 0.0f;
+  for (int b0 = r; b0 < blocks; b0 += 512) {
+    float v[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = p[(int64_t)(b0 + 32 * k < blocks ? b0 + 32 * k : r) * cols];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += b0 + 32 * k < blocks ? v[k] : 0.0f;
+  }
+  part[r][cx] = s;
+  __syncthreads();
+  if (r > 0 || c >= cols) return;
+#pragma unroll
+  for (int k = 1; k < 32; ++k) s += part[k][cx];
+  dgamma[c] = s;
+}
+
 // Rows of any length: read twice, dgamma's sums kept in the block's own row
 // of the partials.
 template <class T>
 __global__ void __launch_bounds__(1024) norm_bwd_long_kernel(BwdArgs a) {
   typedef typename T::storage S;
-  __shared__ Sum2 buf[2][17];
+  __shared__ Sum2 buf[2][1][17];
   int flip = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
     const S *dy = (const S*)a.dy + row * a.lddy, *hp = (const S*)a.h + row * a.ldh;
@@ -526,7 +573,7 @@ __global__ void __launch_bounds__(1024) norm_bwd_long_kernel(BwdArgs a) {
       v.a = fmaf(h, h, v.a);
       v.b = fmaf(a.gamma ? d * a.gamma[c] : d, h, v.b);
     }
-    v = row_reduce<1024>(v, buf, flip);
+    v = row_reduce<1024, 1>(v, buf, flip);
     const float rstd = row_rstd(v.a, (float)a.cols, a.eps), k = rstd * v.b / (float)a.cols;
     for (int c = threadIdx.x; c < a.cols; c += 1024) {
       const float xh = to_f<T>(hp[c]) * rstd, d = to_f<T>(dy[c]);
@@ -541,31 +588,37 @@ __global__ void __launch_bounds__(1024) norm_bwd_long_kernel(BwdArgs a) {
   }
 }
 
-int bwd_rows_per_block(int64_t cols) {
+// Threads per row of the backward pass by the row's chunks; 0: the long-row kernel.
+int bwd_tpr(int64_t cols) {
   const int64_t nch = ceil_div(cols, 8);
-  return cols < 8 || nch > 64 ? 1 : nch <= 16 ? 16 : 4;
+  return cols < 8 || nch > 2048 ? 0 : nch <= 32 ? 16 : nch <= 128 ? 64 : nch <= 512 ? 256 : nch <= 1024 ? 512 : 1024;
 }
-// Blocks of the backward pass: by the sizes alone, so that the workspace and
-// the order of dgamma's sums are the same everywhere.
+// Its blocks (as many as the chip runs at once): by the sizes alone, so that
+// the workspace and the order of dgamma's sums are the same everywhere.
 int64_t bwd_blocks(int64_t rows, int64_t cols) {
-  const int64_t b = ceil_div(rows, bwd_rows_per_block(cols));
-  return b < 512 ? b : 512;
+  const int tpr = bwd_tpr(cols);
+  const int64_t b = ceil_div(rows, tpr == 0 ? 1 : BWD_NT(tpr) / tpr), most = tpr == 0 || tpr == 1024 ? 256 : 512;
+  return b < most ? b : most;
 }
 
 template <class T, int TPR, int NCH>
 void launch_bwd(const BwdArgs& a, int64_t blocks, hipStream_t st) {
-  hipLaunchKernelGGL((norm_bwd_kernel<T, TPR, NCH>), dim3((unsigned)blocks), dim3(TPR < 256 ? 256 : TPR), 0, st, a);
+  hipLaunchKernelGGL((norm_bwd_kernel<T, TPR, NCH>), dim3((unsigned)blocks), dim3(BWD_NT(TPR)), 0, st, a);
 }
 
 template <class T>
 mdnn_status_t run_bwd(const BwdArgs& a, hipStream_t st) {
   const int64_t nch = ceil_div(a.cols, 8), blocks = bwd_blocks(a.rows, a.cols);
-  if (a.cols < 8 || nch > 2048)
+  if (bwd_tpr(a.cols) == 0)
     hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3((unsigned)blocks), dim3(1024), 0, st, a);
   else if (nch <= 16)
     launch_bwd<T, 16, 1>(a, blocks, st);
+  else if (nch <= 32)
+    launch_bwd<T, 16, 2>(a, blocks, st);
   else if (nch <= 64)
     launch_bwd<T, 64, 1>(a, blocks, st);
+  else if (nch <= 128)
+    launch_bwd<T, 64, 2>(a, blocks, st);
   else if (nch <= 256)
     launch_bwd<T, 256, 1>(a, blocks, st);
   else if (nch <= 512)
@@ -584,151 +637,195 @@ mdnn_status_t run_bwd(const BwdArgs& a, hipStream_t st) {
 // the tile round in LDS (its second read of x is 64 KB of a matrix that the
 // last-level cache still holds).
 // ---------------------------------------------------------------------------
-constexpr int SLABS = 64;  // at most
-int64_t slab_rows(int64_t rows) {
-  const int64_t s = ceil_div(rows, SLABS);
-  return s < 32 ? 32 : s;
+// Rows of a slab: about a thousand blocks of 256 columns in pass 1, at most
+// 256 slabs (every tile of pass 2 reads its columns' maxima of each).
+int64_t slab_rows(int64_t rows, int64_t cols) {
+  int64_t most = ceil_div(1024, ceil_div(cols, 256));
+  most = most > 256 ? 256 : most;
+  const int64_t per = ceil_div(ceil_div(rows, most), 16) * 16;
+  return per < 32 ? 32 : per;
 }
-int64_t slab_count(int64_t rows) { return rows > 0 ? ceil_div(rows, slab_rows(rows)) : 0; }
+int64_t slab_count(int64_t rows, int64_t cols) { return rows > 0 && cols > 0 ? ceil_div(rows, slab_rows(rows, cols)) : 0; }
 
-// Four consecutive elements of a row from column c, zero past the row.
-template <class T>
-__device__ __forceinline__ void load_quad(const typename T::storage* p, int64_t c, int64_t cols, float (&v)[4]) {
-  typedef uint32_t u2v_a2 __attribute__((ext_vector_type(2), aligned(2)));
-  if (c + 4 <= cols) {
-    if constexpr (sizeof(typename T::storage) == 2) {
-      const u2v_a2 w = *(const MDNN_GLOBAL u2v_a2*)(p + c);
-      v[0] = to_f<T>((uint16_t)w.x), v[1] = to_f<T>((uint16_t)(w.x >> 16));
-      v[2] = to_f<T>((uint16_t)w.y), v[3] = to_f<T>((uint16_t)(w.y >> 16));
-    } else {
-      const u4v_a4 w = *(const MDNN_GLOBAL u4v_a4*)(p + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(w[e]);
-    }
+// Four consecutive elements of a row: those from `start` (a quad past the
+// row's end starts at its last four and overlaps its neighbour), or, in rows
+// below four columns (NARROW), its elements with the last repeated.
+template <class T, bool NARROW>
+__device__ __forceinline__ Quad<T> load_quad(const typename T::storage* row, int64_t start, int64_t cols) {
+  Quad<T> q;
+  if constexpr (!NARROW) {
+    q.load(row + start);
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? to_f<T>(p[c + e]) : 0.0f;
+    for (int e = 0; e < 4; ++e) {
+      const typename T::storage v = row[e < cols ? e : cols - 1];
+      if constexpr (!Quad<T>::H)
+        q.q[e] = __float_as_uint(v);
+      else if (e & 1)
+        q.q[e >> 1] |= (uint32_t)v << 16;
+      else
+        q.q[e >> 1] = v;
+    }
   }
+  return q;
+}
+template <bool NARROW>
+__device__ __forceinline__ int64_t quad_start(int64_t c, int64_t cols) {
+  return NARROW ? 0 : c + 4 <= cols ? c : cols - 4;
 }
 
-template <class T>
+template <class T, bool NARROW>
 __global__ void __launch_bounds__(256)
 colmax_kernel(const typename T::storage* x, int64_t ldx, int64_t rows, int64_t cols, int64_t per, uint32_t* partial) {
   __shared__ uint32_t red[4][256];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 256 + lane * 4;
+  const int64_t c0 = (int64_t)blockIdx.x * 256, start = quad_start<NARROW>(c0 + lane * 4, cols);
   const int64_t r0 = (int64_t)blockIdx.y * per, r1 = r0 + per < rows ? r0 + per : rows;
   uint32_t m[4] = {0u, 0u, 0u, 0u};
-  if (c < cols)
-    for (int64_t r = r0 + wave; r < r1; r += 4) {
-      float v[4];
-      load_quad<T>(x + r * ldx, c, cols, v);
+  for (int64_t r = r0 + wave; r < r1; r += 32) {
+    Quad<T> v[8];  // eight rows in flight (past the slab: the first again)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = load_quad<T, NARROW>(x + (r + 4 * k < r1 ? r + 4 * k : r) * ldx, start, cols);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t u = __float_as_uint(v[e]) & 0x7fffffffu;
+        const uint32_t u = __float_as_uint(v[k].get(e)) & 0x7fffffffu;
         m[e] = u > m[e] ? u : m[e];
       }
-    }
+  }
+  // (lanes whose quads overlap write the same values)
 #pragma unroll
-  for (int e = 0; e < 4; ++e) red[wave][lane * 4 + e] = m[e];
+  for (int e = 0; e < 4; ++e)
+    if (start + e >= c0) red[wave][start + e - c0] = m[e];
   __syncthreads();
-  const int64_t co = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (co >= cols) return;
+  if (c0 + threadIdx.x >= cols) return;
   uint32_t v = red[0][threadIdx.x];
 #pragma unroll
   for (int w = 1; w < 4; ++w) v = red[w][threadIdx.x] > v ? red[w][threadIdx.x] : v;
-  partial[(int64_t)blockIdx.y * cols + co] = v;
+  partial[(int64_t)blockIdx.y * cols + c0 + threadIdx.x] = v;
 }
 
 constexpr int QT_C = 64, QT_R = 128;  // tile: columns, rows
-template <class T>
+template <class T, bool NARROW>
 __global__ void __launch_bounds__(256)
 quant_t_kernel(const typename T::storage* x, int64_t ldx, int64_t rows, int64_t cols, const uint32_t* partial,
                int slabs, int8_t* q, int64_t ldq, float* scale) {
-  __shared__ uint32_t top[4][QT_C];
-  __shared__ float inv[QT_C];
-  __shared__ uint32_t mask[QT_C];
-  __shared__ uint32_t tile[QT_C][QT_R / 4 + 1];
-  const int tid = threadIdx.x;
-  const int64_t c0 = (int64_t)blockIdx.x * QT_C;
-  {
-    const int c = tid & 63, part = tid >> 6;
-    uint32_t m = 0u;
-    if (c0 + c < cols)
-      for (int s = part; s < slabs; s += 4) {
-        const uint32_t u = partial[(int64_t)s * cols + c0 + c];
-        m = u > m ? u : m;
+  // (three columns of room before the tile's: a last tile of fewer than four columns starts its quads before it)
+  __shared__ uint32_t top[16][QT_C + 4];
+  __shared__ float inv[QT_C + 3];
+  __shared__ uint32_t mask[QT_C + 3];
+  __shared__ uint32_t tile[QT_C + 3][QT_R / 4 + 1];
+  const int tid = threadIdx.x, part = tid >> 4;
+  const int64_t c0 = (int64_t)blockIdx.x * QT_C, start = quad_start<NARROW>(c0 + (tid & 15) * 4, cols);
+  const int cq = (int)(start - c0) + 3;
+  // the columns' maxima over the slabs: a quad of columns and every 16th slab
+  // a thread; 4 x 4 blocks of the tile, four rows' quads, are read meanwhile
+  Quad<F32> u[4];
+  auto load_top = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int s = s0 + 16 * k < slabs ? s0 + 16 * k : slabs - 1;
+      u[k] = load_quad<F32, NARROW>((const float*)partial + (int64_t)s * cols, start, cols);
+    }
+  };
+  uint32_t m[4] = {0u, 0u, 0u, 0u};
+  auto take_top = [&] {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] = u[k].q[e] > m[e] ? u[k].q[e] : m[e];
+  };
+  Quad<T> v[QT_R / 64][4];
+  auto load = [&](int64_t r0) {
+#pragma unroll
+    for (int p = 0; p < QT_R / 64; ++p)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t r = r0 + (part + p * 16) * 4 + e;  // (past the last row: the last again, never stored)
+        v[p][e] = load_quad<T, NARROW>(x + (r < rows ? r : rows - 1) * ldx, start, cols);
       }
-    top[part][c] = m;
+  };
+  int64_t r0 = (int64_t)blockIdx.y * QT_R;
+  if (slabs > 0) {
+    load_top(part);
+    load(r0);
+    take_top();
+    for (int s = part + 64; s < slabs; s += 64) {
+      load_top(s);
+      take_top();
+    }
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (cq + e >= 3) top[part][cq + e - 3] = m[e];
   __syncthreads();
   if (tid < QT_C) {
-    uint32_t m = top[0][tid];
+    uint32_t b = top[0][tid];
 #pragma unroll
-    for (int p = 1; p < 4; ++p) m = top[p][tid] > m ? top[p][tid] : m;
-    const RowScale k = row_scale(m, false);
-    inv[tid] = k.inv;
-    mask[tid] = k.mask;
+    for (int p = 1; p < 16; ++p) b = top[p][tid] > b ? top[p][tid] : b;
+    const RowScale k = row_scale(b, false);
+    inv[tid + 3] = k.inv;
+    mask[tid + 3] = k.mask;
     if (blockIdx.y == 0 && c0 + tid < cols) scale[c0 + tid] = k.scale;
   }
   __syncthreads();
-  for (int64_t r0 = (int64_t)blockIdx.y * QT_R; r0 < rows; r0 += (int64_t)gridDim.y * QT_R) {
-    // 4 x 4 blocks: four rows' quads become one word of four rows per column
-    const int cq = (tid & 15) * 4;
+  typedef uint32_t u1_a1 __attribute__((aligned(1)));
+  while (r0 < rows) {
+    // one word of four rows per column
 #pragma unroll
-    for (int p = 0; p < QT_R / 64; ++p) {
-      const int rq = (tid >> 4) + p * 16;  // row quad
-      float v[4][4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int64_t r = r0 + rq * 4 + e;
-        if (r < rows) {
-          load_quad<T>(x + r * ldx, c0 + cq, cols, v[e]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[e][j] = 0.0f;
-        }
-      }
+    for (int p = 0; p < QT_R / 64; ++p)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        tile[cq + j][rq] = codes4(v[0][j], v[1][j], v[2][j], v[3][j], inv[cq + j]) & mask[cq + j];
-    }
+        tile[cq + j][part + p * 16] =
+            codes4(v[p][0].get(j), v[p][1].get(j), v[p][2].get(j), v[p][3].get(j), inv[cq + j]) & mask[cq + j];
+    const int64_t next = r0 + (int64_t)gridDim.y * QT_R;
+    if (next < rows) load(next);
     __syncthreads();
+    const int w = tid % (QT_R / 4), cc = tid / (QT_R / 4);
+    int8_t* o = q + (c0 + cc) * ldq + r0 + w * 4;
+    if (r0 + QT_R <= rows && c0 + QT_C <= cols) {
 #pragma unroll
-    for (int p = 0; p < QT_C * (QT_R / 4) / 256; ++p) {
-      const int idx = tid + p * 256, c = idx / (QT_R / 4), w = idx % (QT_R / 4);
-      const int64_t r = r0 + w * 4;
-      if (c0 + c >= cols || r >= rows) continue;
-      typedef uint32_t u1_a1 __attribute__((aligned(1)));
-      int8_t* o = q + (c0 + c) * ldq + r;
-      const uint32_t v = tile[c][w];
-      if (r + 4 <= rows) {
-        *(MDNN_GLOBAL u1_a1*)o = v;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-          if (r + e < rows) o[e] = (int8_t)(v >> (8 * e));
+      for (int p = 0; p < QT_C / 8; ++p) *(MDNN_GLOBAL u1_a1*)(o + p * 8 * ldq) = tile[cc + p * 8 + 3][w];
+    } else {
+      const int64_t left = rows - r0 - w * 4;
+      for (int p = 0; p < QT_C / 8; ++p) {
+        if (c0 + cc + p * 8 >= cols) break;
+        const uint32_t w4 = tile[cc + p * 8 + 3][w];
+        if (left >= 4) {
+          *(MDNN_GLOBAL u1_a1*)(o + p * 8 * ldq) = w4;
+        } else {
+          for (int e = 0; e < left; ++e) o[p * 8 * ldq + e] = (int8_t)(w4 >> (8 * e));
+        }
       }
     }
     __syncthreads();
+    r0 = next;
   }
+}
+
+template <class T, bool NARROW>
+mdnn_status_t launch_quant_t(int64_t rows, int64_t cols, const void* x, int64_t ldx, int8_t* q, int64_t ldq,
+                             float* scale, uint32_t* partial, hipStream_t st) {
+  typedef typename T::storage S;
+  const int64_t slabs = slab_count(rows, cols);
+  if (slabs > 0) {
+    hipLaunchKernelGGL((colmax_kernel<T, NARROW>), dim3((unsigned)ceil_div(cols, 256), (unsigned)slabs), dim3(256), 0,
+                       st, (const S*)x, ldx, rows, cols, slab_rows(rows, cols), partial);
+    MDNN_TRY(check_launch("colmax_kernel"));
+  }
+  int64_t gy = ceil_div(rows, QT_R);
+  gy = gy < 1 ? 1 : gy > 65535 ? 65535 : gy;
+  hipLaunchKernelGGL((quant_t_kernel<T, NARROW>), dim3((unsigned)ceil_div(cols, QT_C), (unsigned)gy), dim3(256), 0, st,
+                     (const S*)x, ldx, rows, cols, partial, (int)slabs, q, ldq, scale);
+  return check_launch("quant_t_kernel");
 }
 
 template <class T>
 mdnn_status_t run_quant_t(int64_t rows, int64_t cols, const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale,
                           uint32_t* partial, hipStream_t st) {
-  typedef typename T::storage S;
-  const int64_t slabs = slab_count(rows);
-  if (slabs > 0) {
-    hipLaunchKernelGGL(colmax_kernel<T>, dim3((unsigned)ceil_div(cols, 256), (unsigned)slabs), dim3(256), 0, st,
-                       (const S*)x, ldx, rows, cols, slab_rows(rows), partial);
-    MDNN_TRY(check_launch("colmax_kernel"));
-  }
-  int64_t gy = ceil_div(rows, QT_R);
-  gy = gy < 1 ? 1 : gy > 4096 ? 4096 : gy;
-  hipLaunchKernelGGL(quant_t_kernel<T>, dim3((unsigned)ceil_div(cols, QT_C), (unsigned)gy), dim3(256), 0, st,
-                     (const S*)x, ldx, rows, cols, partial, (int)slabs, q, ldq, scale);
-  return check_launch("quant_t_kernel");
+  return cols < 4 ? launch_quant_t<T, true>(rows, cols, x, ldx, q, ldq, scale, partial, st)
+                  : launch_quant_t<T, false>(rows, cols, x, ldx, q, ldq, scale, partial, st);
 }
 
 constexpr int64_t MAX_COLS = (int64_t)1 << 29;  // 32-bit column indices; a launch holds fewer than 2^32 threads a dimension
@@ -756,7 +853,7 @@ extern "C" mdnn_status_t mdnn_quantize_i8(int64_t rows, int64_t cols, const void
 
 extern "C" size_t mdnn_quantize_i8_t_workspace(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 0 || cols > MAX_COLS) return 0;
-  return (size_t)slab_count(rows) * (size_t)cols * 4;
+  return (size_t)slab_count(rows, cols) * (size_t)cols * 4;
 }
 
 extern "C" mdnn_status_t mdnn_quantize_i8_t(int64_t rows, int64_t cols, const void* x, int64_t ldx,
@@ -831,9 +928,7 @@ extern "C" mdnn_status_t mdnn_rmsnorm_i8_fwd(int64_t rows, int64_t cols, const v
 
 extern "C" size_t mdnn_rmsnorm_bwd_workspace(int64_t rows, int64_t cols) {
   if (rows <= 0 || cols < 1 || cols > MAX_COLS) return 0;
-  // the blocks' sums, then the column sums' own workspace
-  const int64_t b = bwd_blocks(rows, cols);
-  return (((size_t)b * (size_t)cols * 4 + 255) & ~(size_t)255) + column_sums_ws_bytes(b, cols);
+  return (size_t)bwd_blocks(rows, cols) * (size_t)cols * 4;  // the blocks' sums
 }
 
 extern "C" mdnn_status_t mdnn_rmsnorm_bwd(int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* h,
@@ -869,7 +964,7 @@ extern "C" mdnn_status_t mdnn_rmsnorm_bwd(int64_t rows, int64_t cols, const void
     default: MDNN_TRY(run_bwd<BF16>(a, st)); break;
   }
   if (!dgamma) return MDNN_SUCCESS;
-  const int64_t b = bwd_blocks(rows, cols);
-  const size_t used = ((size_t)b * (size_t)cols * 4 + 255) & ~(size_t)255;
-  return column_sums(workspace, nullptr, MDNN_F32, b, cols, dgamma, (char*)workspace + used, need - used, st);
+  hipLaunchKernelGGL(dgamma_kernel, dim3((unsigned)ceil_div(cols, 32)), dim3(1024), 0, st, (const float*)workspace,
+                     (int)bwd_blocks(rows, cols), cols, dgamma);
+  return check_launch("dgamma_kernel");
 }
