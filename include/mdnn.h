@@ -455,8 +455,8 @@ mdnn_status_t mdnn_cast(int64_t n, const void* src, mdnn_dtype_t src_type, void*
  *   weights W[in, out] this is the product's operand B with a scale for each
  *   output.  workspace: mdnn_quantize_i8_t_workspace(rows, cols) bytes,
  *   16-byte aligned (may be NULL when that size is 0).
- * q may start at any byte and have any ldq; ldq a multiple of 16 with a
- * 16-byte aligned q lets mdnn_gemm_i8 take its fastest kernels.  Bytes of q
+ * q may start at any byte and have any ldq; ldq a multiple of 16, better of
+ * 128, with a q aligned alike lets mdnn_gemm_i8 take its fastest kernels.  Bytes of q
  * between a row's width and ldq are left as they are.  cols <= 2^29.
  * Deterministic.  Errors: MDNN_ERR_SHAPE, _DTYPE, _NULL, _LAYOUT (a leading
  * dimension below the width), _MISALIGNED, _WORKSPACE, _LAUNCH.
@@ -475,11 +475,12 @@ mdnn_status_t mdnn_quantize_i8_t(int64_t rows, int64_t cols, const void* x, int6
  * and rounded once.  K <= 131071, so that no sum leaves 32 bits
  * (MDNN_ERR_SHAPE above).  Any M, N, K >= 0 (M or N == 0: no-op; K == 0: the
  * sums are 0), any strides and byte addresses of A and B; 16-byte aligned A
- * and B with lda, ldb multiples of 16 are fastest.  Bytes of A and B past K
+ * and B with lda, ldb multiples of 16 are fast, of 128 fastest.  Bytes of A and B past K
  * in a row are never used.  D must not overlap an input.
  * workspace: NULL, or 16-byte aligned device memory; with at least
- * mdnn_gemm_i8_workspace(M, N, K) bytes a product of few output tiles over a
- * long K splits K across workgroups (the same result: the sums are exact).
+ * mdnn_gemm_i8_workspace(M, N, K) bytes a large product whose rows are not on
+ * 16 bytes first copies them to rows that are (the same result; not used for
+ * aligned rows, and 0 bytes where K is a multiple of 16 or the product small).
  * It is scratch, overwritten; calls that share one must be ordered on one
  * stream.  Deterministic.  Errors as above. */
 size_t mdnn_gemm_i8_workspace(int64_t M, int64_t N, int64_t K);

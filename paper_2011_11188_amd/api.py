@@ -198,10 +198,10 @@ def _like(t, x, name: str):
 
 
 def _codes_like(q, rows: int, cols: int, device):
-    """Room for [rows, cols] codes; allocated rows start on 16 bytes."""
+    """Room for [rows, cols] codes; allocated rows start on 128 bytes (a cache line)."""
     import torch
     if q is None:
-        q = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
+        q = torch.empty((rows, (cols + 127) // 128 * 128), dtype=torch.int8, device=device)[:, :cols]
     elif q.dtype != torch.int8 or tuple(q.shape) != (rows, cols):
         raise ValueError(f"q must be int8 [{rows}, {cols}]")
     return q, _rows_of(q, "q")[2]

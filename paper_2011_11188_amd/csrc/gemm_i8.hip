@@ -37,8 +37,6 @@ struct I8Args {
   void* d;
   int64_t M, N, K, lda, ldb, ldd;
   int32_t act, d_type;
-  int32_t* partial;     // split K: sums [splits][M][N]; or null
-  int64_t k_per_split;  // a multiple of the step
 };
 
 // ------------------------------------------------------------- epilogue
@@ -105,28 +103,7 @@ __device__ __forceinline__ void epilogue_i8_t(const I8Args& g, int64_t mb, int64
 }
 
 template <int FM, int FN>
-__device__ __forceinline__ void epilogue_i8(const I8Args& g, int split, int64_t mb, int64_t nb,
-                                            const int4v (&acc)[FM][FN]) {
-  if (g.partial) {
-    int32_t* p = g.partial + (int64_t)split * g.M * g.N;
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int64_t m = mb + i * 16, n = nb + j * 16;
-        if (m >= g.M || n >= g.N) continue;
-        int32_t* o = p + m * g.N + n;
-        if (n + 4 <= g.N) {
-          typedef int int4_a4 __attribute__((ext_vector_type(4), aligned(4)));
-          *(__attribute__((address_space(1))) int4_a4*)o = (int4_a4){acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-        } else {
-#pragma unroll
-          for (int e = 0; e < 3; ++e)
-            if (n + e < g.N) o[e] = acc[i][j][e];
-        }
-      }
-    return;
-  }
+__device__ __forceinline__ void epilogue_i8(const I8Args& g, int64_t mb, int64_t nb, const int4v (&acc)[FM][FN]) {
   switch (g.d_type) {
     case MDNN_F32: epilogue_i8_t<F32, FM, FN>(g, mb, nb, acc); break;
     case MDNN_F16: epilogue_i8_t<F16, FM, FN>(g, mb, nb, acc); break;
@@ -134,11 +111,25 @@ __device__ __forceinline__ void epilogue_i8(const I8Args& g, int split, int64_t 
   }
 }
 
+// Tile of a workgroup: tile_coords' order (consecutive ids on one
+// XCD, eight tile rows a group) in 32-bit arithmetic; the 64-bit divisions
+// had taken a small product's prologue.
+__device__ __forceinline__ void i8_tile(const I8Args& g, int bm, int bn, int& tm, int& tn) {
+  const uint32_t tiles_m = (uint32_t)((g.M + bm - 1) / bm), tiles_n = (uint32_t)((g.N + bn - 1) / bn);
+  uint32_t id = blockIdx.x;
+  if (gridDim.x % 8 == 0) id = (id % 8) * (gridDim.x / 8) + id / 8;
+  constexpr uint32_t GROUP_M = 8;
+  const uint32_t group = GROUP_M * tiles_n, gid = id / group, in = id - gid * group, first = gid * GROUP_M;
+  const uint32_t size = tiles_m - first < GROUP_M ? tiles_m - first : GROUP_M, col = in / size;
+  tm = (int)(first + in - col * size);
+  tn = (int)col;
+}
+
 // ------------------------------------------------- register-staged kernel
 // Rows that start on any byte, any K: chunks of 16 bytes are read at any
-// address into registers and written to the swizzled LDS tiles (two stages,
-// one barrier a step).  A chunk past the row's end is read from its last 16
-// bytes and shifted; k past K is zero.
+// address into one of NR register sets (NR steps in flight) and written to the
+// swizzled LDS tiles (two stages, one barrier a step).  A chunk past the row's
+// end is read from its last 16 bytes and shifted; k past K is zero.
 
 typedef uint32_t u4v_a1 __attribute__((ext_vector_type(4), aligned(1)));
 
@@ -147,20 +138,29 @@ __device__ __forceinline__ uint4 load_bytes(const int8_t* p) {
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 
-// 16 bytes of a row from byte k, zero from K on.
-__device__ __forceinline__ uint4 row_chunk(const int8_t* row, int64_t k, int64_t K) {
-  if (k + 16 <= K) return load_bytes(row + k);
-  if (k >= K) return make_uint4(0, 0, 0, 0);
-  if (K >= 16) return reg::shift_chunk<1>(load_bytes(row + K - 16), (int)(k - (K - 16)));
+// 16 bytes of a row from byte k, zero from K on, in two halves so that a
+// thread's loads are all in flight before the first is waited for: the load,
+// which stays inside the row, and the shift.  Rows of fewer than 16 bytes are
+// read whole at once.
+__device__ __forceinline__ uint4 load_row(const int8_t* row, int64_t k, int64_t K) {
+  if (K >= 16) return load_bytes(row + (k + 16 <= K ? k : K - 16));  // (uniform)
   uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int e = 0; e < 16; ++e)
-    if (e < K) w[e >> 2] |= (uint32_t)(uint8_t)row[e] << (8 * (e & 3));  // (k is 0 here)
+  for (int e = 0; e < 15; ++e)
+    if (e < K) w[e >> 2] |= (uint32_t)(uint8_t)row[e] << (8 * (e & 3));
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ uint4 fix_row(uint4 v, int64_t k, int64_t K) {
+  if (K >= 16) {
+    const int64_t d = k + 16 - K;  // bytes past the row: how far back the chunk was read
+    if (d > 0) v = reg::shift_chunk<1>(v, d < 16 ? (int)d : 0);
+  }
+  return k < K ? v : make_uint4(0, 0, 0, 0);
+}
 
-template <class TL>
+template <class TL, int NR>
 __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_any_kernel(I8Args g) {
+  static_assert(NR % 2 == 0, "a set's steps have one LDS stage");
   __shared__ __attribute__((aligned(1024))) char lds_a[2][TL::A_BYTES];
   __shared__ __attribute__((aligned(1024))) char lds_b[2][TL::B_BYTES];
   constexpr int FM = TL::FM, FN = TL::FN;
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_any_kernel(I8Args g) 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / TL::WN, wn = wave % TL::WN;
   int tm, tn;
-  tile_coords(ceil_div(g.M, TL::BM), ceil_div(g.N, TL::BN), tm, tn);
+  i8_tile(g, TL::BM, TL::BN, tm, tn);
   const int64_t m0 = (int64_t)tm * TL::BM, n0 = (int64_t)tn * TL::BN;
 
   const int8_t *ra[TL::LA], *rb[TL::LB];
@@ -185,18 +185,24 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_any_kernel(I8Args g) 
     rb[i] = g.b + (n0 + q.r < g.N ? n0 + q.r : g.N - 1) * g.ldb;
     kb[i] = q.c * 2;
   }
-  uint4 va[TL::LA], vb[TL::LB];
-  auto load = [&](int64_t k0) {
+  struct Set {
+    uint4 a[TL::LA], b[TL::LB];
+  };
+  auto load = [&](Set& v, int64_t k0) {
     if (k0 + BKB <= g.K) {
 #pragma unroll
-      for (int i = 0; i < TL::LA; ++i) va[i] = load_bytes(ra[i] + k0 + ka[i]);
+      for (int i = 0; i < TL::LA; ++i) v.a[i] = load_bytes(ra[i] + k0 + ka[i]);
 #pragma unroll
-      for (int i = 0; i < TL::LB; ++i) vb[i] = load_bytes(rb[i] + k0 + kb[i]);
+      for (int i = 0; i < TL::LB; ++i) v.b[i] = load_bytes(rb[i] + k0 + kb[i]);
     } else {
 #pragma unroll
-      for (int i = 0; i < TL::LA; ++i) va[i] = row_chunk(ra[i], k0 + ka[i], g.K);
+      for (int i = 0; i < TL::LA; ++i) v.a[i] = load_row(ra[i], k0 + ka[i], g.K);
 #pragma unroll
-      for (int i = 0; i < TL::LB; ++i) vb[i] = row_chunk(rb[i], k0 + kb[i], g.K);
+      for (int i = 0; i < TL::LB; ++i) v.b[i] = load_row(rb[i], k0 + kb[i], g.K);
+#pragma unroll
+      for (int i = 0; i < TL::LA; ++i) v.a[i] = fix_row(v.a[i], k0 + ka[i], g.K);
+#pragma unroll
+      for (int i = 0; i < TL::LB; ++i) v.b[i] = fix_row(v.b[i], k0 + kb[i], g.K);
     }
   };
   int4v acc[FM][FN];
@@ -206,29 +212,88 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_any_kernel(I8Args g) 
     for (int j = 0; j < FN; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
   const lds::LaneFrag fl = lds::lane_frag<true, TL::BM>(lane);
   const int nk = (int)ceil_div(g.K, BKB);
-  if (nk > 0) load(0);
-  for (int t = 0; t < nk; ++t) {
-    char *sa = lds_a[t & 1], *sb = lds_b[t & 1];
+  Set set[NR];
 #pragma unroll
-    for (int i = 0; i < TL::LA; ++i) *(uint4*)(sa + (wave * TL::LA + i) * 1024 + lane * 16) = va[i];
+  for (int u = 0; u < NR; ++u)
+    if (u < nk) load(set[u], (int64_t)u * BKB);
+  for (int t0 = 0; t0 < nk; t0 += NR) {
 #pragma unroll
-    for (int i = 0; i < TL::LB; ++i) *(uint4*)(sb + (wave * TL::LB + i) * 1024 + lane * 16) = vb[i];
-    if (t + 1 < nk) load((int64_t)(t + 1) * BKB);
-    __syncthreads();
+    for (int u = 0; u < NR; ++u) {
+      const int t = t0 + u;
+      if (t >= nk) break;
+      char *sa = lds_a[u & 1], *sb = lds_b[u & 1];
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      uint4 fa[FM], fb[FN];
+      for (int i = 0; i < TL::LA; ++i) *(uint4*)(sa + (wave * TL::LA + i) * 1024 + lane * 16) = set[u].a[i];
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = lds::fragment<true, TL::BM>(sa, wm * TL::WTM + i * 16, kk, fl);
+      for (int i = 0; i < TL::LB; ++i) *(uint4*)(sb + (wave * TL::LB + i) * 1024 + lane * 16) = set[u].b[i];
+      if (t + NR < nk) load(set[u], (int64_t)(t + NR) * BKB);
+      __syncthreads();
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = lds::fragment<true, TL::BN>(sb, wn * TL::WTN + j * 16, kk, fl);
+      for (int kk = 0; kk < 2; ++kk) {
+        uint4 fa[FM], fb[FN];
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
+        for (int i = 0; i < FM; ++i) fa[i] = lds::fragment<true, TL::BM>(sa, wm * TL::WTM + i * 16, kk, fl);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa[i], acc[i][j]);
+        for (int j = 0; j < FN; ++j) fb[j] = lds::fragment<true, TL::BN>(sb, wn * TL::WTN + j * 16, kk, fl);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa[i], acc[i][j]);
+      }
     }
   }
-  epilogue_i8<FM, FN>(g, 0, m0 + wm * TL::WTM + (lane & 15), n0 + wn * TL::WTN + 4 * (lane >> 4), acc);
+  epilogue_i8<FM, FN>(g, m0 + wm * TL::WTM + (lane & 15), n0 + wn * TL::WTN + 4 * (lane >> 4), acc);
+}
+
+// The last K % 16 bytes (K >= 16) of this lane's fragment rows mb + 16 i of A
+// and nb + 16 j of B, as k 0 .. 15 of one more step in the first 16 lanes.
+// Loaded a few steps before the end and added after it, so that nothing waits
+// for them.
+template <int FM, int FN>
+struct LastBytes {
+  uint4 a[FM], b[FN];
+  __device__ __forceinline__ void load(const I8Args& g, int lane, int64_t mb, int64_t nb) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) b[j] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) a[i] = make_uint4(0, 0, 0, 0);
+    if (lane < 16) {  // (a request a row: the other lanes' copies would be three more)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) b[j] = load_bytes(g.b + (nb + j * 16 < g.N ? nb + j * 16 : g.N - 1) * g.ldb + g.K - 16);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) a[i] = load_bytes(g.a + (mb + i * 16 < g.M ? mb + i * 16 : g.M - 1) * g.lda + g.K - 16);
+    }
+  }
+  __device__ __forceinline__ void add(const I8Args& g, int4v (&acc)[FM][FN]) {
+    const int d = 16 - (int)(g.K & 15);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) b[j] = reg::shift_chunk<1>(b[j], d);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      a[i] = reg::shift_chunk<1>(a[i], d);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(b[j], a[i], acc[i][j]);
+    }
+  }
+};
+
+// Operands copied to rows of whole steps, zeros past K (grid y: A, B).
+struct PackArgs {
+  const int8_t* p[2];
+  int8_t* to[2];
+  int64_t ld[2];
+  uint32_t chunks[2];  // rows x 16-byte chunks; 0: not copied
+  int64_t K;
+  uint32_t per;        // chunks a row
+};
+__global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a) {
+  const int s = blockIdx.y;
+  for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < a.chunks[s]; i += gridDim.x * 256u) {
+    const uint32_t r = i / a.per;
+    const int64_t k = (int64_t)(i - r * a.per) * 16;
+    const uint4 v = fix_row(load_row(a.p[s] + r * a.ld[s], k < a.K ? k : 0, a.K), k, a.K);
+    *(uint4*)(a.to[s] + (int64_t)i * 16) = v;
+  }
 }
 
 // ------------------------------------------------- direct-to-LDS kernel
@@ -252,7 +317,10 @@ struct I8Loader {
   __device__ __forceinline__ void init(const I8Operand& a, int64_t mn0, int64_t kbeg, int wave, int lane) {
     base = (const char*)a.p + mn0 * a.ld + kbeg;
     const int32_t rows = a.MN - mn0 < W ? (int32_t)(a.MN - mn0) : W, ld = (int32_t)a.ld;
-    if constexpr (RAGGED) rsrc = lds::make_rsrc(base, (uint32_t)((rows - 1) * ld + (int32_t)(a.K - kbeg)));
+    if constexpr (RAGGED) {
+      const int32_t bytes = (rows - 1) * ld + (int32_t)(a.K - kbeg);
+      rsrc = lds::make_rsrc(base, bytes > 0 ? (uint32_t)bytes : 0u);
+    }
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const lds::LoadPos q = lds::load_pos<true, W, L>(wave, lane, i);
@@ -295,34 +363,33 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_kernel(I8Args g) {
   __shared__ __attribute__((aligned(NS > 3 ? 1024 : 1))) char lds_b3[NS > 3 ? TL::B_BYTES : 1];
   char* const all_a[4] = {lds_a0, lds_a1, lds_a2, lds_a3};
   char* const all_b[4] = {lds_b0, lds_b1, lds_b2, lds_b3};
+  constexpr int FM = TL::FM, FN = TL::FN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / TL::WN, wn = wave % TL::WN;
   lds::Stages<NS> st;
 #pragma unroll
   for (int s = 0; s < NS; ++s) st.a[s] = all_a[s], st.b[s] = all_b[s];
-  constexpr int FM = TL::FM, FN = TL::FN;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / TL::WN, wn = wave % TL::WN;
-  int tm, tn, split;
-  split_tile_coords(ceil_div(g.M, TL::BM), ceil_div(g.N, TL::BN), tm, tn, split);
+  int tm, tn;
+  i8_tile(g, TL::BM, TL::BN, tm, tn);
   const int64_t m0 = (int64_t)tm * TL::BM, n0 = (int64_t)tn * TL::BN;
-  int64_t kbeg = 0, kend = g.K;
-  if (g.partial) {
-    kbeg = (int64_t)split * g.k_per_split;
-    kend = kbeg + g.k_per_split < g.K ? kbeg + g.k_per_split : g.K;
-  }
   // steps that hold a whole 16-byte chunk
-  const int nk = (int)ceil_div((kend & ~(int64_t)15) - kbeg, (int64_t)BKB);
+  const int nk = (int)ceil_div(g.K & ~(int64_t)15, (int64_t)BKB);
 
   LA la;
   LB lb;
-  la.init(I8Operand{g.a, g.lda, g.M, g.K}, m0, kbeg, wave, lane);
-  lb.init(I8Operand{g.b, g.ldb, g.N, g.K}, n0, kbeg, wave, lane);
+  la.init(I8Operand{g.a, g.lda, g.M, g.K}, m0, 0, wave, lane);
+  lb.init(I8Operand{g.b, g.ldb, g.N, g.K}, n0, 0, wave, lane);
   const uint32_t wa = (uint32_t)(wave * TL::LA) * 1024u, wb = (uint32_t)(wave * TL::LB) * 1024u;
   int4v acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
+  // (256 x 256 tiles have no registers to keep them in over the loop)
+  constexpr bool HOLD = FM + FN <= 8;
+  const int64_t mb = m0 + wm * TL::WTM + (lane & 15), nr = n0 + wn * TL::WTN + (lane & 15);
+  const bool last = RAGGED && (g.K & 15) != 0;
+  LastBytes<HOLD ? FM : 1, HOLD ? FN : 1> held;
   lds::Frags<TL> f0, f1;
   const lds::LaneFrag fa_l = lds::lane_frag<true, TL::BM>(lane), fb_l = lds::lane_frag<true, TL::BN>(lane);
   if (nk > 0) {
@@ -333,23 +400,11 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_kernel(I8Args g) {
         lb.issue(s, lds::lds_address(st.b[s]) + wb);
       }
   }
-  const int64_t mb = m0 + wm * TL::WTM + (lane & 15), nr = n0 + wn * TL::WTN + (lane & 15);
-  if constexpr (RAGGED) {
-    if ((kend & 15) != 0) {  // the last bytes, as k 0 .. 15 of a step in the first 16 lanes, while the first tiles arrive
-      const int64_t k = kend & ~(int64_t)15;
-      uint4 fb[FN];
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int64_t n = nr + j * 16 < g.N ? nr + j * 16 : g.N - 1;
-        fb[j] = lane < 16 ? row_chunk(g.b + n * g.ldb, k, g.K) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const int64_t m = mb + i * 16 < g.M ? mb + i * 16 : g.M - 1;
-        const uint4 fa = lane < 16 ? row_chunk(g.a + m * g.lda, k, g.K) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa, acc[i][j]);
-      }
+  if constexpr (RAGGED && !HOLD) {
+    if (last) {
+      LastBytes<FM, FN> v;
+      v.load(g, lane, mb, nr);
+      v.add(g, acc);
     }
   }
   if (nk > 0) {
@@ -364,88 +419,129 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_kernel(I8Args g) {
   int t = 0;
   for (; t + U - 1 + NS < nk - (RAGGED ? 1 : 0); t += U)  // (the last step is issued with its test)
     lds::pipeline_round<I8, TL, NS, LA, LB, 0, U, false>(t, nk, st, wave, fa_l, fb_l, wm, wn, la, lb, f0, f1, acc);
+  if constexpr (RAGGED && HOLD)
+    if (last) held.load(g, lane, mb, nr);
   for (; t < nk; t += U)
     lds::pipeline_round<I8, TL, NS, LA, LB, 0, U, true>(t, nk, st, wave, fa_l, fb_l, wm, wn, la, lb, f0, f1, acc);
 
-  epilogue_i8<FM, FN>(g, split, mb, n0 + wn * TL::WTN + 4 * (lane >> 4), acc);
+  if constexpr (RAGGED && HOLD)
+    if (last) held.add(g, acc);
+  epilogue_i8<FM, FN>(g, mb, n0 + wn * TL::WTN + 4 * (lane >> 4), acc);
 }
 
-// ------------------------------------------------------- few rows kernel
+// ------------------------------------------------------- few rows kernels
 // At most 64 rows (one to a few samples): the time is B's read.  A block owns
-// FN * 16 columns and its eight waves share K; each wave reads its piece of
-// the operands straight into MFMA fragments (16 bytes of one row a lane, any
-// address), UN steps of 64 k in flight, and the waves' sums are added in LDS.
-constexpr int FEW_WAVES = 8;
-template <int FM, int FN, int UN>
-__global__ void __launch_bounds__(FEW_WAVES * 64) gemm_i8_few_kernel(I8Args g) {
-  static_assert(FM * FN <= FEW_WAVES, "a wave per fragment of the result");
-  __shared__ int4v part[FEW_WAVES][FM * FN][64];
+// FN * 16 columns and its W waves share K; every wave has LDS of its own, so
+// nothing waits for a barrier before the sums are added.  Eight lanes read 128
+// bytes of one row: fragments read from memory directly would touch four rows
+// in every four lanes, which the cache answers a line at a time (64 x 4096 x
+// 4096: 12.1 us, 6.6 through LDS).
+
+// The waves' sums, added in LDS, a fragment of the result a wave.
+template <int FM, int FN, int W>
+__device__ __forceinline__ void join_few(const I8Args& g, char* mem, int wave, int lane, int64_t m0, int64_t n0,
+                                         const int4v (&acc)[FM][FN]) {
+  __syncthreads();  // every wave is done with its stages
+  int4v* part = (int4v*)mem;  // [W][FM * FN][64]
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) part[(wave * FM * FN + i * FN + j) * 64 + lane] = acc[i][j];
+  __syncthreads();
+  for (int f = wave; f < FM * FN; f += W) {
+    int4v sum[1][1] = {{part[f * 64 + lane]}};
+#pragma unroll
+    for (int w = 1; w < W; ++w) sum[0][0] += part[(w * FM * FN + f) * 64 + lane];
+    epilogue_i8<1, 1>(g, m0 + f / FN * 16 + (lane & 15), n0 + f % FN * 16 + 4 * (lane >> 4), sum);
+  }
+}
+
+// Rows that start on any byte, any K: through two register sets.
+template <int FM, int FN, int W>
+__global__ void __launch_bounds__(W * 64) gemm_i8_few_any_kernel(I8Args g) {
+  constexpr int A_BYTES = FM * 2048, STAGE = A_BYTES + FN * 2048;
+  constexpr int ALL = W * STAGE, SUMS = W * FM * FN * 1024;
+  __shared__ __attribute__((aligned(1024))) char mem[ALL > SUMS ? ALL : SUMS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t n0 = (int64_t)blockIdx.x * (FN * 16);
-  const int8_t *ra[FM], *rb[FN];
+  const int64_t n0 = (int64_t)blockIdx.x * (FN * 16), m0 = (int64_t)blockIdx.y * (FM * 16);
+  const int steps = (int)ceil_div(g.K, (int64_t)BKB), per = (int)ceil_div(steps, W);
+  const int s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
+  const int8_t *ra[2 * FM], *rb[2 * FN];
+  int kc[2];  // (a lane's k within a step depends on its load's parity)
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int64_t m = i * 16 + (lane & 15);
-    ra[i] = g.a + (m < g.M ? m : g.M - 1) * g.lda + 16 * (lane >> 4);
+  for (int i = 0; i < 2 * FM; ++i) {
+    const lds::LoadPos q = lds::load_pos<true, FM * 16, 2 * FM>(0, lane, i);
+    ra[i] = g.a + (m0 + q.r < g.M ? m0 + q.r : g.M - 1) * g.lda;
+    if (i < 2) kc[i] = q.c * 2;
   }
 #pragma unroll
-  for (int j = 0; j < FN; ++j) {
-    const int64_t n = n0 + j * 16 + (lane & 15);
-    rb[j] = g.b + (n < g.N ? n : g.N - 1) * g.ldb + 16 * (lane >> 4);
+  for (int i = 0; i < 2 * FN; ++i) {
+    const lds::LoadPos q = lds::load_pos<true, FN * 16, 2 * FN>(0, lane, i);
+    rb[i] = g.b + (n0 + q.r < g.N ? n0 + q.r : g.N - 1) * g.ldb;
   }
-  // this wave's steps of 64 k
-  const int steps = (int)ceil_div(g.K, 64), per = (int)ceil_div(steps, FEW_WAVES);
-  const int s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps, full = (int)(g.K / 64);
+  struct Set {
+    uint4 a[2 * FM], b[2 * FN];
+  };
+  auto load = [&](Set& v, int s) {
+    const int64_t k0 = (int64_t)s * BKB;
+    if (k0 + BKB <= g.K) {
+#pragma unroll
+      for (int i = 0; i < 2 * FN; ++i) v.b[i] = load_bytes(rb[i] + k0 + kc[i & 1]);
+#pragma unroll
+      for (int i = 0; i < 2 * FM; ++i) v.a[i] = load_bytes(ra[i] + k0 + kc[i & 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2 * FN; ++i) v.b[i] = load_row(rb[i], k0 + kc[i & 1], g.K);
+#pragma unroll
+      for (int i = 0; i < 2 * FM; ++i) v.a[i] = load_row(ra[i], k0 + kc[i & 1], g.K);
+#pragma unroll
+      for (int i = 0; i < 2 * FN; ++i) v.b[i] = fix_row(v.b[i], k0 + kc[i & 1], g.K);
+#pragma unroll
+      for (int i = 0; i < 2 * FM; ++i) v.a[i] = fix_row(v.a[i], k0 + kc[i & 1], g.K);
+    }
+  };
   int4v acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
-  int s = s0;
-  for (; s + UN <= s1 && s + UN <= full; s += UN) {
-    uint4 fb[UN][FN], fa[UN][FM];
+  const lds::LaneFrag fl = lds::lane_frag<true, 64>(lane);
+  char* const own = mem + wave * STAGE;
+  Set set[2];
+  if (s0 < s1) load(set[0], s0);
+  if (s0 + 1 < s1) load(set[1], s0 + 1);
+  for (int t = s0; t < s1; t += 2) {
 #pragma unroll
-    for (int u = 0; u < UN; ++u) {
+    for (int u = 0; u < 2; ++u) {
+      if (t + u >= s1) break;
+      // (one wave's LDS accesses run in order: its writes, then its reads)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fb[u][j] = load_bytes(rb[j] + (int64_t)(s + u) * 64);
+      for (int i = 0; i < 2 * FM; ++i) *(uint4*)(own + i * 1024 + lane * 16) = set[u].a[i];
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fa[u][i] = load_bytes(ra[i] + (int64_t)(s + u) * 64);
+      for (int i = 0; i < 2 * FN; ++i) *(uint4*)(own + A_BYTES + i * 1024 + lane * 16) = set[u].b[i];
+      if (t + u + 2 < s1) load(set[u], t + u + 2);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        uint4 fa[FM], fb[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fb[j] = lds::fragment<true, FN * 16>(own + A_BYTES, j * 16, kk, fl);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) fa[i] = lds::fragment<true, FM * 16>(own, i * 16, kk, fl);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa[i], acc[i][j]);
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[u][j], fa[u][i], acc[i][j]);
   }
-  for (; s < s1; ++s) {  // (row_chunk counts k from the row's start)
-    const int64_t k = (int64_t)s * 64 + 16 * (lane >> 4);
-    uint4 fa[FM], fb[FN];
-#pragma unroll
-    for (int j = 0; j < FN; ++j) fb[j] = row_chunk(rb[j] - 16 * (lane >> 4), k, g.K);
-#pragma unroll
-    for (int i = 0; i < FM; ++i) fa[i] = row_chunk(ra[i] - 16 * (lane >> 4), k, g.K);
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa[i], acc[i][j]);
-  }
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) part[wave][i * FN + j][lane] = acc[i][j];
-  __syncthreads();
-  if (wave >= FM * FN) return;
-  int4v sum[1][1] = {{part[0][wave][lane]}};
-#pragma unroll
-  for (int w = 1; w < FEW_WAVES; ++w) sum[0][0] += part[w][wave][lane];
-  epilogue_i8<1, 1>(g, 0, wave / FN * 16 + (lane & 15), n0 + wave % FN * 16 + 4 * (lane >> 4), sum);
+  join_few<FM, FN, W>(g, mem, wave, lane, m0, n0, acc);
 }
 
-// The same for 16-byte aligned rows: a wave's pieces go straight to LDS of its
-// own (whole 128-byte lines of a row per eight lanes; fragments read from
-// memory touch four rows in every four lanes, which the cache answers a line
-// at a time), NS steps of 128 k in flight and no barrier before the sums.
+// 16-byte aligned rows: straight to LDS, NS steps of 128 k in flight.
 template <int FM, int FN, int W, int NS>
 __global__ void __launch_bounds__(W * 64) gemm_i8_few_lds_kernel(I8Args g) {
   constexpr int A_BYTES = FM * 2048, B_BYTES = FN * 2048, STAGE = A_BYTES + B_BYTES, LPT = 2 * (FM + FN);
@@ -461,6 +557,9 @@ __global__ void __launch_bounds__(W * 64) gemm_i8_few_lds_kernel(I8Args g) {
   I8Loader<FN * 16, 2 * FN, true> lb;
   la.init(I8Operand{g.a, g.lda, g.M, g.K}, m0, kbeg, 0, lane);
   lb.init(I8Operand{g.b, g.ldb, g.N, g.K}, n0, kbeg, 0, lane);
+  const bool last = wave == W - 1 && (g.K & 15) != 0;
+  LastBytes<FM, FN> held;
+  if (last) held.load(g, lane, m0 + (lane & 15), n0 + (lane & 15));
   char* const own = mem + wave * (NS * STAGE);
   const uint32_t at = lds::lds_address(own);
 #pragma unroll
@@ -474,22 +573,6 @@ __global__ void __launch_bounds__(W * 64) gemm_i8_few_lds_kernel(I8Args g) {
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
-  if (wave == W - 1 && (g.K & 15) != 0) {  // the last bytes (see gemm_i8_kernel)
-    const int64_t k = g.K & ~(int64_t)15;
-    uint4 fb[FN];
-#pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int64_t n = n0 + j * 16 + lane < g.N ? n0 + j * 16 + lane : g.N - 1;
-      fb[j] = lane < 16 ? row_chunk(g.b + n * g.ldb, k, g.K) : make_uint4(0, 0, 0, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int64_t m = m0 + i * 16 + lane < g.M ? m0 + i * 16 + lane : g.M - 1;
-      const uint4 fa = lane < 16 ? row_chunk(g.a + m * g.lda, k, g.K) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[j], fa, acc[i][j]);
-    }
-  }
   const lds::LaneFrag fl = lds::lane_frag<true, 64>(lane);
   for (int t = 0; t < nk; ++t) {
     lds::wait_tiles<NS - 1, LPT>(nk - 1 - t < NS - 1 ? nk - 1 - t : NS - 1);  // this wave's step t has landed
@@ -516,19 +599,8 @@ __global__ void __launch_bounds__(W * 64) gemm_i8_few_lds_kernel(I8Args g) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<I8>::run(fb[kk][j], fa[kk][i], acc[i][j]);
   }
-  __syncthreads();  // every wave is done with its stages
-  int4v* part = (int4v*)mem;  // [W][FM * FN][64]
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) part[(wave * FM * FN + i * FN + j) * 64 + lane] = acc[i][j];
-  __syncthreads();
-  for (int f = wave; f < FM * FN; f += W) {
-    int4v sum[1][1] = {{part[f * 64 + lane]}};
-#pragma unroll
-    for (int w = 1; w < W; ++w) sum[0][0] += part[(w * FM * FN + f) * 64 + lane];
-    epilogue_i8<1, 1>(g, 0, m0 + f / FN * 16 + (lane & 15), n0 + f % FN * 16 + 4 * (lane >> 4), sum);
-  }
+  if (last) held.add(g, acc);
+  join_few<FM, FN, W>(g, mem, wave, lane, m0, n0, acc);
 }
 
 typedef lds::Tile<64, 64, 2, 2, 2> TileI64;
@@ -537,52 +609,73 @@ typedef lds::Tile<64, 64, 2, 2, 2> TileI64;
 typedef lds::Tile<128, 128, 2, 2, 1> TileI128;
 typedef lds::Tile<256, 128, 4, 2, 2> TileI256x128;
 
-// 16-byte aligned rows that the direct-to-LDS kernel takes.
-bool i8_aligned(const I8Args& g) {
-  return g.K >= 16 && aligned(g.a, 16) && aligned(g.b, 16) && g.lda % 16 == 0 && g.ldb % 16 == 0 &&
-         g.lda <= I8_MAX_LD && g.ldb <= I8_MAX_LD;
+// 16-byte aligned rows, which the direct-to-LDS kernels take (K >= 16).
+bool rows_aligned(const int8_t* p, int64_t ld) { return aligned(p, 16) && ld % 16 == 0 && ld <= I8_MAX_LD; }
+
+// Unaligned operands of products of more than 256 tiles of 256 x 128 are
+// worth a copy to aligned rows: 4095^3 109 us as they are, 61 aligned, the
+// copy about 12.
+int64_t packed_ld(int64_t K) { return ceil_div(K, BKB) * BKB; }
+bool pack_pays(int64_t M, int64_t N, int64_t K) {
+  if (K % 16 == 0 || K < 16) return false;
+  const int64_t tm = ceil_div(M, 256), tn = ceil_div(N, 128);
+  // (a copy's chunks are counted in 32 bits)
+  return tm > 256 / tn && M <= (((int64_t)1 << 32) - 1) / (packed_ld(K) / 16) &&
+         N <= (((int64_t)1 << 32) - 1) / (packed_ld(K) / 16);
 }
 
 template <class TL, int NS>
-void launch_i8(const I8Args& g, int splits, hipStream_t st) {
-  const dim3 grid((unsigned)(ceil_div(g.M, TL::BM) * ceil_div(g.N, TL::BN)), (unsigned)splits);
+void launch_i8(const I8Args& g, hipStream_t st) {
+  const dim3 grid((unsigned)(ceil_div(g.M, TL::BM) * ceil_div(g.N, TL::BN)));
   if (g.K % BKB != 0)
     hipLaunchKernelGGL((gemm_i8_kernel<TL, NS, true>), grid, dim3(TL::NT), 0, st, g);
   else
     hipLaunchKernelGGL((gemm_i8_kernel<TL, NS, false>), grid, dim3(TL::NT), 0, st, g);
 }
 
-template <int FM, int FN, int UN>
-mdnn_status_t launch_few(const I8Args& g, hipStream_t st) {
-  hipLaunchKernelGGL((gemm_i8_few_kernel<FM, FN, UN>), dim3((unsigned)ceil_div(g.N, FN * 16)), dim3(FEW_WAVES * 64), 0,
-                     st, g);
-  return check_launch("gemm_i8_few_kernel");
+template <class TL, int NR>
+void launch_any(const I8Args& g, hipStream_t st) {
+  const int64_t tiles = ceil_div(g.M, TL::BM) * ceil_div(g.N, TL::BN);
+  hipLaunchKernelGGL((gemm_i8_any_kernel<TL, NR>), dim3((unsigned)tiles), dim3(TL::NT), 0, st, g);
 }
 
 template <int FM, int FN, int W, int NS>
-mdnn_status_t launch_few_lds(const I8Args& g, hipStream_t st) {
-  hipLaunchKernelGGL((gemm_i8_few_lds_kernel<FM, FN, W, NS>), dim3((unsigned)ceil_div(g.N, FN * 16), (unsigned)ceil_div(g.M, FM * 16)), dim3(W * 64), 0,
-                     st, g);
-  return check_launch("gemm_i8_few_lds_kernel");
+mdnn_status_t launch_few(const I8Args& g, bool rows16, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(g.N, FN * 16), (unsigned)ceil_div(g.M, FM * 16));
+  if (rows16)
+    hipLaunchKernelGGL((gemm_i8_few_lds_kernel<FM, FN, W, NS>), grid, dim3(W * 64), 0, st, g);
+  else
+    hipLaunchKernelGGL((gemm_i8_few_any_kernel<FM, FN, W>), grid, dim3(W * 64), 0, st, g);
+  return check_launch("gemm_i8_few_kernel");
 }
 
 // Few rows: FM fragments of rows; FN columns of 16 as the caller chose.
 template <int FN>
-mdnn_status_t run_few(const I8Args& g, hipStream_t st) {
-  if (g.M <= 16) return launch_few_lds<1, FN, 8, 2>(g, st);
-  if (g.M <= 32) return launch_few_lds<2, FN, 4, 3>(g, st);
-  if (g.M <= 48) return launch_few_lds<3, FN, 4, FN == 1 ? 3 : 2>(g, st);
-  return launch_few_lds<4, FN, 4, FN == 1 ? 3 : 2>(g, st);
+mdnn_status_t run_few(const I8Args& g, bool rows16, hipStream_t st) {
+  if (g.M <= 16) return launch_few<1, FN, 8, 2>(g, rows16, st);
+  if (g.M <= 32) return launch_few<2, FN, 4, 3>(g, rows16, st);
+  if (g.M <= 48) return launch_few<3, FN, 4, FN == 1 ? 3 : 2>(g, rows16, st);
+  return launch_few<4, FN, 4, FN == 1 ? 3 : 2>(g, rows16, st);
 }
 
-mdnn_status_t run_i8(const I8Args& g, hipStream_t st) {
-  if (!i8_aligned(g)) {
-    if (g.M <= 16) return launch_few<1, 1, 8>(g, st);
-    if (g.M <= 64) return launch_few<4, 1, 4>(g, st);
-    const int64_t tiles = ceil_div(g.M, TileI64::BM) * ceil_div(g.N, TileI64::BN);
-    hipLaunchKernelGGL((gemm_i8_any_kernel<TileI64>), dim3((unsigned)tiles), dim3(TileI64::NT), 0, st, g);
-    return check_launch("gemm_i8_any_kernel");
+mdnn_status_t run_i8(I8Args g, void* ws, size_t ws_bytes, hipStream_t st) {
+  bool a16 = rows_aligned(g.a, g.lda), b16 = rows_aligned(g.b, g.ldb);
+  if ((!a16 || !b16) && ws && pack_pays(g.M, g.N, g.K) && ws_bytes >= mdnn_gemm_i8_workspace(g.M, g.N, g.K)) {
+    const int64_t ld = packed_ld(g.K);
+    PackArgs p = {};
+    p.K = g.K, p.per = (uint32_t)(ld / 16);
+    p.p[0] = g.a, p.ld[0] = g.lda, p.to[0] = (int8_t*)ws, p.chunks[0] = a16 ? 0 : (uint32_t)g.M * p.per;
+    p.p[1] = g.b, p.ld[1] = g.ldb, p.to[1] = (int8_t*)ws + g.M * ld, p.chunks[1] = b16 ? 0 : (uint32_t)g.N * p.per;
+    const uint32_t most = p.chunks[0] > p.chunks[1] ? p.chunks[0] : p.chunks[1];
+    const uint32_t blocks = most / 256 + 1;
+    hipLaunchKernelGGL(pack_rows_kernel, dim3(blocks < 65536 ? blocks : 65536, 2), dim3(256), 0, st, p);
+    MDNN_TRY(check_launch("pack_rows_kernel"));
+    if (!a16 && !b16) g.K = ld;  // (zeros past K in both)
+    if (!a16) g.a = p.to[0], g.lda = ld;
+    if (!b16) g.b = p.to[1], g.ldb = ld;
+    a16 = b16 = true;
   }
+  const bool rows16 = a16 && b16 && g.K >= 16;
   auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(g.M, bm) * ceil_div(g.N, bn); };
   // Up to one workgroup per CU, the few-rows kernel's waves that share K beat
   // a 64 x 64 tile's serial loop over it: 64 x 16 tiles (64 x 4096 x 4096 6.6
@@ -593,8 +686,20 @@ mdnn_status_t run_i8(const I8Args& g, hipStream_t st) {
   // (64 x 8192 x 8192 14.8 us, 64 x 64 tiles 16.3; 16384 x 32 x 4096 13.4,
   // 18.6).  64 x 16 tiles read A once per 16 columns: not where A is the
   // larger operand (4096 x 64 x 4096: 12.2 us, 64 x 32 tiles 8.0).
-  if (g.M <= 16 || g.N <= 16 || (tiles(g.M <= 32 ? 32 : 64, 16) <= 256 && g.M <= g.N)) return run_few<1>(g, st);
-  if (g.M <= 64 || g.N <= 32 || tiles(64, 32) <= 256) return run_few<2>(g, st);
+  if (g.M <= 16 || g.N <= 16 || (tiles(g.M <= 32 ? 32 : 64, 16) <= 256 && g.M <= g.N)) return run_few<1>(g, rows16, st);
+  if (g.M <= 64 || g.N <= 32 || tiles(64, 32) <= 256) return run_few<2>(g, rows16, st);
+  if (!rows16) {
+    // 256 x 128 tiles from more than 256 of them on (4095^3 109 us, 128 x 128
+    // tiles 120, 64 x 64 205), 128 x 128 from more than 128 (2000 x 2000 x 3001
+    // 27 us, 41 and 44; 1000 x 2000 x 3001 25.7, 64 x 64 25.0)
+    if (tiles(256, 128) > 256)
+      launch_any<lds::Tile<256, 128, 4, 2, 2>, 2>(g, st);
+    else if (tiles(128, 128) > 128)
+      launch_any<lds::Tile<128, 128, 2, 4, 2>, 2>(g, st);
+    else
+      launch_any<TileI64, 2>(g, st);
+    return check_launch("gemm_i8_any_kernel");
+  }
   // 256 x 256 tiles from more than 256 tiles of 256 x 128 on (4096^3 61 us,
   // 256 x 128 tiles 73; 3000 x 3008 x 2000, 144 tiles, 35 and 44), unless
   // their padding takes the gain; 256 x 128 while they fill one workgroup per
@@ -603,13 +708,13 @@ mdnn_status_t run_i8(const I8Args& g, hipStream_t st) {
   // 256 x 128 29), and 64 x 64 up to 128 of those (1024 x 2048 x 4096 16.3
   // us, 128 x 128 20.9)
   if (tiles(256, 128) > 256 && 5 * tiles(256, 256) <= 3 * tiles(256, 128))
-    launch_i8<lds::Tile256, 2>(g, 1, st);
+    launch_i8<lds::Tile256, 2>(g, st);
   else if (tiles(256, 128) > 160)
-    launch_i8<TileI256x128, 3>(g, 1, st);
+    launch_i8<TileI256x128, 3>(g, st);
   else if (tiles(128, 128) > 128)
-    launch_i8<TileI128, 3>(g, 1, st);
+    launch_i8<TileI128, 3>(g, st);
   else
-    launch_i8<TileI64, 4>(g, 1, st);
+    launch_i8<TileI64, 4>(g, st);
   return check_launch("gemm_i8_kernel");
 }
 
@@ -619,8 +724,8 @@ mdnn_status_t run_i8(const I8Args& g, hipStream_t st) {
 using namespace mdnn;
 
 extern "C" size_t mdnn_gemm_i8_workspace(int64_t M, int64_t N, int64_t K) {
-  (void)M, (void)N, (void)K;
-  return 0;
+  if (M < 0 || N < 0 || K < 0 || K > I8_MAX_K || M == 0 || N == 0 || !pack_pays(M, N, K)) return 0;
+  return (size_t)(M + N) * (size_t)packed_ld(K);
 }
 
 extern "C" mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t* A, int64_t lda,
@@ -640,11 +745,10 @@ extern "C" mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int
   // (a launch holds fewer than 2^32 threads)
   if (M > INT64_MAX - 64 || N > INT64_MAX - 64 || ceil_div(M, 64) > (((int64_t)1 << 24) - 1) / ceil_div(N, 64))
     return fail(MDNN_ERR_SHAPE, "gemm_i8: problem too large for the launch grid");
-  (void)ws_bytes;
   I8Args g = {};
   g.a = A, g.b = B, g.a_scale = a_scale, g.b_scale = b_scale, g.bias = bias, g.d = D;
   g.M = M, g.N = N, g.K = K, g.lda = lda, g.ldb = ldb, g.ldd = ldd, g.act = act;
   g.d_type = d_type;
   clear_error();
-  return run_i8(g, as_stream(stream));
+  return run_i8(g, workspace, ws_bytes, as_stream(stream));
 }

@@ -182,6 +182,28 @@ def test_product_tiles(mdnn, M, N, K):
         _check(mdnn, M, N, K, out, padded, bias=out != "f32", relu=out == "bf16", offset=offset, ldd_pad=3, seed=N)
 
 
+@pytest.mark.parametrize("M,N,K", [(4200, 4300, 131), (8200, 2100, 45), (1025, 16500, 16 * 9 + 1)])
+def test_product_rows_copied(mdnn, M, N, K):
+    """Large products with unaligned rows copy them into the workspace; one operand or both; a workspace too small,
+    or none, gives the same result, and nothing past it is written."""
+    import torch
+    need = mdnn.mdnn_gemm_i8_workspace(M, N, K)
+    assert need == (M + N) * ((K + 127) // 128 * 128)
+    g = np.random.default_rng(K)
+    sa, sb = dev(g.random(M).astype(np.float32), "f32"), dev(g.random(N).astype(np.float32), "f32")
+    for a_pad, b_pad in ((False, False), (True, False), (False, True)):
+        a, av = _codes(M, K, 1, (K + 15) // 16 * 16 if a_pad else K, 0 if a_pad else 3)
+        b, bv = _codes(N, K, 2, (K + 15) // 16 * 16 if b_pad else K + 5, 0 if b_pad else 1)
+        ws = torch.full((need + 64,), GUARD, dtype=torch.uint8, device="cuda")
+        d = mdnn.gemm_i8(a, sa, b, sb, workspace=ws[:need])
+        assert bool((ws[need:] == GUARD).all())
+        assert torch.equal(d, mdnn.gemm_i8(a, sa, b, sb))
+        assert torch.equal(d, mdnn.gemm_i8(a, sa, b, sb, workspace=ws[:need - 16]))
+        acc = torch.from_numpy(av.astype(np.float64)).cuda() @ torch.from_numpy(bv.astype(np.float64)).cuda().T
+        want = acc * sa.double()[:, None] * sb.double()
+        assert bool(((d.double() - want).abs() <= 3.01 * U * want.abs()).all())
+
+
 def test_product_strided_rows(mdnn):
     """Rows far apart, outputs inside a wider matrix; what lies between stays."""
     for ldd_pad in (1, 4, 5):
