@@ -207,6 +207,16 @@ def _codes_like(q, rows: int, cols: int, device):
     return q, _rows_of(q, "q")[2]
 
 
+def _bytes_of(ws):
+    """(tensor, bytes) of an optional workspace on the current device."""
+    import torch
+    if ws is None:
+        return None, 0
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device.index != torch.cuda.current_device():
+        raise ValueError("workspace must be contiguous bytes on the current GPU")
+    return ws, ws.numel()
+
+
 def quantize_i8(x, transpose: bool = False, q=None, scale=None, workspace=None, stream=None):
     """(codes, scales) of a 2-D tensor: int8 codes with an fp32 scale for each
     row, or with transpose for each column, the codes stored [cols, rows] (a
@@ -222,7 +232,7 @@ def quantize_i8(x, transpose: bool = False, q=None, scale=None, workspace=None, 
     if workspace is None:
         workspace = torch.empty((max(mdnn_quantize_i8_t_workspace(rows, cols), 16),), dtype=torch.uint8,
                                 device=x.device)
-    mdnn_quantize_i8_t(rows, cols, x, ldx, dtype_of(x), q, ldq, scale, workspace, workspace.numel(), stream)
+    mdnn_quantize_i8_t(rows, cols, x, ldx, dtype_of(x), q, ldq, scale, *_bytes_of(workspace), stream)
     return q, scale
 
 
@@ -244,7 +254,7 @@ def gemm_i8(A, a_scale, B, b_scale, bias=None, act: int = ACT_NONE, out_dtype=No
     if workspace is True:
         workspace = torch.empty((max(mdnn_gemm_i8_workspace(M, N, K), 16),), dtype=torch.uint8, device=A.device)
     mdnn_gemm_i8(M, N, K, A, lda, a_scale, B, ldb, b_scale, bias, act, out, _rows_of(out, "out")[2], dtype_of(out),
-                 workspace, workspace.numel() if workspace is not None else 0, stream)
+                 *_bytes_of(workspace), stream)
     return out
 
 
@@ -301,7 +311,7 @@ def rmsnorm_bwd(dy, h, gamma=None, eps: float = 1e-6, dres=None, dx=None, with_d
         workspace = torch.empty((max(mdnn_rmsnorm_bwd_workspace(rows, cols), 256),), dtype=torch.uint8,
                                 device=dy.device)
     mdnn_rmsnorm_bwd(rows, cols, dy, lddy, h, ldh, _vector_of(gamma, cols, "gamma"), eps, dres, lddr, dx, lddx, dgamma,
-                     dtype_of(dy), workspace, workspace.numel() if workspace is not None else 0, stream)
+                     dtype_of(dy), *_bytes_of(workspace), stream)
     return dx, dgamma
 
 

@@ -617,11 +617,11 @@ bool rows_aligned(const int8_t* p, int64_t ld) { return aligned(p, 16) && ld % 1
 // copy about 12.
 int64_t packed_ld(int64_t K) { return ceil_div(K, BKB) * BKB; }
 bool pack_pays(int64_t M, int64_t N, int64_t K) {
-  if (K % 16 == 0 || K < 16) return false;
+  if (K % 16 == 0 || K < 16 || M <= 64 || N <= 32) return false;  // (few rows or columns: see run_i8)
   const int64_t tm = ceil_div(M, 256), tn = ceil_div(N, 128);
-  // (a copy's chunks are counted in 32 bits)
-  return tm > 256 / tn && M <= (((int64_t)1 << 32) - 1) / (packed_ld(K) / 16) &&
-         N <= (((int64_t)1 << 32) - 1) / (packed_ld(K) / 16);
+  // (a copy's chunks, and the stride over them, are counted in 32 bits)
+  const int64_t rows = ((int64_t)1 << 31) / (packed_ld(K) / 16);
+  return tm > 256 / tn && M <= rows && N <= rows;
 }
 
 template <class TL, int NS>
@@ -686,8 +686,11 @@ mdnn_status_t run_i8(I8Args g, void* ws, size_t ws_bytes, hipStream_t st) {
   // (64 x 8192 x 8192 14.8 us, 64 x 64 tiles 16.3; 16384 x 32 x 4096 13.4,
   // 18.6).  64 x 16 tiles read A once per 16 columns: not where A is the
   // larger operand (4096 x 64 x 4096: 12.2 us, 64 x 32 tiles 8.0).
-  if (g.M <= 16 || g.N <= 16 || (tiles(g.M <= 32 ? 32 : 64, 16) <= 256 && g.M <= g.N)) return run_few<1>(g, rows16, st);
-  if (g.M <= 64 || g.N <= 32 || tiles(64, 32) <= 256) return run_few<2>(g, rows16, st);
+  // (Their grid: fewer than 2^32 threads by column tiles, row tiles in y.)
+  const bool fits = g.N < (int64_t)1 << 26 && g.M <= (int64_t)65535 * 64;
+  if (fits && (g.M <= 16 || g.N <= 16 || (tiles(g.M <= 32 ? 32 : 64, 16) <= 256 && g.M <= g.N)))
+    return run_few<1>(g, rows16, st);
+  if (fits && (g.M <= 64 || g.N <= 32 || tiles(64, 32) <= 256)) return run_few<2>(g, rows16, st);
   if (!rows16) {
     // 256 x 128 tiles from more than 256 of them on (4095^3 109 us, 128 x 128
     // tiles 120, 64 x 64 205), 128 x 128 from more than 128 (2000 x 2000 x 3001

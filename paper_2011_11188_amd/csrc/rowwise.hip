@@ -540,22 +540,26 @@ __global__ void __launch_bounds__(BWD_NT(TPR)) norm_bwd_kernel(BwdArgs a) {
 __global__ void __launch_bounds__(1024) dgamma_kernel(const float* partial, int blocks, int64_t cols, float* dgamma) {
   __shared__ float part[32][32];
   const int cx = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int64_t c = (int64_t)blockIdx.x * 32 + cx;
-  const float* p = partial + (c < cols ? c : cols - 1);
-  float s = 0.0f;
-  for (int b0 = r; b0 < blocks; b0 += 512) {
-    float v[16];
+  for (int64_t c0 = (int64_t)blockIdx.x * 32; c0 < cols; c0 += (int64_t)gridDim.x * 32) {
+    const int64_t c = c0 + cx;
+    const float* p = partial + (c < cols ? c : cols - 1);
+    float s = 0.0f;
+    for (int b0 = r; b0 < blocks; b0 += 512) {
+      float v[16];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] = p[(int64_t)(b0 + 32 * k < blocks ? b0 + 32 * k : r) * cols];
+      for (int k = 0; k < 16; ++k) v[k] = p[(int64_t)(b0 + 32 * k < blocks ? b0 + 32 * k : r) * cols];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += b0 + 32 * k < blocks ? v[k] : 0.0f;
+      for (int k = 0; k < 16; ++k) s += b0 + 32 * k < blocks ? v[k] : 0.0f;
+    }
+    part[r][cx] = s;
+    __syncthreads();
+    if (r == 0 && c < cols) {
+#pragma unroll
+      for (int k = 1; k < 32; ++k) s += part[k][cx];
+      dgamma[c] = s;
+    }
+    __syncthreads();  // (before the sums of the next columns)
   }
-  part[r][cx] = s;
-  __syncthreads();
-  if (r > 0 || c >= cols) return;
-#pragma unroll
-  for (int k = 1; k < 32; ++k) s += part[k][cx];
-  dgamma[c] = s;
 }
 
 // Rows of any length: read twice, dgamma's sums kept in the block's own row
@@ -964,7 +968,8 @@ extern "C" mdnn_status_t mdnn_rmsnorm_bwd(int64_t rows, int64_t cols, const void
     default: MDNN_TRY(run_bwd<BF16>(a, st)); break;
   }
   if (!dgamma) return MDNN_SUCCESS;
-  hipLaunchKernelGGL(dgamma_kernel, dim3((unsigned)ceil_div(cols, 32)), dim3(1024), 0, st, (const float*)workspace,
+  const int64_t tiles = ceil_div(cols, 32);
+  hipLaunchKernelGGL(dgamma_kernel, dim3((unsigned)(tiles < MAX_BLOCKS ? tiles : MAX_BLOCKS)), dim3(1024), 0, st, (const float*)workspace,
                      (int)bwd_blocks(rows, cols), cols, dgamma);
   return check_launch("dgamma_kernel");
 }

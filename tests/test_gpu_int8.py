@@ -88,7 +88,8 @@ def _special(cols):
     v[3] = 0
     v[4] *= np.float32(2.0 ** -110)
     v[5] *= np.float32(2.0 ** -140)
-    v[6] = np.clip(v[6] * np.float32(1e38), -3e38, 3e38)
+    with np.errstate(over="ignore"):
+        v[6] = np.clip(v[6] * np.float32(1e38), -3e38, 3e38)
     v[7] = np.float32(2.0 ** -100)
     v[8] = -0.0
     v[9] = np.resize(np.float32([127, 0.5, 1.5, 2.5, -0.5, -1.5, -126.5]), cols)
@@ -285,6 +286,20 @@ def test_product_far_rows(mdnn, M, N, padded):
     assert np.array_equal(mdnn.gemm_i8(b, one[:N], a, one[:M], workspace=True).cpu().numpy(), want.T)
 
 
+@pytest.mark.parametrize("M,N,K", [(4_200_000, 16, 4), (1, (1 << 27) + 5, 4), (20, (1 << 26) + 1, 3)])
+def test_product_more_tiles_than_a_grid_side(mdnn, M, N, K):
+    """More row or column tiles than the few-rows kernels' grid holds."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(1)
+    a = torch.randint(-127, 128, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    b = torch.randint(-127, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    d = mdnn.gemm_i8(a, torch.ones(M, device="cuda"), b, torch.ones(N, device="cuda"), out_dtype=torch.float32)
+    for m in {0, M // 2, M - 1}:
+        assert torch.equal(d[m], (b.float() * a[m].float()).sum(1))
+    for n in {0, N // 2, N - 1}:
+        assert torch.equal(d[:, n], (a.float() * b[n].float()).sum(1))
+
+
 def test_product_layer_of_a_trained_net(mdnn):
     """As it is used: weights of a layer quantised by output channel, a batch normalised into codes, the layer's
     product with bias and ReLU, its result quantised, the next layer's product; against the oracle step by step."""
@@ -364,6 +379,7 @@ def test_api_refuses(mdnn):
                 lambda: mdnn.gemm_i8(a, one.half(), a, one), lambda: mdnn.gemm_i8(a, one, a[:, :16], one),
                 lambda: mdnn.gemm_i8(a.float(), one, a, one), lambda: mdnn.gemm_i8(a, one, a.cpu(), one),
                 lambda: mdnn.gemm_i8(a, one, a, one, bias=one[:2]),
+                lambda: mdnn.gemm_i8(a, one, a, one, workspace=torch.zeros(64, device="cuda")),
                 lambda: mdnn.quantize_i8(a.float().t()), lambda: mdnn.quantize_i8(a.float(), q=a[:, :8]),
                 lambda: mdnn.quantize_i8(a.float(), scale=one[:2]), lambda: mdnn.quantize_i8(a.float().cpu())):
         with pytest.raises(ValueError):

@@ -265,6 +265,20 @@ def test_many_rows(mdnn):
         assert torch.equal(s[lo:lo + (1 << 22)], (a / torch.full_like(a, 127.0)).float()[:, 0])
 
 
+def test_widest_gamma_gradient(mdnn):
+    """More columns than one launch of the gamma gradient's blocks holds threads for."""
+    import torch
+    cols = (1 << 27) + 40
+    h = torch.randn(1, cols, device="cuda").half()
+    dy = torch.randn(1, cols, device="cuda").half()
+    _, dg = mdnn.rmsnorm_bwd(dy, h)
+    rstd = 1 / torch.sqrt(sum(p.double().square().sum() for p in h[0].split(1 << 24)) / cols + 1e-6)
+    for lo in range(0, cols, 1 << 24):
+        want = dy[0, lo:lo + (1 << 24)].double() * h[0, lo:lo + (1 << 24)].double() * rstd
+        # the sum of squares: 2^17 terms a thread
+        assert bool(((dg[lo:lo + (1 << 24)].double() - want).abs() <= _sum_bound(cols) * want.abs() + 1e-30).all())
+
+
 def test_far_rows(mdnn):
     """Rows whose offsets pass 2^32 bytes."""
     import torch
