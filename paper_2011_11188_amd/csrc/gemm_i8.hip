@@ -639,20 +639,24 @@ void launch_any(const I8Args& g, hipStream_t st) {
   hipLaunchKernelGGL((gemm_i8_any_kernel<TL, NR>), dim3((unsigned)tiles), dim3(TL::NT), 0, st, g);
 }
 
-template <int FM, int FN, int W, int NS>
+// W, NS: waves and stages for rows on 16 bytes; WANY: waves for others.
+template <int FM, int FN, int W, int NS, int WANY = W>
 mdnn_status_t launch_few(const I8Args& g, bool rows16, hipStream_t st) {
   const dim3 grid((unsigned)ceil_div(g.N, FN * 16), (unsigned)ceil_div(g.M, FM * 16));
   if (rows16)
     hipLaunchKernelGGL((gemm_i8_few_lds_kernel<FM, FN, W, NS>), grid, dim3(W * 64), 0, st, g);
   else
-    hipLaunchKernelGGL((gemm_i8_few_any_kernel<FM, FN, W>), grid, dim3(W * 64), 0, st, g);
+    hipLaunchKernelGGL((gemm_i8_few_any_kernel<FM, FN, WANY>), grid, dim3(WANY * 64), 0, st, g);
   return check_launch("gemm_i8_few_kernel");
 }
 
-// Few rows: FM fragments of rows; FN columns of 16 as the caller chose.
+// Few rows: FM fragments of rows; FN columns of 16 as the caller chose.  Up to
+// 16 rows four waves of four stages read weights from memory fastest (1 x 4096 x
+// 4096 5.7 us cold, 1 x 8192 x 8192 14.2; eight of two 6.1 and 15.6, where the
+// weights are in the cache 4.3 and 4.2).
 template <int FN>
 mdnn_status_t run_few(const I8Args& g, bool rows16, hipStream_t st) {
-  if (g.M <= 16) return launch_few<1, FN, 8, 2>(g, rows16, st);
+  if (g.M <= 16) return launch_few<1, FN, 4, 4, 8>(g, rows16, st);
   if (g.M <= 32) return launch_few<2, FN, 4, 3>(g, rows16, st);
   if (g.M <= 48) return launch_few<3, FN, 4, FN == 1 ? 3 : 2>(g, rows16, st);
   return launch_few<4, FN, 4, FN == 1 ? 3 : 2>(g, rows16, st);
@@ -709,7 +713,7 @@ mdnn_status_t run_i8(I8Args g, void* ws, size_t ws_bytes, hipStream_t st) {
   // CU (2048 x 4096 x 4096 36 us; 256 x 256 51, 128 x 128 38; 1536 x 4096 x
   // 4096 32, 48, 33); below 160 of them 128 x 128 (1024 x 4096 x 4096 24 us,
   // 256 x 128 29), and 64 x 64 up to 128 of those (1024 x 2048 x 4096 16.3
-  // us, 128 x 128 20.9)
+  // us, 128 x 128 20.9; three stages, 15.4 us for 512 x 4096 x 4096, four 15.8)
   if (tiles(256, 128) > 256 && 5 * tiles(256, 256) <= 3 * tiles(256, 128))
     launch_i8<lds::Tile256, 2>(g, st);
   else if (tiles(256, 128) > 160)
@@ -717,7 +721,7 @@ mdnn_status_t run_i8(I8Args g, void* ws, size_t ws_bytes, hipStream_t st) {
   else if (tiles(128, 128) > 128)
     launch_i8<TileI128, 3>(g, st);
   else
-    launch_i8<TileI64, 4>(g, st);
+    launch_i8<TileI64, 3>(g, st);
   return check_launch("gemm_i8_kernel");
 }
 
