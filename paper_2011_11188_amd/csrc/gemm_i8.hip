@@ -129,7 +129,10 @@ __device__ __forceinline__ void i8_tile(const I8Args& g, int bm, int bn, int& tm
 // Rows that start on any byte, any K: chunks of 16 bytes are read at any
 // address into one of NR register sets (NR steps in flight) and written to the
 // swizzled LDS tiles (two stages, one barrier a step).  A chunk past the row's
-// end is read from its last 16 bytes and shifted; k past K is zero.
+// end is read from its last 16 bytes and shifted; k past K is zero.  1000 x 777
+// x 1531 9.3 us (the latency of 12 steps on one tile per CU), 4095^3 109 us.
+// Four and six sets in flight measured the same (11.1, 11.1 and 11.5 us of a
+// former state of the former): two.
 
 typedef uint32_t u4v_a1 __attribute__((ext_vector_type(4), aligned(1)));
 
@@ -300,7 +303,10 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a) {
 // 16-byte aligned rows (gemm_lds.h's pipeline): every lane's 16 bytes go
 // straight from memory to LDS.  A K that is no multiple of the step reads
 // through a range-checked buffer, whole 16-byte chunks past K as zeros; its
-// last K % 16 bytes are one more fragment step from registers.
+// last K % 16 bytes are one more fragment step from registers.  Large products
+// are bound by the matrix cores at the clock the power limit leaves (4096^3
+// 55-61 us by the data, 16384 x 8192 x 8192 875 us, 2.5 POPS), 64 x 64 tiles by
+// LDS traffic (256 x 4096 x 4096 9.8 us).
 struct I8Operand {
   const int8_t* p;
   int64_t ld, MN, K;
@@ -613,8 +619,8 @@ typedef lds::Tile<256, 128, 4, 2, 2> TileI256x128;
 bool rows_aligned(const int8_t* p, int64_t ld) { return aligned(p, 16) && ld % 16 == 0 && ld <= I8_MAX_LD; }
 
 // Unaligned operands of products of more than 256 tiles of 256 x 128 are
-// worth a copy to aligned rows: 4095^3 109 us as they are, 61 aligned, the
-// copy about 12.
+// worth a copy to aligned rows: 4095^3 109 us as they are, 81 with the copy;
+// 4095 x 4095 x 513 39 and 35; 16383 x 4001 x 1001 161 and 117.
 int64_t packed_ld(int64_t K) { return ceil_div(K, BKB) * BKB; }
 bool pack_pays(int64_t M, int64_t N, int64_t K) {
   if (K % 16 == 0 || K < 16 || M <= 64 || N <= 32) return false;  // (few rows or columns: see run_i8)
@@ -681,6 +687,7 @@ mdnn_status_t run_i8(I8Args g, void* ws, size_t ws_bytes, hipStream_t st) {
   }
   const bool rows16 = a16 && b16 && g.K >= 16;
   auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(g.M, bm) * ceil_div(g.N, bn); };
+  // (K == 0 and other K < 16: the kernels for rows on any byte.)
   // Up to one workgroup per CU, the few-rows kernel's waves that share K beat
   // a 64 x 64 tile's serial loop over it: 64 x 16 tiles (64 x 4096 x 4096 6.6
   // us, 64 x 32 tiles 7.7, 64 x 64 tiles 9.5), then 64 x 32 (128 x 4096 x

@@ -425,6 +425,7 @@ mdnn_status_t run_rows(const RowArgs& a, mdnn_dtype_t t, hipStream_t st) {
 // sums are added in a fixed order.  Loading the next row ahead gained nothing
 // (4096 x 4096 bf16: 28.4 us against 28.1: the other block's loads fill the gap),
 // blocks of 1024 threads wait for each other (28.6; 8192 x 8192 114 against 109).
+// Bound by HBM: 4096 x 4096 fp16 32 us from memory with the blocks' sums (4.4 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int BWD_NT(int tpr) { return tpr <= 512 ? 512 : 1024; }
 struct BwdArgs {
@@ -536,7 +537,8 @@ __global__ void __launch_bounds__(BWD_NT(TPR)) norm_bwd_kernel(BwdArgs a) {
 }
 
 // dgamma from the blocks' sums: 32 columns a block, 32 rows of threads, each
-// adding every 32nd block's sums (sixteen loads in flight), then those in order.
+// adding every 32nd block's sums (sixteen loads in flight), then those in
+// order.  4.8 us for 512 blocks of 4096 columns: a launch and one round trip.
 __global__ void __launch_bounds__(1024) dgamma_kernel(const float* partial, int blocks, int64_t cols, float* dgamma) {
   __shared__ float part[32][32];
   const int cx = threadIdx.x & 31, r = threadIdx.x >> 5;
@@ -638,8 +640,9 @@ mdnn_status_t run_bwd(const BwdArgs& a, hipStream_t st) {
 // columns: codes of x[rows][cols] with a scale for each column, stored
 // transposed, q[cols][rows].  Pass 1: column maxima of row slabs; pass 2:
 // every tile takes its columns' maxima over the slabs, quantises and turns
-// the tile round in LDS (its second read of x is 64 KB of a matrix that the
-// last-level cache still holds).
+// the tile round in LDS.  Bound by x's two reads, the second from the
+// last-level cache where it fits: 4096 x 4096 fp32 25 us, 11.0 (6.1 TB/s) and
+// 14.4 us (5.8 TB/s).
 // ---------------------------------------------------------------------------
 // Rows of a slab: about a thousand blocks of 256 columns in pass 1, at most
 // 256 slabs (every tile of pass 2 reads its columns' maxima of each).

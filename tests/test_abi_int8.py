@@ -75,6 +75,19 @@ def test_gemm_i8_workspace_of_bad_sizes(m):
     assert m.mdnn_gemm_i8_workspace(-1, 4, 4) == 0 and m.mdnn_gemm_i8_workspace(4, 4, 1 << 20) == 0
 
 
+def test_gemm_i8_workspace_is_for_copies_of_large_odd_operands(m):
+    ws = m.mdnn_gemm_i8_workspace
+    assert ws(4095, 4095, 4095) == (4095 + 4095) * 4096
+    # whole 16-byte rows, few rows or columns, small products: no copy
+    for size in ((4096, 4096, 4096), (4096, 4096, 4000), (64, 100000, 4095), (100000, 32, 4095), (1000, 777, 1531),
+                 (4096, 4096, 15), (0, 4096, 4095)):
+        assert ws(*size) == 0, size
+    # the first size above 256 tiles of 256 x 128 (16 x 16 of them at 4096 x 2048)
+    assert ws(4096, 2048, 33) == 0 and ws(4097, 2048, 33) == (4097 + 2048) * 128
+    # a copy's chunks are counted in 32 bits
+    assert ws((1 << 31) // 8 + 1, 64, 100) == 0 and ws(1 << 28, 64, 100) > 0
+
+
 NORM = dict(rows=4, cols=8, x=FAKE, ldx=8, res=FAKE, ldr=8, gamma=FAKE, eps=1e-6, h=FAKE, ldh=8)
 
 
