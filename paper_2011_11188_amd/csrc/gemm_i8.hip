@@ -37,6 +37,8 @@ struct I8Args {
   void* d;
   int64_t M, N, K, lda, ldb, ldd;
   int32_t act, d_type;
+  uint32_t group;    // tile rows a group of workgroups walks together (tile columns with by_cols)
+  bool by_cols;
 };
 
 // ------------------------------------------------------------- epilogue
@@ -111,18 +113,35 @@ __device__ __forceinline__ void epilogue_i8(const I8Args& g, int64_t mb, int64_t
   }
 }
 
-// Tile of a workgroup: tile_coords' order (consecutive ids on one
-// XCD, eight tile rows a group) in 32-bit arithmetic; the 64-bit divisions
-// had taken a small product's prologue.
+// Tile of a workgroup: consecutive ids run on one XCD and walk groups of
+// `group` tile rows column by column (by_cols: groups of tile columns row by
+// row), so that the tiles at work on an XCD share its L2's panels of both
+// operands.  In 32-bit arithmetic: the 64-bit divisions of tile_coords had
+// taken a small product's prologue.
 __device__ __forceinline__ void i8_tile(const I8Args& g, int bm, int bn, int& tm, int& tn) {
   const uint32_t tiles_m = (uint32_t)((g.M + bm - 1) / bm), tiles_n = (uint32_t)((g.N + bn - 1) / bn);
+  const uint32_t major = g.by_cols ? tiles_n : tiles_m, minor = g.by_cols ? tiles_m : tiles_n;
   uint32_t id = blockIdx.x;
   if (gridDim.x % 8 == 0) id = (id % 8) * (gridDim.x / 8) + id / 8;
-  constexpr uint32_t GROUP_M = 8;
-  const uint32_t group = GROUP_M * tiles_n, gid = id / group, in = id - gid * group, first = gid * GROUP_M;
-  const uint32_t size = tiles_m - first < GROUP_M ? tiles_m - first : GROUP_M, col = in / size;
-  tm = (int)(first + in - col * size);
-  tn = (int)col;
+  const uint32_t whole = g.group * minor, gid = id / whole, in = id - gid * whole, first = gid * g.group;
+  const uint32_t size = major - first < g.group ? major - first : g.group, b = in / size, a = first + in - b * size;
+  tm = (int)(g.by_cols ? b : a);
+  tn = (int)(g.by_cols ? a : b);
+}
+
+// The order of the tiles.  Which tiles run at once also decides which pieces
+// of D are written together, and a D of hundreds of MB whose rows are whole
+// multiples of 4 KB is slow to write down its columns: groups of 16 tile
+// columns where D is at least as wide as tall (16384 x 16384 x 2048 897 -> 578
+// us, 4096 x 65536 x 1024 906 -> 374, 4096 x 16384 x 4096 252 -> 217, against
+// groups of 8 tile rows; other widths and small D alike within 2%); taller ones
+// groups of 4 tile rows on such rows (16384 x 8192 x 4096 476 -> 420 us, 32768 x
+// 8192 x 2048 569 -> 523) and 8 on others (12000 x 5000 x 3200 183 -> 176) and
+// far above N (65536 x 4096 x 1024 379 -> 363).
+void set_order(I8Args& g) {
+  g.by_cols = g.N >= g.M;
+  const bool pages = g.ldd * (int64_t)dtype_size((mdnn_dtype_t)g.d_type) % 4096 == 0;
+  g.group = g.by_cols ? 16 : pages && g.M / 8 < g.N ? 4 : 8;
 }
 
 // ------------------------------------------------- register-staged kernel
@@ -763,6 +782,7 @@ extern "C" mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int
   g.a = A, g.b = B, g.a_scale = a_scale, g.b_scale = b_scale, g.bias = bias, g.d = D;
   g.M = M, g.N = N, g.K = K, g.lda = lda, g.ldb = ldb, g.ldd = ldd, g.act = act;
   g.d_type = d_type;
+  set_order(g);
   clear_error();
   return run_i8(g, workspace, ws_bytes, as_stream(stream));
 }
