@@ -519,7 +519,8 @@ mdnn_status_t mdnn_rmsnorm_i8_fwd(int64_t rows, int64_t cols, const void* x, int
  *        is the gradient that reaches h along the residual)
  *   dgamma[c] = sum over rows of dy * xh         (fp32, overwritten)
  * dy, h, dres, dx are `dtype`; dx and dgamma may each be NULL.  dx may lie
- * exactly in place of dy, h or dres.  workspace: at least
+ * exactly in place of dy, h or dres; otherwise outputs must not overlap inputs
+ * or each other.  workspace: at least
  * mdnn_rmsnorm_bwd_workspace(rows, cols) bytes, 256-byte aligned, when dgamma
  * is asked for (otherwise NULL is allowed); scratch.  Sums in a fixed order
  * (deterministic).  rows == 0: dgamma = 0.  Errors as above. */

@@ -150,8 +150,7 @@ void set_order(I8Args& g) {
 // swizzled LDS tiles (two stages, one barrier a step).  A chunk past the row's
 // end is read from its last 16 bytes and shifted; k past K is zero.  1000 x 777
 // x 1531 9.3 us (the latency of 12 steps on one tile per CU), 4095^3 109 us.
-// Four and six sets in flight measured the same (11.1, 11.1 and 11.5 us of a
-// former state of the former): two.
+// Four and six sets in flight are not faster than two.
 
 typedef uint32_t u4v_a1 __attribute__((ext_vector_type(4), aligned(1)));
 

@@ -318,9 +318,22 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_kernel(RowArgs a) {
   }
 }
 
-// Rows of any length, element by element, read again for each use.  A thread
+// Rows of any length, element by element, read again for each use, LONG_U
+// elements of a thread in flight (past the row's end: its last element again,
+// not used; one in flight: 4096 x 40000 bf16 725 us, eight 370).  A thread
 // reads an element for the last time before it writes that element, so
 // outputs may lie in place of the inputs as in the kernel above.
+constexpr int LONG_U = 8;
+template <class T>
+struct LongRow {
+  typedef typename T::storage S;
+  float v[LONG_U];
+  __device__ __forceinline__ void load(const S* p, int c0, int cols) {
+#pragma unroll
+    for (int u = 0; u < LONG_U; ++u) v[u] = to_f<T>(p[c0 + u * 1024 < cols ? c0 + u * 1024 : cols - 1]);
+  }
+};
+
 template <class T, int MODE>
 __global__ void __launch_bounds__(1024) row_long_kernel(RowArgs a) {
   typedef typename T::storage S;
@@ -329,33 +342,50 @@ __global__ void __launch_bounds__(1024) row_long_kernel(RowArgs a) {
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
     const S* x = (const S*)a.x + row * a.ldx;
     const S* res = MODE != QUANT && a.res ? (const S*)a.res + row * a.ldr : nullptr;
-    auto value = [&](int c) {
-      float h = to_f<T>(x[c]);
-      if (res) h = add_rn(h, to_f<T>(res[c]));
-      return h;
+    auto load = [&](int c0, LongRow<T>& h, LongRow<F32>& g) {
+      LongRow<T> r;
+      h.load(x, c0, a.cols);
+      if (res) r.load(res, c0, a.cols);
+      if (MODE != QUANT && a.gamma) g.load(a.gamma, c0, a.cols);
+      if (res) {
+#pragma unroll
+        for (int u = 0; u < LONG_U; ++u) h.v[u] = add_rn(h.v[u], r.v[u]);
+      }
     };
+    LongRow<T> h;
+    LongRow<F32> g;
     SumMax v = {0.0f, 0u};
-    for (int c = threadIdx.x; c < a.cols; c += 1024) {
-      float h = value(c);
-      if (MODE != QUANT) v.s = fmaf(h, h, v.s);
-      if (MODE == NORM_I8 && a.gamma) h = mul_rn(h, a.gamma[c]);
-      const uint32_t u = __float_as_uint(h) & 0x7fffffffu;
-      v.m = u > v.m ? u : v.m;
+    for (int c0 = threadIdx.x; c0 < a.cols; c0 += LONG_U * 1024) {
+      load(c0, h, g);
+#pragma unroll
+      for (int u = 0; u < LONG_U; ++u) {
+        if (c0 + u * 1024 >= a.cols) continue;
+        float t = h.v[u];
+        if (MODE != QUANT) v.s = fmaf(t, t, v.s);
+        if (MODE == NORM_I8 && a.gamma) t = mul_rn(t, g.v[u]);
+        const uint32_t b = __float_as_uint(t) & 0x7fffffffu;
+        v.m = b > v.m ? b : v.m;
+      }
     }
     v = row_reduce<1024>(v, buf, flip);
     const float rstd = MODE == QUANT ? 1.0f : row_rstd(v.s, (float)a.cols, a.eps);
     const RowScale k = row_scale(v.m, MODE == NORM_I8 && !isfinite(v.s));
     if (MODE != NORM && threadIdx.x == 0) a.scale[row] = MODE == QUANT ? k.scale : k.scale * rstd;
-    for (int c = threadIdx.x; c < a.cols; c += 1024) {
-      const float h = value(c);
-      if (MODE != QUANT && a.h) ((S*)a.h + row * a.ldh)[c] = from_f<T>(h);
-      if (MODE == NORM) {
-        float y = h * rstd;
-        if (a.gamma) y *= a.gamma[c];
-        ((S*)a.y + row * a.ldy)[c] = from_f<T>(y);
-      } else {
-        const float s = MODE == NORM_I8 && a.gamma ? mul_rn(h, a.gamma[c]) : h;
-        a.q[row * a.ldq + c] = (int8_t)(codes4(s, 0.0f, 0.0f, 0.0f, k.inv) & k.mask);
+    for (int c0 = threadIdx.x; c0 < a.cols; c0 += LONG_U * 1024) {
+      load(c0, h, g);
+#pragma unroll
+      for (int u = 0; u < LONG_U; ++u) {
+        const int c = c0 + u * 1024;
+        if (c >= a.cols) continue;
+        if (MODE != QUANT && a.h) ((S*)a.h + row * a.ldh)[c] = from_f<T>(h.v[u]);
+        if (MODE == NORM) {
+          float y = h.v[u] * rstd;
+          if (a.gamma) y *= g.v[u];
+          ((S*)a.y + row * a.ldy)[c] = from_f<T>(y);
+        } else {
+          const float t = MODE == NORM_I8 && a.gamma ? mul_rn(h.v[u], g.v[u]) : h.v[u];
+          a.q[row * a.ldq + c] = (int8_t)(codes4(t, 0.0f, 0.0f, 0.0f, k.inv) & k.mask);
+        }
       }
     }
   }
@@ -573,23 +603,40 @@ __global__ void __launch_bounds__(1024) norm_bwd_long_kernel(BwdArgs a) {
   int flip = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
     const S *dy = (const S*)a.dy + row * a.lddy, *hp = (const S*)a.h + row * a.ldh;
+    LongRow<T> h, d, r;
+    LongRow<F32> g, p;
     Sum2 v = {0.0f, 0.0f};
-    for (int c = threadIdx.x; c < a.cols; c += 1024) {
-      const float h = to_f<T>(hp[c]), d = to_f<T>(dy[c]);
-      v.a = fmaf(h, h, v.a);
-      v.b = fmaf(a.gamma ? d * a.gamma[c] : d, h, v.b);
+    for (int c0 = threadIdx.x; c0 < a.cols; c0 += LONG_U * 1024) {
+      h.load(hp, c0, a.cols);
+      d.load(dy, c0, a.cols);
+      if (a.gamma) g.load(a.gamma, c0, a.cols);
+#pragma unroll
+      for (int u = 0; u < LONG_U; ++u) {
+        if (c0 + u * 1024 >= a.cols) continue;
+        v.a = fmaf(h.v[u], h.v[u], v.a);
+        v.b = fmaf(a.gamma ? d.v[u] * g.v[u] : d.v[u], h.v[u], v.b);
+      }
     }
     v = row_reduce<1024, 1>(v, buf, flip);
     const float rstd = row_rstd(v.a, (float)a.cols, a.eps), k = rstd * v.b / (float)a.cols;
-    for (int c = threadIdx.x; c < a.cols; c += 1024) {
-      const float xh = to_f<T>(hp[c]) * rstd, d = to_f<T>(dy[c]);
-      float o = rstd * ((a.gamma ? d * a.gamma[c] : d) - xh * k);
-      if (a.dres) o += to_f<T>(((const S*)a.dres + row * a.lddr)[c]);
-      if (a.partial) {
-        float* p = a.partial + (int64_t)blockIdx.x * a.cols + c;
-        *p = row == (int64_t)blockIdx.x ? d * xh : fmaf(d, xh, *p);
+    float* sums = a.partial ? a.partial + (int64_t)blockIdx.x * a.cols : nullptr;
+    const bool first = row == (int64_t)blockIdx.x;
+    for (int c0 = threadIdx.x; c0 < a.cols; c0 += LONG_U * 1024) {
+      h.load(hp, c0, a.cols);
+      d.load(dy, c0, a.cols);
+      if (a.gamma) g.load(a.gamma, c0, a.cols);
+      if (a.dres) r.load((const S*)a.dres + row * a.lddr, c0, a.cols);
+      if (sums && !first) p.load(sums, c0, a.cols);
+#pragma unroll
+      for (int u = 0; u < LONG_U; ++u) {
+        const int c = c0 + u * 1024;
+        if (c >= a.cols) continue;
+        const float xh = h.v[u] * rstd;
+        float o = rstd * ((a.gamma ? d.v[u] * g.v[u] : d.v[u]) - xh * k);
+        if (a.dres) o += r.v[u];
+        if (sums) sums[c] = first ? d.v[u] * xh : fmaf(d.v[u], xh, p.v[u]);
+        if (a.dx) ((S*)a.dx + row * a.lddx)[c] = from_f<T>(o);
       }
-      if (a.dx) ((S*)a.dx + row * a.lddx)[c] = from_f<T>(o);
     }
   }
 }
@@ -604,7 +651,11 @@ int bwd_tpr(int64_t cols) {
 int64_t bwd_blocks(int64_t rows, int64_t cols) {
   const int tpr = bwd_tpr(cols);
   const int64_t b = ceil_div(rows, tpr == 0 ? 1 : BWD_NT(tpr) / tpr), most = tpr == 0 || tpr == 1024 ? 256 : 512;
-  return b < most ? b : most;
+  // A single block needs no second launch: worth up to three rows a thread
+  // group of 16 (96 x 112 bf16 5.3 us, over two launches 5.7), two of 64 or 256
+  // (16 x 1000 5.7 and 6.5, 4 x 4096 6.3 and 6.9; 24 x 1000 7.5 and 6.5).
+  const int64_t alone = tpr == 16 ? 3 : tpr == 64 || tpr == 256 ? 2 : 1;
+  return b <= alone ? 1 : b < most ? b : most;
 }
 
 template <class T, int TPR, int NCH>
@@ -652,7 +703,10 @@ int64_t slab_rows(int64_t rows, int64_t cols) {
   const int64_t per = ceil_div(ceil_div(rows, most), 16) * 16;
   return per < 32 ? 32 : per;
 }
-int64_t slab_count(int64_t rows, int64_t cols) { return rows > 0 && cols > 0 ? ceil_div(rows, slab_rows(rows, cols)) : 0; }
+// (none where one tile holds all rows: it takes its own maxima, in one launch;
+// 128 x 4096 bf16 6.7 -> 3.7 us)
+constexpr int QT_C = 64, QT_R = 128;  // tile of pass 2: columns, rows
+int64_t slab_count(int64_t rows, int64_t cols) { return rows > QT_R && cols > 0 ? ceil_div(rows, slab_rows(rows, cols)) : 0; }
 
 // Four consecutive elements of a row: those from `start` (a quad past the
 // row's end starts at its last four and overlaps its neighbour), or, in rows
@@ -713,7 +767,6 @@ colmax_kernel(const typename T::storage* x, int64_t ldx, int64_t rows, int64_t c
   partial[(int64_t)blockIdx.y * cols + c0 + threadIdx.x] = v;
 }
 
-constexpr int QT_C = 64, QT_R = 128;  // tile: columns, rows
 template <class T, bool NARROW>
 __global__ void __launch_bounds__(256)
 quant_t_kernel(const typename T::storage* x, int64_t ldx, int64_t rows, int64_t cols, const uint32_t* partial,
@@ -754,7 +807,18 @@ quant_t_kernel(const typename T::storage* x, int64_t ldx, int64_t rows, int64_t 
       }
   };
   int64_t r0 = (int64_t)blockIdx.y * QT_R;
-  if (slabs > 0) {
+  if (slabs == 0 && rows > 0) {
+    load(r0);
+#pragma unroll
+    for (int p = 0; p < QT_R / 64; ++p)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t b = __float_as_uint(v[p][e].get(j)) & 0x7fffffffu;
+          m[j] = b > m[j] ? b : m[j];
+        }
+  } else if (slabs > 0) {
     load_top(part);
     load(r0);
     take_top();
@@ -963,16 +1027,19 @@ extern "C" mdnn_status_t mdnn_rmsnorm_bwd(int64_t rows, int64_t cols, const void
     return fail(MDNN_ERR_WORKSPACE, "rmsnorm_bwd: workspace of %zu bytes (256-byte aligned) required", need);
   clear_error();
   BwdArgs a = {};
-  a.dy = dy, a.h = h, a.dres = dres, a.gamma = gamma, a.dx = dx, a.partial = dgamma ? (float*)workspace : nullptr;
+  // (a single block's sums are the gradient)
+  const int64_t blocks = bwd_blocks(rows, cols);
+  a.dy = dy, a.h = h, a.dres = dres, a.gamma = gamma, a.dx = dx;
+  a.partial = !dgamma || blocks == 1 ? dgamma : (float*)workspace;
   a.rows = rows, a.lddy = lddy, a.ldh = ldh, a.lddr = lddr, a.lddx = lddx, a.cols = (int32_t)cols, a.eps = eps;
   switch (dtype) {
     case MDNN_F32: MDNN_TRY(run_bwd<F32>(a, st)); break;
     case MDNN_F16: MDNN_TRY(run_bwd<F16>(a, st)); break;
     default: MDNN_TRY(run_bwd<BF16>(a, st)); break;
   }
-  if (!dgamma) return MDNN_SUCCESS;
+  if (!dgamma || blocks == 1) return MDNN_SUCCESS;
   const int64_t tiles = ceil_div(cols, 32);
   hipLaunchKernelGGL(dgamma_kernel, dim3((unsigned)(tiles < MAX_BLOCKS ? tiles : MAX_BLOCKS)), dim3(1024), 0, st, (const float*)workspace,
-                     (int)bwd_blocks(rows, cols), cols, dgamma);
+                     (int)blocks, cols, dgamma);
   return check_launch("dgamma_kernel");
 }

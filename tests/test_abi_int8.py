@@ -40,11 +40,12 @@ def test_quantize_refuses(m, args, status):
 
 
 def test_quantize_columns_refuses_workspaces(m):
-    need = m.mdnn_quantize_i8_t_workspace(100, 40)
-    assert need == 4 * 40 * 4 and m.mdnn_quantize_i8_t_workspace(-1, 4) == 0 and m.mdnn_quantize_i8_t_workspace(0, 4) == 0
+    need = m.mdnn_quantize_i8_t_workspace(300, 40)
+    assert need == 10 * 40 * 4 and m.mdnn_quantize_i8_t_workspace(-1, 4) == 0 and m.mdnn_quantize_i8_t_workspace(0, 4) == 0
+    assert m.mdnn_quantize_i8_t_workspace(128, 40) == 0 and m.mdnn_quantize_i8_t_workspace(129, 40) > 0  # one tile of rows
     for ws, nb in ((None, need), (FAKE, need - 1), (FAKE + 4, need)):
-        _refuses(m, m.ERR_WORKSPACE, m.mdnn_quantize_i8_t, 100, 40, FAKE, 40, 0, FAKE, 100, FAKE, ws, nb)
-    _refuses(m, m.ERR_LAYOUT, m.mdnn_quantize_i8_t, 100, 40, FAKE, 40, 0, FAKE, 99, FAKE, FAKE, need)
+        _refuses(m, m.ERR_WORKSPACE, m.mdnn_quantize_i8_t, 300, 40, FAKE, 40, 0, FAKE, 300, FAKE, ws, nb)
+    _refuses(m, m.ERR_LAYOUT, m.mdnn_quantize_i8_t, 300, 40, FAKE, 40, 0, FAKE, 299, FAKE, FAKE, need)
 
 
 @pytest.mark.parametrize("args,status", [
