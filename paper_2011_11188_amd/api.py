@@ -217,6 +217,16 @@ def _bytes_of(ws):
     return ws, ws.numel()
 
 
+def _scratch(n: int, device, stream):
+    """A workspace of n bytes that belongs to the call's stream: released when
+    the wrapper returns, it goes to later work of that stream only."""
+    import torch
+    if stream is None:
+        return torch.empty((n,), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        return torch.empty((n,), dtype=torch.uint8, device=device)
+
+
 def quantize_i8(x, transpose: bool = False, q=None, scale=None, workspace=None, stream=None):
     """(codes, scales) of a 2-D tensor: int8 codes with an fp32 scale for each
     row, or with transpose for each column, the codes stored [cols, rows] (a
@@ -230,8 +240,7 @@ def quantize_i8(x, transpose: bool = False, q=None, scale=None, workspace=None, 
         mdnn_quantize_i8(rows, cols, x, ldx, dtype_of(x), q, ldq, scale, stream)
         return q, scale
     if workspace is None:
-        workspace = torch.empty((max(mdnn_quantize_i8_t_workspace(rows, cols), 16),), dtype=torch.uint8,
-                                device=x.device)
+        workspace = _scratch(max(mdnn_quantize_i8_t_workspace(rows, cols), 16), x.device, stream)
     mdnn_quantize_i8_t(rows, cols, x, ldx, dtype_of(x), q, ldq, scale, *_bytes_of(workspace), stream)
     return q, scale
 
@@ -252,7 +261,7 @@ def gemm_i8(A, a_scale, B, b_scale, bias=None, act: int = ACT_NONE, out_dtype=No
     elif tuple(out.shape) != (M, N):
         raise ValueError(f"out must be [{M}, {N}]")
     if workspace is True:
-        workspace = torch.empty((max(mdnn_gemm_i8_workspace(M, N, K), 16),), dtype=torch.uint8, device=A.device)
+        workspace = _scratch(max(mdnn_gemm_i8_workspace(M, N, K), 16), A.device, stream)
     mdnn_gemm_i8(M, N, K, A, lda, a_scale, B, ldb, b_scale, bias, act, out, _rows_of(out, "out")[2], dtype_of(out),
                  *_bytes_of(workspace), stream)
     return out
@@ -308,8 +317,7 @@ def rmsnorm_bwd(dy, h, gamma=None, eps: float = 1e-6, dres=None, dx=None, with_d
     else:
         _vector_of(dgamma, cols, "dgamma")
     if with_dgamma and workspace is None:
-        workspace = torch.empty((max(mdnn_rmsnorm_bwd_workspace(rows, cols), 256),), dtype=torch.uint8,
-                                device=dy.device)
+        workspace = _scratch(max(mdnn_rmsnorm_bwd_workspace(rows, cols), 256), dy.device, stream)
     mdnn_rmsnorm_bwd(rows, cols, dy, lddy, h, ldh, _vector_of(gamma, cols, "gamma"), eps, dres, lddr, dx, lddx, dgamma,
                      dtype_of(dy), *_bytes_of(workspace), stream)
     return dx, dgamma

@@ -371,6 +371,33 @@ def test_product_streams_and_graphs(mdnn, M, N, K):
         assert torch.equal(out, got), i
 
 
+@pytest.mark.parametrize("handle", [False, True])
+def test_own_workspaces_follow_the_stream(mdnn, handle):
+    """A workspace that a wrapper allocates is not handed to other work while the call's stream still waits."""
+    import torch
+    x = torch.randn(2000, 500, device="cuda")
+    g = torch.randn(2000, 500, device="cuda")
+    a = torch.randint(-127, 128, (4100, 33), dtype=torch.int8, device="cuda")
+    b = torch.randint(-127, 128, (8300, 33), dtype=torch.int8, device="cuda")
+    sa, sb = torch.rand(4100, device="cuda"), torch.rand(8300, device="cuda")
+    assert mdnn.mdnn_gemm_i8_workspace(4100, 8300, 33) > 0
+    calls = [(mdnn.mdnn_quantize_i8_t_workspace(2000, 500), lambda **k: mdnn.quantize_i8(x, transpose=True, **k)),
+             (mdnn.mdnn_rmsnorm_bwd_workspace(2000, 500), lambda **k: mdnn.rmsnorm_bwd(g, x, **k)),
+             (mdnn.mdnn_gemm_i8_workspace(4100, 8300, 33),
+              lambda **k: (mdnn.gemm_i8(a, sa, b, sb, workspace=True, **k),))]
+    side = torch.cuda.Stream()
+    for nbytes, call in calls:
+        want = call()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        got = call(stream=side.cuda_stream if handle else side)
+        other = [torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        assert all((o == 255).all() for o in other)
+        assert all(torch.equal(w, v) for w, v in zip(want, got))
+
+
 def test_api_refuses(mdnn):
     import torch
     a = torch.zeros((4, 32), dtype=torch.int8, device="cuda")
