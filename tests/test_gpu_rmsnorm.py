@@ -265,18 +265,39 @@ def test_many_rows(mdnn):
         assert torch.equal(s[lo:lo + (1 << 22)], (a / torch.full_like(a, 127.0)).float()[:, 0])
 
 
-def test_widest_gamma_gradient(mdnn):
-    """More columns than one launch of the gamma gradient's blocks holds threads for."""
+@pytest.mark.parametrize("rows,cols", [(1, (1 << 27) + 40), (2, (1 << 25) + 72)])
+def test_widest_gamma_gradient(mdnn, rows, cols):
+    """One row, whose sums are the gradient, and more columns than the gamma gradient's launch has blocks for."""
     import torch
-    cols = (1 << 27) + 40
-    h = torch.randn(1, cols, device="cuda").half()
-    dy = torch.randn(1, cols, device="cuda").half()
+    h = torch.randn(rows, cols, device="cuda").half()
+    dy = torch.randn(rows, cols, device="cuda").half()
     _, dg = mdnn.rmsnorm_bwd(dy, h)
-    rstd = 1 / torch.sqrt(sum(p.double().square().sum() for p in h[0].split(1 << 24)) / cols + 1e-6)
+    square = sum(p.double().square().sum(1, keepdim=True) for p in h.split(1 << 24, 1))
+    rstd = 1 / torch.sqrt(square / cols + 1e-6)
     for lo in range(0, cols, 1 << 24):
-        want = dy[0, lo:lo + (1 << 24)].double() * h[0, lo:lo + (1 << 24)].double() * rstd
-        # the sum of squares: 2^17 terms a thread
-        assert bool(((dg[lo:lo + (1 << 24)].double() - want).abs() <= _sum_bound(cols) * want.abs() + 1e-30).all())
+        terms = dy[:, lo:lo + (1 << 24)].double() * h[:, lo:lo + (1 << 24)].double() * rstd
+        err = (dg[lo:lo + (1 << 24)].double() - terms.sum(0)).abs()
+        # the sum of squares: at most 2^17 terms a thread
+        assert bool((err <= _sum_bound(cols) * terms.abs().sum(0) + 1e-30).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(96, 112), (97, 112), (16, 1000), (17, 1000), (4, 4096), (5, 4096), (2, 9000),
+                                       (257, 40000)])
+def test_gradients_by_blocks(mdnn, rows, cols):
+    """The most rows that one block takes, whose sums are the gradient, one row more, and more long rows than blocks."""
+    import torch
+    h = torch.randn(rows, cols, device="cuda")
+    dy = torch.randn(rows, cols, device="cuda")
+    dx, dg = mdnn.rmsnorm_bwd(dy, h, eps=EPS)
+    h, dy = h.double(), dy.double()
+    r = 1 / torch.sqrt((h * h).mean(1, keepdim=True) + EPS)
+    terms = dy * h * r
+    tol = ((rows + 8) * U + _sum_bound(cols) / 2 + 8 * U) * terms.abs().sum(0)
+    assert bool(((dg.double() - terms.sum(0)).abs() <= tol).all())
+    want = r * (dy - h * r * terms.mean(1, keepdim=True))
+    size = r * (dy.abs() + (h * r).abs() * terms.abs().mean(1, keepdim=True))
+    tol = (2 * _sum_bound(cols) + 12 * U) * size + 1.01 * HALF["f32"] * want.abs()
+    assert bool(((dx.double() - want).abs() <= tol).all())
 
 
 def test_far_rows(mdnn):
