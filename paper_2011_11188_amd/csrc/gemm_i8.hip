@@ -15,6 +15,7 @@
 namespace mdnn {
 
 typedef int int4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u4v_a2 __attribute__((ext_vector_type(4), aligned(2)));
 struct I8 {
   typedef int8_t storage;
 };
@@ -39,9 +40,15 @@ struct I8Args {
   int32_t act, d_type;
   uint32_t group;    // tile rows a group of workgroups walks together (tile columns with by_cols)
   bool by_cols;
+  bool pairs;        // the tiled kernels' columns are ordered by pair_col
 };
 
 // ------------------------------------------------------------- epilogue
+
+// The column that row r of a tile's B holds where D is of 16 bits: two
+// neighbouring fragments' four columns of a lane are eight consecutive ones, 16
+// bytes of D.
+__device__ __forceinline__ int pair_col(int r) { return (r & ~31) | ((r & 12) << 1) | ((r & 16) >> 2) | (r & 3); }
 
 // Four consecutive floats from column n, columns past N read as the last.
 __device__ __forceinline__ void load_cols(const float* p, int64_t n, int64_t N, float (&v)[4]) {
@@ -56,29 +63,35 @@ __device__ __forceinline__ void load_cols(const float* p, int64_t n, int64_t N, 
   }
 }
 
-// One lane's four consecutive columns n .. n + 3 of row m.
 template <class OutT>
-__device__ __forceinline__ void store_i8(const I8Args& g, int64_t m, int64_t n, int4v acc, float sa,
-                                         const float (&sb)[4], const float (&bias)[4]) {
-  typedef typename OutT::storage S;
-  float v[4];
+__device__ __forceinline__ Quad<OutT> quad_of(const float (&v)[4]) {
+  Quad<OutT> q;
+  if constexpr (Quad<OutT>::H) {
+    q.q[0] = (uint32_t)from_f<OutT>(v[0]) | ((uint32_t)from_f<OutT>(v[1]) << 16);
+    q.q[1] = (uint32_t)from_f<OutT>(v[2]) | ((uint32_t)from_f<OutT>(v[3]) << 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q.q[e] = __float_as_uint(v[e]);
+  }
+  return q;
+}
+
+// One lane's four consecutive columns n .. n + 3 of row m.
+__device__ __forceinline__ void values_i8(const I8Args& g, int4v acc, float sa, const float (&sb)[4],
+                                          const float (&bias)[4], float (&v)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     v[e] = (float)acc[e] * sa * sb[e];
     if (g.bias) v[e] += bias[e];
     if (g.act == MDNN_ACT_RELU) v[e] = relu_f(v[e]);
   }
+}
+template <class OutT>
+__device__ __forceinline__ void store_i8(const I8Args& g, int64_t m, int64_t n, const float (&v)[4]) {
+  typedef typename OutT::storage S;
   S* d = (S*)g.d + m * g.ldd + n;
   if (n + 4 <= g.N) {
-    Quad<OutT> q;
-    if constexpr (Quad<OutT>::H) {
-      q.q[0] = (uint32_t)from_f<OutT>(v[0]) | ((uint32_t)from_f<OutT>(v[1]) << 16);
-      q.q[1] = (uint32_t)from_f<OutT>(v[2]) | ((uint32_t)from_f<OutT>(v[3]) << 16);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) q.q[e] = __float_as_uint(v[e]);
-    }
-    q.store(d);
+    quad_of<OutT>(v).store(d);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -86,30 +99,58 @@ __device__ __forceinline__ void store_i8(const I8Args& g, int64_t m, int64_t n, 
   }
 }
 
-// A wave's FM x FN fragments; mb, nb: this lane's first row and column.
-template <class OutT, int FM, int FN>
+// A wave's FM x FN fragments; mb, nb: this lane's first row and the wave's
+// first column.  PAIRS: the columns are in pair_col's order.
+template <class OutT, int FM, int FN, bool PAIRS>
 __device__ __forceinline__ void epilogue_i8_t(const I8Args& g, int64_t mb, int64_t nb, const int4v (&acc)[FM][FN]) {
+  typedef typename OutT::storage S;
+  const int q = (threadIdx.x & 63) >> 4;
+  int64_t n[FN];
   float sa[FM], sb[FN][4], bias[FN][4];
 #pragma unroll
   for (int i = 0; i < FM; ++i) sa[i] = g.a_scale[mb + i * 16 < g.M ? mb + i * 16 : g.M - 1];
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
-    load_cols(g.b_scale, nb + j * 16, g.N, sb[j]);
-    if (g.bias) load_cols(g.bias, nb + j * 16, g.N, bias[j]);
+    n[j] = nb + (PAIRS ? (j >> 1) * 32 + q * 8 + (j & 1) * 4 : j * 16 + q * 4);
+    load_cols(g.b_scale, n[j], g.N, sb[j]);
+    if (g.bias) load_cols(g.bias, n[j], g.N, bias[j]);
   }
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
+  for (int i = 0; i < FM; ++i) {
+    const int64_t m = mb + i * 16;
+    if (m >= g.M) continue;
+    if constexpr (PAIRS) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
-      if (mb + i * 16 < g.M && nb + j * 16 < g.N) store_i8<OutT>(g, mb + i * 16, nb + j * 16, acc[i][j], sa[i], sb[j], bias[j]);
+      for (int j = 0; j < FN; j += 2) {
+        float v[2][4];
+        values_i8(g, acc[i][j], sa[i], sb[j], bias[j], v[0]);
+        values_i8(g, acc[i][j + 1], sa[i], sb[j + 1], bias[j + 1], v[1]);
+        if (n[j] + 8 <= g.N) {
+          const Quad<OutT> a = quad_of<OutT>(v[0]), b = quad_of<OutT>(v[1]);
+          *(__attribute__((address_space(1))) u4v_a2*)((S*)g.d + m * g.ldd + n[j]) = (u4v_a2){a.q[0], a.q[1], b.q[0], b.q[1]};
+        } else {
+          store_i8<OutT>(g, m, n[j], v[0]);
+          store_i8<OutT>(g, m, n[j + 1], v[1]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        if (n[j] >= g.N) continue;
+        float v[4];
+        values_i8(g, acc[i][j], sa[i], sb[j], bias[j], v);
+        store_i8<OutT>(g, m, n[j], v);
+      }
+    }
+  }
 }
 
-template <int FM, int FN>
+template <int FM, int FN, bool PAIRS>
 __device__ __forceinline__ void epilogue_i8(const I8Args& g, int64_t mb, int64_t nb, const int4v (&acc)[FM][FN]) {
   switch (g.d_type) {
-    case MDNN_F32: epilogue_i8_t<F32, FM, FN>(g, mb, nb, acc); break;
-    case MDNN_F16: epilogue_i8_t<F16, FM, FN>(g, mb, nb, acc); break;
-    default: epilogue_i8_t<BF16, FM, FN>(g, mb, nb, acc); break;
+    case MDNN_F32: epilogue_i8_t<F32, FM, FN, false>(g, mb, nb, acc); break;
+    case MDNN_F16: epilogue_i8_t<F16, FM, FN, PAIRS>(g, mb, nb, acc); break;
+    default: epilogue_i8_t<BF16, FM, FN, PAIRS>(g, mb, nb, acc); break;
   }
 }
 
@@ -203,7 +244,8 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_any_kernel(I8Args g) 
 #pragma unroll
   for (int i = 0; i < TL::LB; ++i) {
     const lds::LoadPos q = lds::load_pos<true, TL::BN, TL::LB>(wave, lane, i);
-    rb[i] = g.b + (n0 + q.r < g.N ? n0 + q.r : g.N - 1) * g.ldb;
+    const int64_t n = n0 + (g.pairs ? pair_col(q.r) : q.r);
+    rb[i] = g.b + (n < g.N ? n : g.N - 1) * g.ldb;
     kb[i] = q.c * 2;
   }
   struct Set {
@@ -263,24 +305,27 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_any_kernel(I8Args g) 
       }
     }
   }
-  epilogue_i8<FM, FN>(g, m0 + wm * TL::WTM + (lane & 15), n0 + wn * TL::WTN + 4 * (lane >> 4), acc);
+  epilogue_i8<FM, FN, true>(g, m0 + wm * TL::WTM + (lane & 15), n0 + wn * TL::WTN, acc);
 }
 
 // The last K % 16 bytes (K >= 16) of this lane's fragment rows mb + 16 i of A
-// and nb + 16 j of B, as k 0 .. 15 of one more step in the first 16 lanes.
+// and of B's from nb on, as k 0 .. 15 of one more step in the first 16 lanes.
 // Loaded a few steps before the end and added after it, so that nothing waits
 // for them.
 template <int FM, int FN>
 struct LastBytes {
   uint4 a[FM], b[FN];
-  __device__ __forceinline__ void load(const I8Args& g, int lane, int64_t mb, int64_t nb) {
+  __device__ __forceinline__ void load(const I8Args& g, int lane, int64_t mb, int64_t nb, bool pairs) {
 #pragma unroll
     for (int j = 0; j < FN; ++j) b[j] = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < FM; ++i) a[i] = make_uint4(0, 0, 0, 0);
     if (lane < 16) {  // (a request a row: the other lanes' copies would be three more)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) b[j] = load_bytes(g.b + (nb + j * 16 < g.N ? nb + j * 16 : g.N - 1) * g.ldb + g.K - 16);
+      for (int j = 0; j < FN; ++j) {
+        const int64_t n = nb + (pairs ? pair_col(j * 16 + lane) : j * 16 + lane);
+        b[j] = load_bytes(g.b + (n < g.N ? n : g.N - 1) * g.ldb + g.K - 16);
+      }
 #pragma unroll
       for (int i = 0; i < FM; ++i) a[i] = load_bytes(g.a + (mb + i * 16 < g.M ? mb + i * 16 : g.M - 1) * g.lda + g.K - 16);
     }
@@ -338,7 +383,8 @@ struct I8Loader {
   int32_t left[P];
   uint32_t off[L];
 
-  __device__ __forceinline__ void init(const I8Operand& a, int64_t mn0, int64_t kbeg, int wave, int lane) {
+  __device__ __forceinline__ void init(const I8Operand& a, int64_t mn0, int64_t kbeg, int wave, int lane,
+                                       bool pairs = false) {
     base = (const char*)a.p + mn0 * a.ld + kbeg;
     const int32_t rows = a.MN - mn0 < W ? (int32_t)(a.MN - mn0) : W, ld = (int32_t)a.ld;
     if constexpr (RAGGED) {
@@ -348,7 +394,7 @@ struct I8Loader {
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const lds::LoadPos q = lds::load_pos<true, W, L>(wave, lane, i);
-      const int32_t r = q.r < rows ? q.r : rows - 1;
+      const int32_t c = pairs ? pair_col(q.r) : q.r, r = c < rows ? c : rows - 1;
       off[i] = (uint32_t)(r * ld + q.c * 2);
       if (i < P) left[i] = (int32_t)((a.K & ~(int64_t)15) - kbeg) - q.c * 2;
     }
@@ -402,7 +448,7 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_kernel(I8Args g) {
   LA la;
   LB lb;
   la.init(I8Operand{g.a, g.lda, g.M, g.K}, m0, 0, wave, lane);
-  lb.init(I8Operand{g.b, g.ldb, g.N, g.K}, n0, 0, wave, lane);
+  lb.init(I8Operand{g.b, g.ldb, g.N, g.K}, n0, 0, wave, lane, g.pairs);
   const uint32_t wa = (uint32_t)(wave * TL::LA) * 1024u, wb = (uint32_t)(wave * TL::LB) * 1024u;
   int4v acc[FM][FN];
 #pragma unroll
@@ -411,7 +457,7 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_kernel(I8Args g) {
     for (int j = 0; j < FN; ++j) acc[i][j] = (int4v){0, 0, 0, 0};
   // (256 x 256 tiles have no registers to keep them in over the loop)
   constexpr bool HOLD = FM + FN <= 8;
-  const int64_t mb = m0 + wm * TL::WTM + (lane & 15), nr = n0 + wn * TL::WTN + (lane & 15);
+  const int64_t mb = m0 + wm * TL::WTM + (lane & 15), nw = n0 + wn * TL::WTN;
   const bool last = RAGGED && (g.K & 15) != 0;
   LastBytes<HOLD ? FM : 1, HOLD ? FN : 1> held;
   lds::Frags<TL> f0, f1;
@@ -427,7 +473,7 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_kernel(I8Args g) {
   if constexpr (RAGGED && !HOLD) {
     if (last) {
       LastBytes<FM, FN> v;
-      v.load(g, lane, mb, nr);
+      v.load(g, lane, mb, nw, g.pairs);
       v.add(g, acc);
     }
   }
@@ -444,13 +490,13 @@ __global__ void __launch_bounds__(TL::NT, TL::OCC) gemm_i8_kernel(I8Args g) {
   for (; t + U - 1 + NS < nk - (RAGGED ? 1 : 0); t += U)  // (the last step is issued with its test)
     lds::pipeline_round<I8, TL, NS, LA, LB, 0, U, false>(t, nk, st, wave, fa_l, fb_l, wm, wn, la, lb, f0, f1, acc);
   if constexpr (RAGGED && HOLD)
-    if (last) held.load(g, lane, mb, nr);
+    if (last) held.load(g, lane, mb, nw, g.pairs);
   for (; t < nk; t += U)
     lds::pipeline_round<I8, TL, NS, LA, LB, 0, U, true>(t, nk, st, wave, fa_l, fb_l, wm, wn, la, lb, f0, f1, acc);
 
   if constexpr (RAGGED && HOLD)
     if (last) held.add(g, acc);
-  epilogue_i8<FM, FN>(g, mb, n0 + wn * TL::WTN + 4 * (lane >> 4), acc);
+  epilogue_i8<FM, FN, true>(g, mb, nw, acc);
 }
 
 // ------------------------------------------------------- few rows kernels
@@ -476,7 +522,7 @@ __device__ __forceinline__ void join_few(const I8Args& g, char* mem, int wave, i
     int4v sum[1][1] = {{part[f * 64 + lane]}};
 #pragma unroll
     for (int w = 1; w < W; ++w) sum[0][0] += part[(w * FM * FN + f) * 64 + lane];
-    epilogue_i8<1, 1>(g, m0 + f / FN * 16 + (lane & 15), n0 + f % FN * 16 + 4 * (lane >> 4), sum);
+    epilogue_i8<1, 1, false>(g, m0 + f / FN * 16 + (lane & 15), n0 + f % FN * 16, sum);
   }
 }
 
@@ -583,7 +629,7 @@ __global__ void __launch_bounds__(W * 64) gemm_i8_few_lds_kernel(I8Args g) {
   lb.init(I8Operand{g.b, g.ldb, g.N, g.K}, n0, kbeg, 0, lane);
   const bool last = wave == W - 1 && (g.K & 15) != 0;
   LastBytes<FM, FN> held;
-  if (last) held.load(g, lane, m0 + (lane & 15), n0 + (lane & 15));
+  if (last) held.load(g, lane, m0 + (lane & 15), n0, false);
   char* const own = mem + wave * (NS * STAGE);
   const uint32_t at = lds::lds_address(own);
 #pragma unroll
@@ -780,7 +826,7 @@ extern "C" mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int
   I8Args g = {};
   g.a = A, g.b = B, g.a_scale = a_scale, g.b_scale = b_scale, g.bias = bias, g.d = D;
   g.M = M, g.N = N, g.K = K, g.lda = lda, g.ldb = ldb, g.ldd = ldd, g.act = act;
-  g.d_type = d_type;
+  g.d_type = d_type, g.pairs = d_type != MDNN_F32;
   set_order(g);
   clear_error();
   return run_i8(g, workspace, ws_bytes, as_stream(stream));
