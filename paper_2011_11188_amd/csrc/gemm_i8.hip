@@ -674,6 +674,9 @@ __global__ void __launch_bounds__(W * 64) gemm_i8_few_lds_kernel(I8Args g) {
 }
 
 typedef lds::Tile<64, 64, 2, 2, 2> TileI64;
+// 128 x 128 with eight waves of 64 x 32 and two stages (64 KB): two workgroups
+// per CU
+typedef lds::Tile<128, 128, 2, 4, 4> TileI128x8;
 // 128 x 128 with three stages (96 KB), 256 x 128 with eight waves of 64 x 64
 // and three stages (144 KB): one workgroup per CU each
 typedef lds::Tile<128, 128, 2, 2, 1> TileI128;
@@ -767,32 +770,48 @@ mdnn_status_t run_i8(I8Args g, void* ws, size_t ws_bytes, hipStream_t st) {
     return run_few<1>(g, rows16, st);
   if (fits && (g.M <= 64 || g.N <= 32 || tiles(64, 32) <= 256)) return run_few<2>(g, rows16, st);
   if (!rows16) {
-    // 256 x 128 tiles from more than 256 of them on (4095^3 109 us, 128 x 128
-    // tiles 120, 64 x 64 205), 128 x 128 from more than 128 (2000 x 2000 x 3001
-    // 27 us, 41 and 44; 1000 x 2000 x 3001 25.7, 64 x 64 25.0)
-    if (tiles(256, 128) > 256)
+    // 256 x 128 tiles from more than 256 of them on (4095^3 108 us, 128 x 128
+    // tiles 120, 64 x 64 206) unless steps are few (9783 x 1984 x 129 30.2 us, 128
+    // x 128 23.7; 4095 x 4095 x 513 40 and 39), 128 x 128 from more than 128 (2000
+    // x 2000 x 3001 28 us, 256 x 128 41, 64 x 64 43; 1000 x 2000 x 3001 27, 64 x
+    // 64 25)
+    if (tiles(256, 128) > 256 && g.K > 512)
       launch_any<lds::Tile<256, 128, 4, 2, 2>, 2>(g, st);
     else if (tiles(128, 128) > 128)
-      launch_any<lds::Tile<128, 128, 2, 4, 2>, 2>(g, st);
+      launch_any<TileI128x8, 2>(g, st);
     else
       launch_any<TileI64, 2>(g, st);
     return check_launch("gemm_i8_any_kernel");
   }
-  // 256 x 256 tiles from more than 256 tiles of 256 x 128 on (4096^3 61 us,
-  // 256 x 128 tiles 73; 3000 x 3008 x 2000, 144 tiles, 35 and 44), unless
-  // their padding takes the gain; 256 x 128 while they fill one workgroup per
-  // CU (2048 x 4096 x 4096 36 us; 256 x 256 51, 128 x 128 38; 1536 x 4096 x
-  // 4096 32, 48, 33); below 160 of them 128 x 128 (1024 x 4096 x 4096 24 us,
-  // 256 x 128 29), and 64 x 64 up to 128 of those (1024 x 2048 x 4096 16.3
-  // us, 128 x 128 20.9; three stages, 15.4 us for 512 x 4096 x 4096, four 15.8)
-  if (tiles(256, 128) > 256 && 5 * tiles(256, 256) <= 3 * tiles(256, 128))
+  // 256 x 256 tiles from more than 256 tiles of 256 x 128 on (4096^3 57 us,
+  // 256 x 128 tiles 68), unless their padding takes the gain; 256 x 128 while
+  // they fill one workgroup per CU (2048 x 4096 x 4096 35 us; 256 x 256 48, 128 x
+  // 128 37); below 160 of them 128 x 128, and 64 x 64 up to 128 of those (1024 x
+  // 2048 x 4096 15.8 us, 128 x 128 19.1; three stages, 15.7 us for 512 x 4096 x
+  // 4096, two 18.3), up to 160 with few steps (1500 x 1500 x 1024 8.1 us, 128 x
+  // 128 8.8).
+  // 128 x 128 tiles of eight waves, two workgroups to a CU, store one tile while
+  // they multiply the next.  They take the place of the large tiles where steps
+  // are few (9783 x 1984 x 256 17.8 us, 256 x 256 26.0; 2048 x 4096 x 512 10.7,
+  // 256 x 128 11.4), and where the last round of 256 x 256 tiles leaves many CUs
+  // idle, which costs those a quarter more work a CU (4100 x 4100 x 4096 89.7 us,
+  // 256 x 256 95.8; 5184 x 4544 x 4096 107 and 101); of four waves with three
+  // stages where more than one tile falls to a CU (1100 x 4096 x 4096 28.2 us,
+  // three stages 36.9) or steps are few (2048 x 2048 x 1024 9.2 and 10.6; 4096
+  // deep 25.7 and 22.4).
+  const int64_t t256 = tiles(256, 256), t = tiles(256, 128), t128 = tiles(128, 128);
+  auto rounds = [](int64_t n) { return ceil_div(n, (int64_t)256); };
+  const bool padded = 5 * t256 > 3 * t;
+  if (t128 <= (g.K <= 2048 ? 160 : 128))
+    launch_i8<TileI64, 3>(g, st);
+  else if (t > 256 && !padded && g.K > 512 && 80 * rounds(t256) <= (g.K > 1024 ? 27 : 24) * rounds(t128))
     launch_i8<lds::Tile256, 2>(g, st);
-  else if (tiles(256, 128) > 160)
+  else if (t > 160 && (t <= 256 || padded) && g.K > 1024)
     launch_i8<TileI256x128, 3>(g, st);
-  else if (tiles(128, 128) > 128)
+  else if (t128 <= 256 && g.K > 1536)
     launch_i8<TileI128, 3>(g, st);
   else
-    launch_i8<TileI64, 3>(g, st);
+    launch_i8<TileI128x8, 2>(g, st);
   return check_launch("gemm_i8_kernel");
 }
 
