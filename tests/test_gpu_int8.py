@@ -183,6 +183,16 @@ def test_product_tiles(mdnn, M, N, K):
         _check(mdnn, M, N, K, out, padded, bias=out != "f32", relu=out == "bf16", offset=offset, ldd_pad=3, seed=N)
 
 
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(1000, 783, 333), (1500, 1502, 1000), (1700, 1701, 300), (4100, 1985, 129),
+                                   (1100, 4099, 1700), (1800, 1803, 1605), (2500, 2500, 1101), (4090, 4086, 605)])
+def test_product_each_tile(mdnn, M, N, K, out):
+    """Every tile of rows on 16 bytes, in each type, over the edges of D (by the sizes: 64 x 64, 128 x 128 of both
+    kinds, 256 x 128, 256 x 256), and the same sizes as rows on any byte."""
+    for padded in (True, False):
+        _check(mdnn, M, N, K, out, padded, bias=padded, relu=not padded, ldd_pad=3 if padded else 0, ws=False, seed=K)
+
+
 @pytest.mark.parametrize("M,N,K", [(4200, 4300, 131), (8200, 2100, 45), (1025, 16500, 16 * 9 + 1)])
 def test_product_rows_copied(mdnn, M, N, K):
     """Large products with unaligned rows copy them into the workspace; one operand or both; a workspace too small,
