@@ -723,14 +723,21 @@ mdnn_status_t launch_few(const I8Args& g, bool rows16, hipStream_t st) {
   return check_launch("gemm_i8_few_kernel");
 }
 
-// Few rows: FM fragments of rows; FN columns of 16 as the caller chose.  Up to
-// 16 rows four waves of four stages read weights from memory fastest (1 x 4096 x
-// 4096 5.7 us cold, 1 x 8192 x 8192 14.2; eight of two 6.1 and 15.6, where the
-// weights are in the cache 4.3 and 4.2).
+// Few rows: FM fragments of rows; FN columns of 16 as the caller chose.  FM is
+// the least that needs no more than one block per CU (64 x 1024 x 4096 with 1
+// 4.2 us, 4 5.7; 64 x 2048 x 8192 with 2 7.2, 4 9.4; 40 x 201 x 7085 on any
+// byte 8.6 and 14.5), and otherwise what holds the rows, which reads B once (40
+// x 4096 x 1024 with 3 3.8 us, 1 4.6).  Up to 16 rows four waves of four stages
+// read weights from memory fastest (1 x 4096 x 4096 5.7 us cold, 1 x 8192 x 8192
+// 14.2; eight of two 6.1 and 15.6, where the weights are in the cache 4.3 and
+// 4.2).
 template <int FN>
 mdnn_status_t run_few(const I8Args& g, bool rows16, hipStream_t st) {
-  if (g.M <= 16) return launch_few<1, FN, 4, 4, 8>(g, rows16, st);
-  if (g.M <= 32) return launch_few<2, FN, 4, 3>(g, rows16, st);
+  auto enough = [&](int fm) {
+    return g.M <= fm * 16 || ceil_div(g.M, (int64_t)fm * 16) * ceil_div(g.N, (int64_t)FN * 16) <= 256;
+  };
+  if (enough(1)) return launch_few<1, FN, 4, 4, 8>(g, rows16, st);
+  if (enough(2)) return launch_few<2, FN, 4, 3>(g, rows16, st);
   if (g.M <= 48) return launch_few<3, FN, 4, FN == 1 ? 3 : 2>(g, rows16, st);
   return launch_few<4, FN, 4, FN == 1 ? 3 : 2>(g, rows16, st);
 }
