@@ -847,8 +847,8 @@ extern "C" mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int
   if (!aligned(D, dtype_size(d_type)) || !aligned(a_scale, 4) || !aligned(b_scale, 4) || !aligned(bias, 4) ||
       !aligned(workspace, 16))
     return fail(MDNN_ERR_MISALIGNED, "gemm_i8: misaligned buffer");
-  // (a launch holds fewer than 2^32 threads)
-  if (M > INT64_MAX - 64 || N > INT64_MAX - 64 || ceil_div(M, 64) > (((int64_t)1 << 24) - 1) / ceil_div(N, 64))
+  // (a launch holds fewer than 2^32 threads: 64 x 64 tiles of 256, and half as many tiles of 512 where a side is one tile)
+  if (M > INT64_MAX - 64 || N > INT64_MAX - 64 || ceil_div(M, 64) > (((int64_t)1 << 24) - 2) / ceil_div(N, 64))
     return fail(MDNN_ERR_SHAPE, "gemm_i8: problem too large for the launch grid");
   I8Args g = {};
   g.a = A, g.b = B, g.a_scale = a_scale, g.b_scale = b_scale, g.bias = bias, g.d = D;
