@@ -191,7 +191,7 @@ void set_order(I8Args& g) {
 // address into one of NR register sets (NR steps in flight) and written to the
 // swizzled LDS tiles (two stages, one barrier a step).  A chunk past the row's
 // end is read from its last 16 bytes and shifted; k past K is zero.  1000 x 777
-// x 1531 9.3 us (the latency of 12 steps on one tile per CU), 4095^3 109 us.
+// x 1531 9.0 us (the latency of 12 steps on one tile per CU), 4095^3 109 us.
 // Four and six sets in flight are not faster than two.
 
 typedef uint32_t u4v_a1 __attribute__((ext_vector_type(4), aligned(1)));
@@ -675,6 +675,9 @@ __global__ void __launch_bounds__(W * 64) gemm_i8_few_lds_kernel(I8Args g) {
 }
 
 typedef lds::Tile<64, 64, 2, 2, 2> TileI64;
+// rows on any byte: eight waves, half as many loads and their addresses a wave
+// (1000 x 777 x 1531 9.0 us, four waves 9.8; 500 x 2000 x 1001 7.4 and 8.2)
+typedef lds::Tile<64, 64, 4, 2, 4> TileI64x8;
 // 128 x 128 with eight waves of 64 x 32 and two stages (64 KB): two workgroups
 // per CU
 typedef lds::Tile<128, 128, 2, 4, 4> TileI128x8;
@@ -788,7 +791,7 @@ mdnn_status_t run_i8(I8Args g, void* ws, size_t ws_bytes, hipStream_t st) {
     else if (tiles(128, 128) > 128)
       launch_any<TileI128x8, 2>(g, st);
     else
-      launch_any<TileI64, 2>(g, st);
+      launch_any<TileI64x8, 2>(g, st);
     return check_launch("gemm_i8_any_kernel");
   }
   // 256 x 256 tiles from more than 256 tiles of 256 x 128 on (4096^3 57 us,
