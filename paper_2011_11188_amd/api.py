@@ -217,13 +217,22 @@ def _bytes_of(ws):
     return ws, ws.numel()
 
 
+def _torch_stream(stream):
+    """torch's object of a call's stream.  The handle 0 is the default stream
+    (an ExternalStream of 0 would be one of torch's pool of side streams)."""
+    import torch
+    if not isinstance(stream, int):
+        return stream
+    return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+
+
 def _scratch(n: int, device, stream):
     """A workspace of n bytes that belongs to the call's stream: released when
     the wrapper returns, it goes to later work of that stream only."""
     import torch
     if stream is None:
         return torch.empty((n,), dtype=torch.uint8, device=device)
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+    with torch.cuda.stream(_torch_stream(stream)):
         return torch.empty((n,), dtype=torch.uint8, device=device)
 
 
