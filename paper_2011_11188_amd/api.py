@@ -30,6 +30,38 @@ def torch_dtype(code: int):
     return {F32: torch.float32, F16: torch.float16, BF16: torch.bfloat16}[code]
 
 
+def _torch_stream(stream):
+    """torch's object of a call's stream.  The handle 0 is the default stream
+    (an ExternalStream of 0 would be one of torch's pool of side streams)."""
+    import torch
+    if not isinstance(stream, int):
+        return stream
+    return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+
+
+def _scratch(n: int, device, stream):
+    """A workspace of n bytes that belongs to the call's stream: released when
+    the wrapper returns, it goes to later work of that stream only."""
+    import torch
+    if stream is None:
+        return torch.empty((n,), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(_torch_stream(stream)):
+        return torch.empty((n,), dtype=torch.uint8, device=device)
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory for a result of a call on `stream`: that stream's own, which no
+    pending work of another one still uses, and not handed out again before
+    the work that the caller's current stream has by its release is done."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_torch_stream(stream)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def gemm(layout: int, A, B, out_dtype=None, bias=None, act: int = ACT_NONE, mask=None,
          alpha: float = 1.0, beta: float = 0.0, Cm=None, out=None, stream=None, workspace=None,
          nonfinite=None):
@@ -197,11 +229,11 @@ def _like(t, x, name: str):
     return t, _rows_of(t, name)[2]
 
 
-def _codes_like(q, rows: int, cols: int, device):
+def _codes_like(q, rows: int, cols: int, device, stream):
     """Room for [rows, cols] codes; allocated rows start on 128 bytes (a cache line)."""
     import torch
     if q is None:
-        q = torch.empty((rows, (cols + 127) // 128 * 128), dtype=torch.int8, device=device)[:, :cols]
+        q = _empty((rows, (cols + 127) // 128 * 128), torch.int8, device, stream)[:, :cols]
     elif q.dtype != torch.int8 or tuple(q.shape) != (rows, cols):
         raise ValueError(f"q must be int8 [{rows}, {cols}]")
     return q, _rows_of(q, "q")[2]
@@ -217,25 +249,6 @@ def _bytes_of(ws):
     return ws, ws.numel()
 
 
-def _torch_stream(stream):
-    """torch's object of a call's stream.  The handle 0 is the default stream
-    (an ExternalStream of 0 would be one of torch's pool of side streams)."""
-    import torch
-    if not isinstance(stream, int):
-        return stream
-    return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-
-
-def _scratch(n: int, device, stream):
-    """A workspace of n bytes that belongs to the call's stream: released when
-    the wrapper returns, it goes to later work of that stream only."""
-    import torch
-    if stream is None:
-        return torch.empty((n,), dtype=torch.uint8, device=device)
-    with torch.cuda.stream(_torch_stream(stream)):
-        return torch.empty((n,), dtype=torch.uint8, device=device)
-
-
 def quantize_i8(x, transpose: bool = False, q=None, scale=None, workspace=None, stream=None):
     """(codes, scales) of a 2-D tensor: int8 codes with an fp32 scale for each
     row, or with transpose for each column, the codes stored [cols, rows] (a
@@ -243,8 +256,8 @@ def quantize_i8(x, transpose: bool = False, q=None, scale=None, workspace=None, 
     import torch
     rows, cols, ldx = _rows_of(x, "x")
     n = cols if transpose else rows
-    q, ldq = _codes_like(q, n, rows if transpose else cols, x.device)
-    scale = torch.empty((n,), dtype=torch.float32, device=x.device) if scale is None else _vector_of(scale, n, "scale")
+    q, ldq = _codes_like(q, n, rows if transpose else cols, x.device, stream)
+    scale = _empty((n,), torch.float32, x.device, stream) if scale is None else _vector_of(scale, n, "scale")
     if not transpose:
         mdnn_quantize_i8(rows, cols, x, ldx, dtype_of(x), q, ldq, scale, stream)
         return q, scale
@@ -266,7 +279,7 @@ def gemm_i8(A, a_scale, B, b_scale, bias=None, act: int = ACT_NONE, out_dtype=No
         raise ValueError("A and B must be int8 codes of one depth")
     _vector_of(a_scale, M, "a_scale"), _vector_of(b_scale, N, "b_scale"), _vector_of(bias, N, "bias")
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype or torch.float32, device=A.device)
+        out = _empty((M, N), out_dtype or torch.float32, A.device, stream)
     elif tuple(out.shape) != (M, N):
         raise ValueError(f"out must be [{M}, {N}]")
     if workspace is True:
@@ -279,13 +292,12 @@ def gemm_i8(A, a_scale, B, b_scale, bias=None, act: int = ACT_NONE, out_dtype=No
 def rmsnorm(x, gamma=None, residual=None, eps: float = 1e-6, h_out=None, out=None, stream=None):
     """y = h * gamma / sqrt(mean(h^2) + eps) of the rows of h = x + residual.
     Returns y, or (y, h) with a residual (h_out is allocated then)."""
-    import torch
     rows, cols, ldx = _rows_of(x, "x")
     residual, ldr = _like(residual, x, "residual")
     if residual is not None and h_out is None:
-        h_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        h_out = _empty((rows, cols), x.dtype, x.device, stream)
     h_out, ldh = _like(h_out, x, "h_out")
-    out, ldy = _like(torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out, x, "out")
+    out, ldy = _like(_empty((rows, cols), x.dtype, x.device, stream) if out is None else out, x, "out")
     mdnn_rmsnorm_fwd(rows, cols, x, ldx, residual, ldr, _vector_of(gamma, cols, "gamma"), eps, h_out, ldh, out, ldy,
                      dtype_of(x), stream)
     return (out, h_out) if h_out is not None else out
@@ -298,11 +310,10 @@ def rmsnorm_i8(x, gamma=None, residual=None, eps: float = 1e-6, h_out=None, q=No
     rows, cols, ldx = _rows_of(x, "x")
     residual, ldr = _like(residual, x, "residual")
     if residual is not None and h_out is None:
-        h_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        h_out = _empty((rows, cols), x.dtype, x.device, stream)
     h_out, ldh = _like(h_out, x, "h_out")
-    q, ldq = _codes_like(q, rows, cols, x.device)
-    scale = (torch.empty((rows,), dtype=torch.float32, device=x.device) if scale is None
-             else _vector_of(scale, rows, "scale"))
+    q, ldq = _codes_like(q, rows, cols, x.device, stream)
+    scale = _empty((rows,), torch.float32, x.device, stream) if scale is None else _vector_of(scale, rows, "scale")
     mdnn_rmsnorm_i8_fwd(rows, cols, x, ldx, residual, ldr, _vector_of(gamma, cols, "gamma"), eps, h_out, ldh, q, ldq,
                         scale, dtype_of(x), stream)
     return (q, scale, h_out) if h_out is not None else (q, scale)
@@ -318,11 +329,11 @@ def rmsnorm_bwd(dy, h, gamma=None, eps: float = 1e-6, dres=None, dx=None, with_d
         raise ValueError("h is required")
     h, ldh = _like(h, dy, "h")
     dres, lddr = _like(dres, dy, "dres")
-    dx, lddx = _like(torch.empty((rows, cols), dtype=dy.dtype, device=dy.device) if dx is None else dx, dy, "dx")
+    dx, lddx = _like(_empty((rows, cols), dy.dtype, dy.device, stream) if dx is None else dx, dy, "dx")
     if not with_dgamma:
         dgamma = None
     elif dgamma is None:
-        dgamma = torch.empty((cols,), dtype=torch.float32, device=dy.device)
+        dgamma = _empty((cols,), torch.float32, dy.device, stream)
     else:
         _vector_of(dgamma, cols, "dgamma")
     if with_dgamma and workspace is None:

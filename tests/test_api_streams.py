@@ -30,13 +30,25 @@ def streams(monkeypatch):
     monkeypatch.setattr(torch.cuda, "stream", s.use)
     monkeypatch.setattr(torch.cuda, "ExternalStream", external)
     monkeypatch.setattr(torch.cuda, "default_stream", lambda *a: "default")
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: s.stack[-1])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)  # (a host tensor's device index)
     empty = torch.empty
     s.made = []
+    s.also_used = []
+
+    class Device(torch.Tensor):
+        """A host tensor that the wrappers take for one of the current GPU."""
+        is_cuda = True
+
+        def record_stream(self, stream):
+            s.also_used.append((tuple(self.shape), stream))
 
     def record(*args, **kw):
-        t = empty(*args, **kw)
+        t = empty(*args, **kw).as_subclass(Device)
         s.made.append((tuple(t.shape), s.stack[-1]))
         return t
+
+    s.tensor = lambda shape, dtype=torch.float32: torch.zeros(shape, dtype=dtype).as_subclass(Device)
 
     monkeypatch.setattr(torch, "empty", record)
     return s
@@ -47,4 +59,40 @@ def test_a_workspace_belongs_to_the_calls_stream(streams, given, owner):
     from paper_2011_11188_amd import api
     api._scratch(48, "cpu", given)
     assert streams.made == [((48,), owner)]
+    assert streams.stack == ["current"]
+
+
+def _calls(m, new):
+    """(call, shapes of the results that it allocates) of the wrappers of the 8-bit and norm operators."""
+    import torch
+    x = new((6, 20))
+    codes, wcodes = new((6, 20), torch.int8), new((9, 20), torch.int8)
+    v6, v9, v20 = new((6,)), new((9,)), new((20,))
+    return {
+        "quantize_i8": (lambda **k: m.quantize_i8(x, **k), [(6, 128), (6,)]),
+        "quantize_i8 columns": (lambda **k: m.quantize_i8(x, transpose=True, **k), [(20, 128), (20,)]),
+        "gemm_i8": (lambda **k: m.gemm_i8(codes, v6, wcodes, v9, workspace=True, **k), [(6, 9)]),
+        "rmsnorm": (lambda **k: m.rmsnorm(x, v20, x, **k), [(6, 20), (6, 20)]),
+        "rmsnorm_i8": (lambda **k: m.rmsnorm_i8(x, v20, x, **k), [(6, 20), (6, 128), (6,)]),
+        "rmsnorm_bwd": (lambda **k: m.rmsnorm_bwd(x, x, v20, **k), [(6, 20), (20,)]),
+    }
+
+
+NAMES = ["quantize_i8", "quantize_i8 columns", "gemm_i8", "rmsnorm", "rmsnorm_i8", "rmsnorm_bwd"]
+
+
+@pytest.mark.parametrize("given,owner", [(None, "current"), (0, "default"), (64, ("external", 64)), ("side", "side")])
+@pytest.mark.parametrize("name", NAMES)
+def test_results_belong_to_the_calls_stream(streams, monkeypatch, name, given, owner):
+    """What a wrapper allocates is the memory of the stream that writes it, and its results are also kept for the
+    stream that was current, where the caller uses them."""
+    import paper_2011_11188_amd as m
+    from paper_2011_11188_amd import api
+    for f in dir(api):
+        if f.startswith("mdnn_") and not f.endswith("_workspace"):
+            monkeypatch.setattr(api, f, lambda *a, **k: None)
+    call, results = _calls(m, streams.tensor)[name]
+    call(stream=given)
+    assert len(streams.made) >= len(results) and all(o == owner for _, o in streams.made), streams.made
+    assert sorted(streams.also_used) == ([] if given is None else sorted((r, "current") for r in results))
     assert streams.stack == ["current"]
