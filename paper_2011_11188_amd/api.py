@@ -2,6 +2,10 @@
 
 These derive sizes and leading dimensions from torch tensor shapes, allocate
 outputs and workspaces with torch, and call the ``mdnn_*`` entry points.
+With a ``stream`` argument (a torch stream or a handle; None: the current one)
+the call runs on that stream and what it allocates is that stream's memory;
+results are kept, too, until the current stream's work at their release is done.
+Ordering the two streams is the caller's, as with torch's own operations.
 """
 from __future__ import annotations
 
@@ -77,7 +81,7 @@ def gemm(layout: int, A, B, out_dtype=None, bias=None, act: int = ACT_NONE, mask
         M, K = A.shape
     N = B.shape[0] if layout == NT else B.shape[1]
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype or torch.float32, device=A.device)
+        out = _empty((M, N), out_dtype or torch.float32, A.device, stream)
     args = (layout, M, N, K, alpha, A, A.stride(0), B, B.stride(0), dtype_of(A), beta, Cm,
             Cm.stride(0) if Cm is not None else 0, out, out.stride(0), dtype_of(out), bias,
             act, mask, mask.stride(0) if mask is not None else 0)
@@ -86,7 +90,7 @@ def gemm(layout: int, A, B, out_dtype=None, bias=None, act: int = ACT_NONE, mask
         return out
     if workspace is True:
         nb = mdnn_gemm_workspace(dtype_of(A), M, N, K)
-        workspace = torch.empty((max(nb, 16),), dtype=torch.uint8, device=A.device)
+        workspace = _scratch(max(nb, 16), A.device, stream)
     mdnn_gemm_mixed_ws(*args, workspace, workspace.numel() if workspace is not None else 0, stream,
                        nonfinite=nonfinite)
     return out
@@ -99,10 +103,10 @@ def split_f16(x, scale: float = 1.0, stream=None, scale_out=None):
     not given, returned as the third value)."""
     import torch
     rows, cols = x.shape
-    hi = torch.empty((rows, cols), dtype=torch.float16, device=x.device)
-    lo = torch.empty_like(hi)
+    hi = _empty((rows, cols), torch.float16, x.device, stream)
+    lo = _empty((rows, cols), torch.float16, x.device, stream)
     if scale == 0.0 and scale_out is None:
-        scale_out = torch.empty((1,), dtype=torch.float32, device=x.device)
+        scale_out = _empty((1,), torch.float32, x.device, stream)
     mdnn_split_f16(rows, cols, x, x.stride(0), scale, scale_out, hi, cols, lo, cols, stream)
     return (hi, lo, scale_out) if scale == 0.0 else (hi, lo)
 
@@ -118,9 +122,9 @@ def gemm_split3(layout: int, A, B, a_scale: float = 1.0, b_scale: float = 1.0, a
         M, K = A.shape
     N = B.shape[0] if layout == NT else B.shape[1]
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float32, device=A.device)
+        out = _empty((M, N), torch.float32, A.device, stream)
     ws_bytes = mdnn_gemm_split3_workspace(M, N, K)
-    ws = torch.empty((max(ws_bytes, 256),), dtype=torch.uint8, device=A.device)
+    ws = _scratch(max(ws_bytes, 256), A.device, stream)
     mdnn_gemm_split3(layout, M, N, K, alpha, A, A.stride(0), a_scale, B, B.stride(0), b_scale, beta, Cm,
                      Cm.stride(0) if Cm is not None else 0, out, out.stride(0), ws, ws_bytes, stream)
     return out
@@ -132,11 +136,10 @@ def conv_shape(x_shape: Sequence[int], c_out: int, r: int, s: int, pad: int) -> 
 
 
 def conv2d_fwd(x, w, pad: int, bias=None, act: int = ACT_NONE, out_dtype=None, stream=None):
-    import torch
     k, r, s, c = w.shape
     sh = conv_shape(x.shape, k, r, s, pad)
     ho, wo = sh.h + 2 * pad - r + 1, sh.w + 2 * pad - s + 1
-    y = torch.empty((sh.n, ho, wo, k), dtype=out_dtype or x.dtype, device=x.device)
+    y = _empty((sh.n, ho, wo, k), out_dtype or x.dtype, x.device, stream)
     mdnn_conv2d_fwd(sh, x, w, dtype_of(x), bias, act, y, dtype_of(y), stream)
     return y
 
@@ -146,15 +149,14 @@ def conv2d_fwd_algo(x, w, pad: int, algo: int, bias=None, act: int = ACT_NONE, o
     """conv2d_fwd through a chosen algorithm (CONV_AUTO: the library's
     per-layer choice for the given workspace; a workspace of the algorithm's
     size is allocated when none is given)."""
-    import torch
     k, r, s, c = w.shape
     sh = conv_shape(x.shape, k, r, s, pad)
     ho, wo = sh.h + 2 * pad - r + 1, sh.w + 2 * pad - s + 1
-    y = torch.empty((sh.n, ho, wo, k), dtype=out_dtype or x.dtype, device=x.device)
+    y = _empty((sh.n, ho, wo, k), out_dtype or x.dtype, x.device, stream)
     io = dtype_of(x)
     if workspace is None:
         need = mdnn_conv2d_fwd_algo_workspace(sh, io, algo)
-        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=x.device)
+        workspace = _scratch(max(need, 256), x.device, stream)
     mdnn_conv2d_fwd_algo(sh, x, w, io, bias, act, y, dtype_of(y), algo, workspace, workspace.numel(), stream)
     return y
 
@@ -162,23 +164,21 @@ def conv2d_fwd_algo(x, w, pad: int, algo: int, bias=None, act: int = ACT_NONE, o
 def conv2d_fwd_winograd(x, w, pad: int, bias=None, act: int = ACT_NONE, out_dtype=None, workspace=None,
                         stream=None):
     """conv2d_fwd through Winograd F(2x2, 3x3) (3x3 filters, fp16 / bf16)."""
-    import torch
     k, r, s, c = w.shape
     sh = conv_shape(x.shape, k, r, s, pad)
     ho, wo = sh.h + 2 * pad - r + 1, sh.w + 2 * pad - s + 1
-    y = torch.empty((sh.n, ho, wo, k), dtype=out_dtype or x.dtype, device=x.device)
+    y = _empty((sh.n, ho, wo, k), out_dtype or x.dtype, x.device, stream)
     nb = mdnn_conv2d_fwd_winograd_workspace(sh, dtype_of(x))
     if workspace is None:
-        workspace = torch.empty((max(nb, 256),), dtype=torch.uint8, device=x.device)
+        workspace = _scratch(max(nb, 256), x.device, stream)
     mdnn_conv2d_fwd_winograd(sh, x, w, dtype_of(x), bias, act, y, dtype_of(y), workspace, workspace.numel(), stream)
     return y
 
 
 def conv2d_bwd_data(dy, w, pad: int, h: int, wd: int, mask=None, out_dtype=None, stream=None):
-    import torch
     k, r, s, c = w.shape
     sh = ConvShape(dy.shape[0], h, wd, c, k, r, s, pad)
-    dx = torch.empty((sh.n, h, wd, c), dtype=out_dtype or dy.dtype, device=dy.device)
+    dx = _empty((sh.n, h, wd, c), out_dtype or dy.dtype, dy.device, stream)
     mdnn_conv2d_bwd_data(sh, dy, w, dtype_of(dy), mask, dx, dtype_of(dx), stream)
     return dx
 
@@ -188,10 +188,10 @@ def conv2d_bwd_filter(x, dy, r: int, s: int, pad: int, with_db: bool = True, str
     n, h, wd, c = x.shape
     k = dy.shape[3]
     sh = ConvShape(n, h, wd, c, k, r, s, pad)
-    dw = torch.empty((k, r, s, c), dtype=torch.float32, device=x.device)
-    db = torch.empty((k,), dtype=torch.float32, device=x.device) if with_db else None
+    dw = _empty((k, r, s, c), torch.float32, x.device, stream)
+    db = _empty((k,), torch.float32, x.device, stream) if with_db else None
     ws_bytes = mdnn_conv2d_bwd_filter_workspace(sh, dtype_of(x))
-    ws = torch.empty((max(ws_bytes, 16),), dtype=torch.uint8, device=x.device)
+    ws = _scratch(max(ws_bytes, 16), x.device, stream)
     mdnn_conv2d_bwd_filter(sh, x, dy, dtype_of(x), dw, db, ws, ws_bytes, stream)
     return dw, db
 

@@ -63,9 +63,10 @@ def test_a_workspace_belongs_to_the_calls_stream(streams, given, owner):
 
 
 def _calls(m, new):
-    """(call, shapes of the results that it allocates) of the wrappers of the 8-bit and norm operators."""
+    """(call, shapes of the results that it allocates) of every wrapper that takes a stream."""
     import torch
-    x = new((6, 20))
+    x, w = new((6, 20)), new((9, 20))
+    img, filt, dy = new((2, 8, 8, 4), torch.float16), new((5, 3, 3, 4), torch.float16), new((2, 8, 8, 5), torch.float16)
     codes, wcodes = new((6, 20), torch.int8), new((9, 20), torch.int8)
     v6, v9, v20 = new((6,)), new((9,)), new((20,))
     return {
@@ -75,10 +76,19 @@ def _calls(m, new):
         "rmsnorm": (lambda **k: m.rmsnorm(x, v20, x, **k), [(6, 20), (6, 20)]),
         "rmsnorm_i8": (lambda **k: m.rmsnorm_i8(x, v20, x, **k), [(6, 20), (6, 128), (6,)]),
         "rmsnorm_bwd": (lambda **k: m.rmsnorm_bwd(x, x, v20, **k), [(6, 20), (20,)]),
+        "gemm": (lambda **k: m.gemm(m.NT, x, w, workspace=True, **k), [(6, 9)]),
+        "split_f16": (lambda **k: m.split_f16(x, 0.0, **k), [(6, 20), (6, 20), (1,)]),
+        "gemm_split3": (lambda **k: m.gemm_split3(m.NT, x, w, **k), [(6, 9)]),
+        "conv2d_fwd": (lambda **k: m.conv2d_fwd(img, filt, 1, **k), [(2, 8, 8, 5)]),
+        "conv2d_fwd_algo": (lambda **k: m.conv2d_fwd_algo(img, filt, 1, m.CONV_AUTO, **k), [(2, 8, 8, 5)]),
+        "conv2d_fwd_winograd": (lambda **k: m.conv2d_fwd_winograd(img, filt, 1, **k), [(2, 8, 8, 5)]),
+        "conv2d_bwd_data": (lambda **k: m.conv2d_bwd_data(dy, filt, 1, 8, 8, **k), [(2, 8, 8, 4)]),
+        "conv2d_bwd_filter": (lambda **k: m.conv2d_bwd_filter(img, dy, 3, 3, 1, **k), [(5, 3, 3, 4), (5,)]),
     }
 
 
-NAMES = ["quantize_i8", "quantize_i8 columns", "gemm_i8", "rmsnorm", "rmsnorm_i8", "rmsnorm_bwd"]
+NAMES = ["quantize_i8", "quantize_i8 columns", "gemm_i8", "rmsnorm", "rmsnorm_i8", "rmsnorm_bwd", "gemm", "split_f16",
+         "gemm_split3", "conv2d_fwd", "conv2d_fwd_algo", "conv2d_fwd_winograd", "conv2d_bwd_data", "conv2d_bwd_filter"]
 
 
 @pytest.mark.parametrize("given,owner", [(None, "current"), (0, "default"), (64, ("external", 64)), ("side", "side")])

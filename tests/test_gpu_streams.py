@@ -20,15 +20,27 @@ def _calls(m):
     codes = torch.randint(-127, 128, (4100, 33), generator=g, dtype=torch.int8, device="cuda")
     wide = torch.randint(-127, 128, (8300, 33), generator=g, dtype=torch.int8, device="cuda")
     sa, sb = torch.rand(4100, generator=g, device="cuda"), torch.rand(8300, generator=g, device="cuda")
+    half = x.half()
+    img, grad = (torch.randn(64, 28, 28, c, generator=g, device="cuda").half() for c in (32, 64))
+    filt = torch.randn(64, 3, 3, 32, generator=g, device="cuda").half()
     return {"quantize_i8": lambda **k: m.quantize_i8(x, **k),
             "quantize_i8 columns": lambda **k: m.quantize_i8(x, transpose=True, **k),
             "gemm_i8": lambda **k: (m.gemm_i8(codes, sa, wide, sb, workspace=True, **k),),
             "rmsnorm": lambda **k: m.rmsnorm(x, gamma, dy, **k),
             "rmsnorm_i8": lambda **k: m.rmsnorm_i8(x, gamma, dy, **k),
-            "rmsnorm_bwd": lambda **k: m.rmsnorm_bwd(dy, x, gamma, **k)}
+            "rmsnorm_bwd": lambda **k: m.rmsnorm_bwd(dy, x, gamma, **k),
+            "gemm": lambda **k: (m.gemm(m.NT, half, half, workspace=True, **k),),
+            "split_f16": lambda **k: m.split_f16(x, 0.0, **k),
+            "gemm_split3": lambda **k: (m.gemm_split3(m.NT, x, dy, **k),),
+            "conv2d_fwd": lambda **k: (m.conv2d_fwd(img, filt, 1, **k),),
+            "conv2d_fwd_algo": lambda **k: (m.conv2d_fwd_algo(img, filt, 1, m.CONV_IM2COL_GEMM, **k),),
+            "conv2d_fwd_winograd": lambda **k: (m.conv2d_fwd_winograd(img, filt, 1, **k),),
+            "conv2d_bwd_data": lambda **k: (m.conv2d_bwd_data(grad, filt, 1, 28, 28, **k),),
+            "conv2d_bwd_filter": lambda **k: m.conv2d_bwd_filter(img, grad, 3, 3, 1, **k)}
 
 
-NAMES = ["quantize_i8", "quantize_i8 columns", "gemm_i8", "rmsnorm", "rmsnorm_i8", "rmsnorm_bwd"]
+NAMES = ["quantize_i8", "quantize_i8 columns", "gemm_i8", "rmsnorm", "rmsnorm_i8", "rmsnorm_bwd", "gemm", "split_f16",
+         "gemm_split3", "conv2d_fwd", "conv2d_fwd_algo", "conv2d_fwd_winograd", "conv2d_bwd_data", "conv2d_bwd_filter"]
 
 
 @pytest.mark.parametrize("handle", [False, True])
