@@ -438,3 +438,31 @@ def test_own_workspaces_on_the_default_streams_handle(mdnn):
     x, dy = torch.randn(2000, 500, device="cuda"), torch.randn(2000, 500, device="cuda")
     for call in (lambda **k: mdnn.quantize_i8(x, transpose=True, **k), lambda **k: mdnn.rmsnorm_bwd(dy, x, **k)):
         assert all(torch.equal(a, b) for a, b in zip(call(), call(stream=0)))
+
+
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(1000, 783, 384), (1000, 783, 1152),     # 64 x 64
+                                   (2500, 2500, 256), (2500, 2500, 640),    # 128 x 128, eight waves
+                                   (1800, 1803, 1664), (1800, 1803, 2048),  # 128 x 128, four waves
+                                   (1100, 4099, 1792), (1100, 4099, 1920),  # 256 x 128
+                                   (4090, 4086, 640), (4090, 4086, 1280)])  # 256 x 256
+def test_product_whole_steps(mdnn, M, N, K, out):
+    """Depths of whole 128-byte steps, whose loads are not checked against the row's end, on every tile of rows on 16
+    bytes, over the edges of D and with an even and an odd count of steps after the steady rounds."""
+    assert K % 128 == 0
+    _check(mdnn, M, N, K, out, True, bias=out != "f16", relu=out != "f32", ldd_pad=3, ws=False, seed=K)
+
+
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("K", [1040, 1111, 1407])
+def test_product_ragged_depths_of_the_largest_tile(mdnn, K, out):
+    """256 x 256 tiles whose last step is a partial one: whole 16-byte chunks, and bytes beyond them."""
+    _check(mdnn, 4090, 4086, K, out, True, bias=True, relu=False, ldd_pad=5, ws=False, seed=K)
+
+
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("K", [1021, 1660])
+def test_product_rows_copied_to_whole_steps(mdnn, K, out):
+    """Copied rows of more than 512 bytes, which the 256 x 256 tiles take."""
+    assert mdnn.mdnn_gemm_i8_workspace(4095, 4095, K) == 2 * 4095 * ((K + 127) // 128 * 128)
+    _check(mdnn, 4095, 4095, K, out, False, bias=True, relu=True, offset=3, seed=K)
