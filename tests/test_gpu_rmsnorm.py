@@ -336,3 +336,45 @@ def test_api_refuses(mdnn):
             bad()
     with pytest.raises(mdnn.MdnnError):
         mdnn.rmsnorm(x, g, eps=0.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(40001, 128), (40001, 200), (9000, 512), (9001, 1000), (2600, 2000), (2601, 3999),
+                                       (1100, 8192), (1101, 8185), (700, 16384), (701, 9001), (600, 20000)])
+def test_gradients_of_many_rows(mdnn, rows, cols, dtype):
+    """Every shape of the gradients' kernels with several rows to a block in turn, the last turn a partial one, with
+    gamma and the residual's gradient; in 64 bits on the GPU."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(rows + cols)
+    make = lambda: (torch.randn(rows, cols, generator=g, device="cuda")
+                    * torch.exp(torch.randn(rows, 1, generator=g, device="cuda"))).to(_t(dtype))
+    h, dy, dres = make(), make(), make()
+    gamma = 1 + 0.2 * torch.randn(cols, generator=g, device="cuda")
+    dx, dg = mdnn.rmsnorm_bwd(dy, h, gamma, EPS, dres)
+    h, dy, dres, gamma = h.double(), dy.double(), dres.double(), gamma.double()
+    r = 1 / torch.sqrt((h * h).mean(1, keepdim=True) + EPS)
+    xh, along = h * r, gamma * dy
+    want = r * (along - xh * (along * xh).mean(1, keepdim=True)) + dres
+    size = r * (along.abs() + xh.abs() * (along * xh).abs().mean(1, keepdim=True)) + dres.abs()
+    tol = (2 * _sum_bound(cols) + 12 * U) * size + 1.01 * HALF[dtype] * want.abs() + TINY[dtype]
+    assert bool(((dx.double() - want).abs() <= tol).all())
+    # a column's sum: 256 thread groups at least take the rows in turn, at most 32 of them are joined in a block, and
+    # the blocks' sums in chains of at most 16 and 32; each term within the rms' error and two products
+    terms = dy * xh
+    chain = -(-rows // 256) + 32 + 16 + 32
+    tol = (chain * U + _sum_bound(cols) / 2 + 8 * U) * terms.abs().sum(0)
+    assert bool(((dg.double() - terms.sum(0)).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 20) + 5, 5), ((1 << 24) + 5, 130), ((1 << 22) + 5, 264), ((1 << 20) + 5, 1032),
+                                       ((1 << 20) + 5, 4104)])
+def test_more_rows_than_blocks(mdnn, rows, cols):
+    """Blocks that walk on to a second row: each half of the rows by itself, one row a block, gives the same."""
+    import torch
+    x = torch.empty((rows, cols), dtype=torch.float16, device="cuda").normal_()
+    gamma = dev(_gamma(cols), "f32")
+    for f in (lambda t: (mdnn.rmsnorm(t, gamma, eps=EPS),), lambda t: mdnn.rmsnorm_i8(t, gamma, eps=EPS),
+              lambda t: mdnn.quantize_i8(t)):
+        whole = f(x)
+        for half in (slice(0, rows // 2), slice(rows // 2, rows)):
+            assert all(torch.equal(a[half], b) for a, b in zip(whole, f(x[half])))
