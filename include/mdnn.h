@@ -498,7 +498,8 @@ mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int8_t* A, int
  *   mdnn_rmsnorm_i8_fwd  codes and a scale for each row, as defined above for
  *     t = fl(h * gamma), with scale = fl(a / 127) / sqrt(mean(h^2) + eps): the
  *     root is common to a row's elements, so the codes do not depend on it.
- * Sums are fp32 in a fixed order (deterministic).  A row that holds Inf or
+ * Sums are in a fixed order (deterministic), fp32 and, in rows longer than the
+ * registers hold, partly 64-bit.  A row that holds Inf or
  * NaN, or whose sum of squares passes fp32's range, gives NaN in all of y
  * (codes 0 and scale NaN; also where h * gamma overflows).
  * cols >= 1 and <= 2^29, any rows >= 0, leading dimensions >= cols; buffers

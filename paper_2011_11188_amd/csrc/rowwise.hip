@@ -320,7 +320,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_kernel(RowArgs a) {
 
 // Rows of any length, element by element, read again for each use, LONG_U
 // elements of a thread in flight (past the row's end: its last element again,
-// not used; one in flight: 4096 x 40000 bf16 725 us, eight 370).  A thread
+// not used; one in flight: 4096 x 40000 bf16 725 us, eight 370).  A thread adds
+// the elements in flight in fp32 and those sums in 64 bits: up to 2^19 elements
+// fall to one, and in a chain of fp32 additions terms of one size lose their low
+// bits on one side (2^26 columns of 0.1: the norm off by 2.7e-4).  A thread
 // reads an element for the last time before it writes that element, so
 // outputs may lie in place of the inputs as in the kernel above.
 constexpr int LONG_U = 8;
@@ -355,18 +358,22 @@ __global__ void __launch_bounds__(1024) row_long_kernel(RowArgs a) {
     LongRow<T> h;
     LongRow<F32> g;
     SumMax v = {0.0f, 0u};
+    double sum = 0.0;
     for (int c0 = threadIdx.x; c0 < a.cols; c0 += LONG_U * 1024) {
       load(c0, h, g);
+      float s = 0.0f;
 #pragma unroll
       for (int u = 0; u < LONG_U; ++u) {
         if (c0 + u * 1024 >= a.cols) continue;
         float t = h.v[u];
-        if (MODE != QUANT) v.s = fmaf(t, t, v.s);
+        if (MODE != QUANT) s = fmaf(t, t, s);
         if (MODE == NORM_I8 && a.gamma) t = mul_rn(t, g.v[u]);
         const uint32_t b = __float_as_uint(t) & 0x7fffffffu;
         v.m = b > v.m ? b : v.m;
       }
+      if (MODE != QUANT) sum += (double)s;
     }
+    v.s = (float)sum;
     v = row_reduce<1024>(v, buf, flip);
     const float rstd = MODE == QUANT ? 1.0f : row_rstd(v.s, (float)a.cols, a.eps);
     const RowScale k = row_scale(v.m, MODE == NORM_I8 && !isfinite(v.s));
@@ -605,19 +612,21 @@ __global__ void __launch_bounds__(1024) norm_bwd_long_kernel(BwdArgs a) {
     const S *dy = (const S*)a.dy + row * a.lddy, *hp = (const S*)a.h + row * a.ldh;
     LongRow<T> h, d, r;
     LongRow<F32> g, p;
-    Sum2 v = {0.0f, 0.0f};
+    double sum_a = 0.0, sum_b = 0.0;
     for (int c0 = threadIdx.x; c0 < a.cols; c0 += LONG_U * 1024) {
       h.load(hp, c0, a.cols);
       d.load(dy, c0, a.cols);
       if (a.gamma) g.load(a.gamma, c0, a.cols);
+      Sum2 s = {0.0f, 0.0f};
 #pragma unroll
       for (int u = 0; u < LONG_U; ++u) {
         if (c0 + u * 1024 >= a.cols) continue;
-        v.a = fmaf(h.v[u], h.v[u], v.a);
-        v.b = fmaf(a.gamma ? d.v[u] * g.v[u] : d.v[u], h.v[u], v.b);
+        s.a = fmaf(h.v[u], h.v[u], s.a);
+        s.b = fmaf(a.gamma ? d.v[u] * g.v[u] : d.v[u], h.v[u], s.b);
       }
+      sum_a += (double)s.a, sum_b += (double)s.b;
     }
-    v = row_reduce<1024, 1>(v, buf, flip);
+    const Sum2 v = row_reduce<1024, 1>(Sum2{(float)sum_a, (float)sum_b}, buf, flip);
     const float rstd = row_rstd(v.a, (float)a.cols, a.eps), k = rstd * v.b / (float)a.cols;
     float* sums = a.partial ? a.partial + (int64_t)blockIdx.x * a.cols : nullptr;
     const bool first = row == (int64_t)blockIdx.x;

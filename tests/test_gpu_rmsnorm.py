@@ -378,3 +378,37 @@ def test_more_rows_than_blocks(mdnn, rows, cols):
         whole = f(x)
         for half in (slice(0, rows // 2), slice(rows // 2, rows)):
             assert all(torch.equal(a[half], b) for a, b in zip(whole, f(x[half])))
+
+
+# The sums of the kernels for long rows, whatever the length: eight terms at a time in fp32 and those sums in 64 bits,
+# a rounding to fp32, and the tree and chain of at most 26 additions over the threads.
+LONG_SUM = (8 + 1 + 26) * U
+
+
+@pytest.mark.parametrize("value", [1.1, 0.1, 1.37])
+def test_long_rows_of_one_magnitude(mdnn, value):
+    """Terms of one size, whose roundings all fall to one side: the sums do not lose bits with the row's length."""
+    import torch
+    rows, cols = 2, (1 << 26) + 3
+    h = torch.full((rows, cols), value, device="cuda")
+    h[1] *= -2
+    hd = h[:, :1].double()
+    y = mdnn.rmsnorm(h, None, eps=EPS)
+    want = hd / torch.sqrt(hd * hd + EPS)
+    assert bool(((y.double() - want).abs() <= (LONG_SUM / 2 + 9 * U + 1.01 * HALF["f32"]) * want.abs()).all())
+    q, s = mdnn.rmsnorm_i8(h, None, eps=EPS)
+    want = (hd.abs() / 127 / torch.sqrt(hd * hd + EPS))[:, 0]
+    assert bool(((s.double() - want).abs() <= (LONG_SUM / 2 + 9 * U) * want).all())
+    # every other gradient 0: mean(dy xh) is not lost in dx's difference
+    dy = torch.zeros(rows, cols, device="cuda")
+    dy[:, ::2] = 0.7
+    d = dy[:, :2].double()
+    r = 1 / torch.sqrt(hd * hd + EPS)
+    mean = d[:, :1] * hd * r * ((cols + 1) // 2) / cols
+    dx, dg = mdnn.rmsnorm_bwd(dy, h, eps=EPS)
+    size = r * (d.abs() + (hd * r).abs() * mean.abs())
+    for c in (0, 1):
+        want = r * (d[:, c:c + 1] - hd * r * mean)
+        assert bool(((dx[:, c::2].double() - want).abs() <= (2 * LONG_SUM + 13 * U) * size[:, c:c + 1]).all())
+        terms = d[:, c:c + 1] * hd * r
+        assert bool(((dg[c::2].double() - terms.sum(0)).abs() <= (LONG_SUM / 2 + 10 * U) * terms.abs().sum(0)).all())
