@@ -602,11 +602,14 @@ __global__ void __launch_bounds__(1024) dgamma_kernel(const float* partial, int 
 }
 
 // Rows of any length: read twice, dgamma's sums kept in the block's own row
-// of the partials.
-template <class T>
+// of the partials.  Rows below eight elements (NARROW) come by the million: a
+// thread keeps its one column's sum in 64 bits and writes it at the end (as a
+// chain in fp32 it was 1.7e-4 off over 2^22 rows of one value).
+template <class T, bool NARROW>
 __global__ void __launch_bounds__(1024) norm_bwd_long_kernel(BwdArgs a) {
   typedef typename T::storage S;
   __shared__ Sum2 buf[2][1][17];
+  double own = 0.0;
   int flip = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
     const S *dy = (const S*)a.dy + row * a.lddy, *hp = (const S*)a.h + row * a.ldh;
@@ -628,7 +631,7 @@ __global__ void __launch_bounds__(1024) norm_bwd_long_kernel(BwdArgs a) {
     }
     const Sum2 v = row_reduce<1024, 1>(Sum2{(float)sum_a, (float)sum_b}, buf, flip);
     const float rstd = row_rstd(v.a, (float)a.cols, a.eps), k = rstd * v.b / (float)a.cols;
-    float* sums = a.partial ? a.partial + (int64_t)blockIdx.x * a.cols : nullptr;
+    float* sums = a.partial && !NARROW ? a.partial + (int64_t)blockIdx.x * a.cols : nullptr;
     const bool first = row == (int64_t)blockIdx.x;
     for (int c0 = threadIdx.x; c0 < a.cols; c0 += LONG_U * 1024) {
       h.load(hp, c0, a.cols);
@@ -644,10 +647,12 @@ __global__ void __launch_bounds__(1024) norm_bwd_long_kernel(BwdArgs a) {
         float o = rstd * ((a.gamma ? d.v[u] * g.v[u] : d.v[u]) - xh * k);
         if (a.dres) o += r.v[u];
         if (sums) sums[c] = first ? d.v[u] * xh : fmaf(d.v[u], xh, p.v[u]);
+        if (NARROW) own += (double)d.v[u] * (double)xh;  // (one column a thread)
         if (a.dx) ((S*)a.dx + row * a.lddx)[c] = from_f<T>(o);
       }
     }
   }
+  if (NARROW && a.partial && (int)threadIdx.x < a.cols) a.partial[(int64_t)blockIdx.x * a.cols + threadIdx.x] = (float)own;
 }
 
 // Threads per row of the backward pass by the row's chunks; 0: the long-row kernel.
@@ -675,8 +680,10 @@ void launch_bwd(const BwdArgs& a, int64_t blocks, hipStream_t st) {
 template <class T>
 mdnn_status_t run_bwd(const BwdArgs& a, hipStream_t st) {
   const int64_t nch = ceil_div(a.cols, 8), blocks = bwd_blocks(a.rows, a.cols);
-  if (bwd_tpr(a.cols) == 0)
-    hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3((unsigned)blocks), dim3(1024), 0, st, a);
+  if (a.cols < 8)
+    hipLaunchKernelGGL((norm_bwd_long_kernel<T, true>), dim3((unsigned)blocks), dim3(1024), 0, st, a);
+  else if (bwd_tpr(a.cols) == 0)
+    hipLaunchKernelGGL((norm_bwd_long_kernel<T, false>), dim3((unsigned)blocks), dim3(1024), 0, st, a);
   else if (nch <= 16)
     launch_bwd<T, 16, 1>(a, blocks, st);
   else if (nch <= 32)

@@ -412,3 +412,21 @@ def test_long_rows_of_one_magnitude(mdnn, value):
         assert bool(((dx[:, c::2].double() - want).abs() <= (2 * LONG_SUM + 13 * U) * size[:, c:c + 1]).all())
         terms = d[:, c:c + 1] * hd * r
         assert bool(((dg[c::2].double() - terms.sum(0)).abs() <= (LONG_SUM / 2 + 10 * U) * terms.abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 22, 1), ((1 << 24) + 3, 4), (1 << 22, 7)])
+def test_gamma_gradient_of_many_narrow_rows(mdnn, rows, cols):
+    """Millions of rows below eight columns, all terms of one sign and size: a column's sum is taken in 64 bits over a
+    block's rows, rounded once, and the blocks' sums are added in chains of at most 8 and 32; each term is a rounded
+    product of dy and h / rms, whose root's error is that of a sum of fewer than eight terms."""
+    import torch
+    h = torch.full((rows, cols), 1.1, device="cuda")
+    dy = torch.full((rows, cols), 0.7, device="cuda")
+    dx, dg = mdnn.rmsnorm_bwd(dy, h, eps=EPS)
+    hd, d = h[0].double(), dy[0].double()
+    r = 1 / torch.sqrt(hd * hd + EPS)
+    want = rows * d * hd * r
+    assert bool(((dg.double() - want).abs() <= (1 + 8 + 32 + 16) * U * want.abs()).all())
+    # the blocks' rows in turn, the last ones included
+    first, *_ = mdnn.rmsnorm_bwd(dy[:5], h[:5], eps=EPS)
+    assert bool((dx == first[0]).all())
