@@ -472,7 +472,8 @@ mdnn_status_t mdnn_quantize_i8_t(int64_t rows, int64_t cols, const void* x, int6
  * A [M][lda >= K] and B [N][ldb >= K] are 8-bit codes (any value -128..127),
  * a_scale fp32 [M], b_scale fp32 [N], bias NULL or fp32 [N], D [M][ldd >= N]
  * of d_type (fp32, fp16 or bf16), computed in fp32 from the exact int32 sum
- * and rounded once.  K <= 131071, so that no sum leaves 32 bits
+ * (converted, times a_scale, then b_scale and bias in one rounding: the same
+ * bits whatever the sizes and strides) and rounded once.  K <= 131071, so that no sum leaves 32 bits
  * (MDNN_ERR_SHAPE above).  Any M, N, K >= 0 (M or N == 0: no-op; K == 0: the
  * sums are 0), any strides and byte addresses of A and B; 16-byte aligned A
  * and B with lda, ldb multiples of 16 are fast, of 128 fastest.  Bytes of A and B past K

@@ -77,13 +77,16 @@ __device__ __forceinline__ Quad<OutT> quad_of(const float (&v)[4]) {
   return q;
 }
 
-// One lane's four consecutive columns n .. n + 3 of row m.
+// One lane's four consecutive columns n .. n + 3 of row m.  The last product and
+// the bias are one rounding by name, not by the compiler's choice, so that every
+// kernel gives the same bits.
 __device__ __forceinline__ void values_i8(const I8Args& g, int4v acc, float sa, const float (&sb)[4],
                                           const float (&bias)[4], float (&v)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    v[e] = (float)acc[e] * sa * sb[e];
-    if (g.bias) v[e] += bias[e];
+    const float p = (float)acc[e] * sa;
+    v[e] = p * sb[e];
+    if (g.bias) v[e] = fmaf(p, sb[e], bias[e]);
     if (g.act == MDNN_ACT_RELU) v[e] = relu_f(v[e]);
   }
 }

@@ -466,3 +466,36 @@ def test_product_rows_copied_to_whole_steps(mdnn, K, out):
     """Copied rows of more than 512 bytes, which the 256 x 256 tiles take."""
     assert mdnn.mdnn_gemm_i8_workspace(4095, 4095, K) == 2 * 4095 * ((K + 127) // 128 * 128)
     _check(mdnn, 4095, 4095, K, out, False, bias=True, relu=True, offset=3, seed=K)
+
+
+@pytest.mark.parametrize("K", [1792, 1791])
+def test_product_bits_are_those_of_the_definition_in_every_kernel(mdnn, K):
+    """The sum's conversion, its product with the row's scale, and the column's scale with the bias in one rounding:
+    the same bits from every tile, few-rows and any-byte kernel and with copied rows."""
+    import torch
+    M, N = 3840, 4099
+    a, av = _codes(M, K, 1, 1792)
+    b, bv = _codes(N, K, 2, 1792)
+    a1, _ = _codes(M, K, 1, 1793, 5)  # the same codes in rows on any byte
+    b1, _ = _codes(N, K, 2, 1793, 3)
+    g = np.random.default_rng(3)
+    sa, sb = np.exp(g.standard_normal(M)).astype(np.float32), np.exp(g.standard_normal(N)).astype(np.float32) / 1000
+    bias = (100 * g.standard_normal(N)).astype(np.float32)
+    acc = torch.from_numpy(av).cuda().double() @ torch.from_numpy(bv).cuda().double().T
+    p = acc.float() * dev(sa, "f32")[:, None]
+    exact = p.double() * dev(sb, "f32").double()  # (48 bits)
+    hi = exact + dev(bias, "f32").double()
+    back = hi - exact
+    lo = (exact - (hi - back)) + (dev(bias, "f32").double() - back)
+    # hi rounds to fp32 as the whole sum does unless it lies on a midpoint that lo moves it off
+    sure = (lo == 0) | ((hi.view(torch.int64) & 0x1fffffff) != 0x10000000)
+    want, plain = hi.float(), exact.float()
+    dsa, dsb, dbias = dev(sa, "f32"), dev(sb, "f32"), dev(bias, "f32")
+    for rows, cols in ((3840, 4099), (1100, 4099), (900, 4099), (1800, 1803), (300, 4099), (100, 4099), (40, 4099),
+                       (17, 500), (16, 4099), (1, 4099), (1000, 20)):
+        for x, y in ((a, b), (a1, b1), (a, b1)):
+            for ws in (None, True):
+                args = (x[:rows], dsa[:rows], y[:cols], dsb[:cols])
+                d = mdnn.gemm_i8(*args, dbias[:cols], workspace=ws)
+                assert bool(((d == want[:rows, :cols]) | ~sure[:rows, :cols]).all()), (rows, cols)
+                assert torch.equal(mdnn.gemm_i8(*args, workspace=ws), plain[:rows, :cols]), (rows, cols)
