@@ -474,8 +474,9 @@ mdnn_status_t mdnn_quantize_i8_t(int64_t rows, int64_t cols, const void* x, int6
  * of d_type (fp32, fp16 or bf16), computed in fp32 from the exact int32 sum
  * (converted, times a_scale, then b_scale and bias in one rounding: the same
  * bits whatever the sizes and strides) and rounded once.  K <= 131071, so that no sum leaves 32 bits
- * (MDNN_ERR_SHAPE above).  Any M, N, K >= 0 (M or N == 0: no-op; K == 0: the
- * sums are 0), any strides and byte addresses of A and B; 16-byte aligned A
+ * (MDNN_ERR_SHAPE above).  M, N, K >= 0 (M or N == 0: no-op; K == 0: the
+ * sums are 0) up to what a launch holds, ceil(M / 64) * ceil(N / 64) <= 2^24 - 2
+ * (MDNN_ERR_SHAPE above), any strides and byte addresses of A and B; 16-byte aligned A
  * and B with lda, ldb multiples of 16 are fast, of 128 fastest.  Bytes of A and B past K
  * in a row are never used.  D must not overlap an input.
  * workspace: NULL, or 16-byte aligned device memory; with at least

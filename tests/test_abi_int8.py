@@ -130,3 +130,10 @@ def test_workspace_sizes(m):
     assert m.mdnn_rmsnorm_bwd_workspace(4, 8) >= 8 * 4
     # the blocks' sums do not grow with the rows without end
     assert m.mdnn_rmsnorm_bwd_workspace(1 << 40, 4096) == m.mdnn_rmsnorm_bwd_workspace(1 << 30, 4096)
+
+
+@pytest.mark.parametrize("M,N", [((1 << 30) - 127, 64), (64, (1 << 30) - 127), (1 << 18, 1 << 18), (1 << 62, 1),
+                                 (1, (1 << 63) - 1)])
+def test_gemm_i8_refuses_more_tiles_than_a_launch_holds(m, M, N):
+    """The documented limit, 2^24 - 2 tiles of 64 x 64: the first sizes above it, and sizes whose count would wrap."""
+    _refuses(m, m.ERR_SHAPE, m.mdnn_gemm_i8, M, N, 4, FAKE, 4, FAKE, FAKE, 4, FAKE, None, 0, FAKE, N, 0)
