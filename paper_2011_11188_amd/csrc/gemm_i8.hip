@@ -27,6 +27,28 @@ template <> struct Mfma<I8> {
   }
 };
 
+// The order of the tiles.  Where D is at least as wide as tall, groups of 8 tile
+// columns: the 32 workgroups of an XCD then hold 8 x 4 tiles, the fewest panels in
+// its L2 (16 columns x 2 rows: 1024 x 1024 x 4096 11.7 us against 9.5, 192 x 4096 x
+// 4096 11.5 and 9.4, 1000 x 1001 x 4001 on any byte 18.7 and 16.0).  Which tiles
+// run at once also decides which pieces of D are written together, and a D of
+// hundreds of MB whose rows are whole multiples of 4 KB is slow to write down its
+// columns: such a D wants wider groups, 16 tile columns from 256 MB on (4096 x
+// 65536 x 1024 fp32 451 us, groups of 8 485; 16384 x 16384 x 2048 fp16 565 and 571,
+// groups of 8 tile rows 619; at 128 MB 8 columns still lead: 8192 x 8192 x 2048 fp16
+// 130 us, 16 133; 4096 x 8192 x 1024 fp32 52 and 54).  Taller ones take groups of 4
+// tile rows on such rows (16384 x 8192 x 4096 420 us, 8 tile rows 476; 32768 x 8192 x
+// 2048 523 and 569) and 8 on others (12000 x 5000 x 3200 176, 4 183) and far above N
+// (65536 x 4096 x 1024 363, 4 379).
+struct I8Order {
+  bool by_cols;
+  uint32_t group;
+};
+I8Order i8_tile_order(int64_t M, int64_t N, int64_t ldd, int64_t elem_bytes) {
+  const bool by_cols = N >= M, pages = ldd * elem_bytes % 4096 == 0, large = M >= ((int64_t)1 << 28) / elem_bytes / N;
+  return {by_cols, by_cols ? (large ? 16u : 8u) : pages && M / 8 < N ? 4u : 8u};
+}
+
 namespace {
 
 constexpr int BKB = 128;           // bytes of k per step
@@ -172,21 +194,6 @@ __device__ __forceinline__ void i8_tile(const I8Args& g, int bm, int bn, int& tm
   const uint32_t size = major - first < g.group ? major - first : g.group, b = in / size, a = first + in - b * size;
   tm = (int)(g.by_cols ? b : a);
   tn = (int)(g.by_cols ? a : b);
-}
-
-// The order of the tiles.  Which tiles run at once also decides which pieces
-// of D are written together, and a D of hundreds of MB whose rows are whole
-// multiples of 4 KB is slow to write down its columns: groups of 16 tile
-// columns where D is at least as wide as tall (16384 x 16384 x 2048 897 -> 578
-// us, 4096 x 65536 x 1024 906 -> 374, 4096 x 16384 x 4096 252 -> 217, against
-// groups of 8 tile rows; other widths and small D alike within 2%); taller ones
-// groups of 4 tile rows on such rows (16384 x 8192 x 4096 476 -> 420 us, 32768 x
-// 8192 x 2048 569 -> 523) and 8 on others (12000 x 5000 x 3200 183 -> 176) and
-// far above N (65536 x 4096 x 1024 379 -> 363).
-void set_order(I8Args& g) {
-  g.by_cols = g.N >= g.M;
-  const bool pages = g.ldd * (int64_t)dtype_size((mdnn_dtype_t)g.d_type) % 4096 == 0;
-  g.group = g.by_cols ? 16 : pages && g.M / 8 < g.N ? 4 : 8;
 }
 
 // ------------------------------------------------- register-staged kernel
@@ -860,7 +867,8 @@ extern "C" mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int
   g.a = A, g.b = B, g.a_scale = a_scale, g.b_scale = b_scale, g.bias = bias, g.d = D;
   g.M = M, g.N = N, g.K = K, g.lda = lda, g.ldb = ldb, g.ldd = ldd, g.act = act;
   g.d_type = d_type, g.pairs = d_type != MDNN_F32;
-  set_order(g);
+  const I8Order order = i8_tile_order(M, N, ldd, (int64_t)dtype_size(d_type));
+  g.by_cols = order.by_cols, g.group = order.group;
   clear_error();
   return run_i8(g, workspace, ws_bytes, as_stream(stream));
 }

@@ -64,3 +64,48 @@ def test_direct_to_lds_convolution_launches_stay_below_2_32_threads(lib):
                 taken += 1
                 assert 512 * max(-(-m // 128) * -(-n // 128), -(-m // 256) * -(-n // 64)) < 2 ** 32, (m, n)
     assert taken > 30 and all(fit(1 << 20, n) for n in (1, 64, 200, 1000))
+
+
+class _I8Order(C.Structure):
+    _fields_ = [("by_cols", C.c_bool), ("group", C.c_uint32)]
+
+
+def _i8_order(lib, M, N, ldd, elem_bytes):
+    f = lib["_ZN4mdnn13i8_tile_orderEllll"]
+    f.argtypes, f.restype = [C.c_int64] * 4, _I8Order
+    return f(M, N, ldd, elem_bytes)
+
+
+def _walk(order, tiles_m, tiles_n):
+    """The tiles (row, column) of consecutive workgroups: groups of `group` tile columns row by row, or of tile rows
+    column by column."""
+    major, minor = (tiles_n, tiles_m) if order.by_cols else (tiles_m, tiles_n)
+    for g in range(0, major, order.group):
+        for b in range(minor):
+            for a in range(g, min(g + order.group, major)):
+                yield (b, a) if order.by_cols else (a, b)
+
+
+@pytest.mark.parametrize("M,N", [(256, 4096), (512, 2048), (1024, 1024), (1024, 2048), (4096, 512)])
+def test_int8_tiles_of_an_xcd_share_their_panels(lib, M, N):
+    """Grids of 64 x 64 tiles of a few to a CU: the 32 workgroups that an XCD starts with read 12 panels of the
+    operands, the fewest that 32 tiles in whole rows of 4 or 8 have (in groups of 16 columns they read 18)."""
+    order = _i8_order(lib, M, N, N, 2)
+    at = list(_walk(order, M // 64, N // 64))
+    assert len(set(at)) == len(at) == (M // 64) * (N // 64)
+    for x in range(0, len(at), 32):
+        rows, cols = {r for r, _ in at[x:x + 32]}, {c for _, c in at[x:x + 32]}
+        assert len(rows) + len(cols) <= 12, (x, rows, cols)
+
+
+def test_int8_tile_order_by_the_size_of_d(lib):
+    """Wide D: 8 tile columns below 256 MB, 16 from there on; tall D: 4 tile rows where its rows are whole pages and
+    it is not far above N, 8 elsewhere."""
+    for es, n in ((2, 1 << 14), (4, 1 << 13)):
+        at = (1 << 28) // es // n
+        assert (_i8_order(lib, at - 1, n, n, es).by_cols, _i8_order(lib, at - 1, n, n, es).group) == (True, 8)
+        assert (_i8_order(lib, at, n, n, es).by_cols, _i8_order(lib, at, n, n, es).group) == (True, 16)
+    for args, group in (((16384, 8192, 8192, 2), 4), ((65536, 4096, 4096, 2), 8), ((12000, 5000, 5000, 2), 8),
+                        ((20, 10, 10, 4), 8)):
+        o = _i8_order(lib, *args)
+        assert (o.by_cols, o.group) == (False, group)
