@@ -49,6 +49,41 @@ I8Order i8_tile_order(int64_t M, int64_t N, int64_t ldd, int64_t elem_bytes) {
   return {by_cols, by_cols ? (large ? 16u : 8u) : pages && M / 8 < N ? 4u : 8u};
 }
 
+// The tile of rows on 16 bytes.
+//   64 x 64 up to 128 tiles of 128 x 128 (1024 x 2048 x 4096 15.2 us, 128 x 128 18.6),
+//     up to 160 with few steps (1500 x 1500 x 512 6.8 us, 128 x 128 7.2; x 2048 both
+//     11.5).
+//   256 x 256 from more than 256 tiles of 256 x 128 on (4096^3 57 us, 256 x 128 68),
+//     unless their padding takes the gain or steps are at most four.
+//   128 x 128 of eight waves, two workgroups to a CU, store one tile while they
+//     multiply the next.  They take the place of 256 x 256 where steps are few
+//     (5184 x 4544 x 512 27 us, 256 x 256 33) and where its last round leaves many CUs
+//     idle: a round of 256 x 256 has the work of four of theirs and took the time of
+//     2.6 to 3.2 above K = 1024 (five rounds for two: 4100 x 4100 x 4096 92 us, 256 x
+//     256 96; six for two: 5184 x 4544 x 4096 106 and 100, x 1280 46.6 and 47.9; seven
+//     for two: 5000 x 5500 x 2048 67 and 61), of 2.8 to 3.8 below (six for two: 5184 x
+//     4544 x 640 30.5 and 34.6, x 1024 both 41.5; seven for two: 5000 x 5500 x 640 33.0
+//     and 34.5, x 1024 42.3 and 41.9; eleven for three: 6500 x 6500 x 640 61 and 54).
+//   256 x 128 while they fill one workgroup per CU and above K = 1536 (2048 x 4096 x 4096
+//     34.8 us, 128 x 128 of eight waves 36.8; at 1536 seven shapes of 160 to 470 tiles
+//     were 1 to 14% slower, at 1800 7% faster to 4% slower but for 30000 x 300, 40.6
+//     and 36.1).
+//   128 x 128 of four waves with three stages, one workgroup to a CU, up to 256 tiles
+//     above K = 1536 (2048 x 2048 x 4096 21.9 us, eight waves 24.3; at 1536 12.5 and
+//     11.2, at 1800 16.7 and 16.0, 1100 x 3000 x 1800 15.6 and 16.4); more than one
+//     tile to a CU goes to eight waves (1100 x 4096 x 4096 36.9 us, eight waves 28.2).
+enum I8Tile { I8_64, I8_128, I8_128X8, I8_256X128, I8_256 };
+I8Tile i8_tile_choice(int64_t M, int64_t N, int64_t K) {
+  auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(M, bm) * ceil_div(N, bn); };
+  auto rounds = [](int64_t n) { return ceil_div(n, (int64_t)256); };
+  const int64_t t256 = tiles(256, 256), t = tiles(256, 128), t128 = tiles(128, 128);
+  const bool padded = 5 * t256 > 3 * t;
+  if (t128 <= (K <= 2048 ? 160 : 128)) return I8_64;
+  if (t > 256 && !padded && K > 512 && 3 * rounds(t128) >= (K > 1024 ? 9 : 10) * rounds(t256)) return I8_256;
+  if (t > 160 && (t <= 256 || padded) && K > 1536) return I8_256X128;
+  return t128 <= 256 && K > 1536 ? I8_128 : I8_128X8;
+}
+
 namespace {
 
 constexpr int BKB = 128;           // bytes of k per step
@@ -804,35 +839,13 @@ mdnn_status_t run_i8(I8Args g, void* ws, size_t ws_bytes, hipStream_t st) {
       launch_any<TileI64x8, 2>(g, st);
     return check_launch("gemm_i8_any_kernel");
   }
-  // 256 x 256 tiles from more than 256 tiles of 256 x 128 on (4096^3 57 us,
-  // 256 x 128 tiles 68), unless their padding takes the gain; 256 x 128 while
-  // they fill one workgroup per CU (2048 x 4096 x 4096 35 us; 256 x 256 48, 128 x
-  // 128 37); below 160 of them 128 x 128, and 64 x 64 up to 128 of those (1024 x
-  // 2048 x 4096 15.8 us, 128 x 128 19.1; three stages, 15.7 us for 512 x 4096 x
-  // 4096, two 18.3), up to 160 with few steps (1500 x 1500 x 1024 8.1 us, 128 x
-  // 128 8.8).
-  // 128 x 128 tiles of eight waves, two workgroups to a CU, store one tile while
-  // they multiply the next.  They take the place of the large tiles where steps
-  // are few (9783 x 1984 x 256 17.8 us, 256 x 256 26.0; 2048 x 4096 x 512 10.7,
-  // 256 x 128 11.4), and where the last round of 256 x 256 tiles leaves many CUs
-  // idle, which costs those a quarter more work a CU (4100 x 4100 x 4096 89.7 us,
-  // 256 x 256 95.8; 5184 x 4544 x 4096 107 and 101); of four waves with three
-  // stages where more than one tile falls to a CU (1100 x 4096 x 4096 28.2 us,
-  // three stages 36.9) or steps are few (2048 x 2048 x 1024 9.2 and 10.6; 4096
-  // deep 25.7 and 22.4).
-  const int64_t t256 = tiles(256, 256), t = tiles(256, 128), t128 = tiles(128, 128);
-  auto rounds = [](int64_t n) { return ceil_div(n, (int64_t)256); };
-  const bool padded = 5 * t256 > 3 * t;
-  if (t128 <= (g.K <= 2048 ? 160 : 128))
-    launch_i8<TileI64, 3>(g, st);
-  else if (t > 256 && !padded && g.K > 512 && 80 * rounds(t256) <= (g.K > 1024 ? 27 : 24) * rounds(t128))
-    launch_i8<lds::Tile256, 2>(g, st);
-  else if (t > 160 && (t <= 256 || padded) && g.K > 1024)
-    launch_i8<TileI256x128, 3>(g, st);
-  else if (t128 <= 256 && g.K > 1536)
-    launch_i8<TileI128, 3>(g, st);
-  else
-    launch_i8<TileI128x8, 2>(g, st);
+  switch (i8_tile_choice(g.M, g.N, g.K)) {
+    case I8_64: launch_i8<TileI64, 3>(g, st); break;
+    case I8_128: launch_i8<TileI128, 3>(g, st); break;
+    case I8_128X8: launch_i8<TileI128x8, 2>(g, st); break;
+    case I8_256X128: launch_i8<TileI256x128, 3>(g, st); break;
+    case I8_256: launch_i8<lds::Tile256, 2>(g, st); break;
+  }
   return check_launch("gemm_i8_kernel");
 }
 

@@ -109,3 +109,45 @@ def test_int8_tile_order_by_the_size_of_d(lib):
                         ((20, 10, 10, 4), 8)):
         o = _i8_order(lib, *args)
         assert (o.by_cols, o.group) == (False, group)
+
+
+I8_64, I8_128, I8_128X8, I8_256X128, I8_256 = range(5)
+
+
+def _i8_choice(lib, *size):
+    f = lib["_ZN4mdnn14i8_tile_choiceElll"]
+    f.argtypes, f.restype = [C.c_int64] * 3, C.c_int
+    return f(*size)
+
+
+@pytest.mark.parametrize("size,tile", [
+    # 128 tiles of 128 x 128 and one more; 160 of them, one more, and one step more
+    ((1024, 2048, 4096), I8_64), ((1152, 2048, 4096), I8_128), ((1280, 2048, 2048), I8_64), ((1280, 2048, 2049), I8_128),
+    ((1408, 2048, 1024), I8_128X8),
+    # 256 of them, and one more
+    ((2048, 2048, 1536), I8_128X8), ((2048, 2048, 1537), I8_128), ((2049, 2048, 1537), I8_128X8),
+    # 160 tiles of 256 x 128 and more, 256 and more
+    ((1024, 5120, 4096), I8_128X8), ((1100, 4099, 1536), I8_128X8), ((1100, 4099, 1537), I8_256X128),
+    ((2048, 4096, 4096), I8_256X128), ((2500, 2500, 1152), I8_128X8), ((30000, 300, 1537), I8_256X128),
+    # whole rounds of 256 x 256 tiles; four steps and one byte more
+    ((4096, 4096, 512), I8_128X8), ((4096, 4096, 513), I8_256), ((16384, 8192, 8192), I8_256),
+    # five, six and seven rounds of 128 x 128 for two of 256 x 256, below and above K = 1024
+    ((4100, 4100, 4096), I8_128X8), ((5184, 4544, 1024), I8_128X8), ((5184, 4544, 1025), I8_256),
+    ((5000, 5500, 640), I8_256)])
+def test_int8_tile_choice(lib, size, tile):
+    """Both sides of the rule's lines."""
+    assert _i8_choice(lib, *size) == tile
+
+
+def test_int8_tests_reach_every_tile(lib):
+    """The sizes of the product's GPU tests run every tile of rows on 16 bytes with whole last steps and with partial
+    ones (two different kernels each)."""
+    from tests import test_gpu_int8 as g
+
+    def sizes(test):
+        return [size[:3] for mark in test.pytestmark if mark.args[0] == "M,N,K" for size in mark.args[1]]
+
+    assert {_i8_choice(lib, *s) for s in sizes(g.test_product_whole_steps)} == set(range(5))
+    assert all(s[2] % 128 == 0 for s in sizes(g.test_product_whole_steps))
+    partial = [s for s in sizes(g.test_product_each_tile) if s[2] % 128]
+    assert {_i8_choice(lib, *s) for s in partial} == set(range(5))
