@@ -233,11 +233,14 @@ __device__ __forceinline__ void i8_tile(const I8Args& g, int bm, int bn, int& tm
 
 // ------------------------------------------------- register-staged kernel
 // Rows that start on any byte, any K: chunks of 16 bytes are read at any
-// address into one of NR register sets (NR steps in flight) and written to the
-// swizzled LDS tiles (two stages, one barrier a step).  A chunk past the row's
-// end is read from its last 16 bytes and shifted; k past K is zero.  1000 x 777
-// x 1531 9.0 us (the latency of 12 steps on one tile per CU), 4095^3 109 us.
-// Four and six sets in flight are not faster than two.
+// address into one of NR register sets and written to the swizzled LDS tiles (two
+// stages, one barrier a step).  A chunk past the row's end is read from its last
+// 16 bytes and shifted; k past K is zero.  The last step's loads meet the whole
+// steps' at a join past which the compiler does not count them: the first set's
+// LDS writes wait for every load, the second set's too, so a round trip to memory
+// is paid every NR steps and not hidden.  1000 x 777 x 1531 9.0 us (waves wait 68%
+// of their cycles; matrix cores busy 6%, LDS 15%), 7 with rows on 16 bytes; 4095^3
+// 109-114 us.
 
 typedef uint32_t u4v_a1 __attribute__((ext_vector_type(4), aligned(1)));
 
@@ -413,9 +416,13 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a) {
 // straight from memory to LDS.  A K that is no multiple of the step reads
 // through a range-checked buffer, whole 16-byte chunks past K as zeros; its
 // last K % 16 bytes are one more fragment step from registers.  Large products
-// are bound by the matrix cores at the clock the power limit leaves (4096^3
-// 55-57 us by the data, 16384 x 8192 x 8192 810-870, 2.5-2.7 POPS), 64 x 64 tiles by
-// LDS traffic (256 x 4096 x 4096 9.8 us).
+// keep the matrix cores busy in 56-69% of the cycles: 4096^3 55 us at the 2.1 GHz that
+// half-zero codes leave under the power limit, 58 at the 1.7 of normal ones, so
+// what fills the rest does not follow the clock (tiles on their way from beyond L2:
+// waves are at waits 30% of their cycles); 16384 x 8192 x 8192 820-900 us at 1.7 GHz,
+// 2.4-2.7 POPS.  LDS reads take 26% of the cycles.  64 x 64 tiles wait for their
+// loads: 256 x 4096 x 4096, one tile a CU, 10.1 us, 730 cycles a step against 128 of
+// matrix work and as many of LDS reads; an L2 read takes 460.
 struct I8Operand {
   const int8_t* p;
   int64_t ld, MN, K;

@@ -268,13 +268,11 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_kernel(RowArgs a) {
           c.set(h[i]);
           c.store((S*)a.h + row * a.ldh + pos[i].start, pos[i].lo);
         }
-        if (a.gamma) {
+        if (MODE == NORM_I8 && a.gamma) {
           Chunk<F32> g;
           g.load(a.gamma + pos[i].start);
-          if (MODE == NORM_I8) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[i][e] = mul_rn(h[i][e], g.get(e));
-          }
+          for (int e = 0; e < 8; ++e) h[i][e] = mul_rn(h[i][e], g.get(e));
         }
       }
       if (MODE != NORM) {
