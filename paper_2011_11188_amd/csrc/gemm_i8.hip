@@ -54,16 +54,22 @@ I8Order i8_tile_order(int64_t M, int64_t N, int64_t ldd, int64_t elem_bytes) {
 //     up to 160 with few steps (1500 x 1500 x 512 6.8 us, 128 x 128 7.2; x 2048 both
 //     11.5).
 //   256 x 256 from more than 256 tiles of 256 x 128 on (4096^3 57 us, 256 x 128 68),
-//     unless their padding takes the gain or steps are at most four.
+//     unless their padding takes the gain.
 //   128 x 128 of eight waves, two workgroups to a CU, store one tile while they
-//     multiply the next.  They take the place of 256 x 256 where steps are few
-//     (5184 x 4544 x 512 27 us, 256 x 256 33) and where its last round leaves many CUs
-//     idle: a round of 256 x 256 has the work of four of theirs and took the time of
+//     multiply the next.  They take the place of 256 x 256 where its last round leaves
+//     many CUs idle: a round of 256 x 256 has the work of four of theirs and took the time of
 //     2.6 to 3.2 above K = 1024 (five rounds for two: 4100 x 4100 x 4096 92 us, 256 x
 //     256 96; six for two: 5184 x 4544 x 4096 106 and 100, x 1280 46.6 and 47.9; seven
 //     for two: 5000 x 5500 x 2048 67 and 61), of 2.8 to 3.8 below (six for two: 5184 x
 //     4544 x 640 30.5 and 34.6, x 1024 both 41.5; seven for two: 5000 x 5500 x 640 33.0
-//     and 34.5, x 1024 42.3 and 41.9; eleven for three: 6500 x 6500 x 640 61 and 54).
+//     and 34.5, x 1024 42.3 and 41.9; eleven for three: 6500 x 6500 x 640 61 and 54),
+//     and up to four steps of nearly all four (11 for 3 and less: 6144 x 4096 x 256 21
+//     and 24, 9783 x 1984 x 256 18 and 26, 14000 x 5000 x 320 66 and 72; 41 for 11: 13000 x
+//     13000 x 320 185 and 152; 4 for 1: 16384 x 16384 x 128 189 and 171, 8192 x 8192 x 512
+//     65 and 62, 20000 x 4000 x 128 49 and 51), except where large tiles store slowly:
+//     bf16, for its conversion (8192 x 8192 x 512 69 and 75, 32768 x 4096 x 128 97 and
+//     106; but 13000 x 13000 x 320 195 and 183), and tall fp32 D in rows of whole pages
+//     (32768 x 4096 x 128 117 and 148, 10240 x 8192 x 128 74 and 91; but x 512 110 and 105).
 //   256 x 128 while they fill one workgroup per CU and above K = 1536 (2048 x 4096 x 4096
 //     34.8 us, 128 x 128 of eight waves 36.8; at 1536 seven shapes of 160 to 470 tiles
 //     were 1 to 14% slower, at 1800 7% faster to 4% slower but for 30000 x 300, 40.6
@@ -73,13 +79,14 @@ I8Order i8_tile_order(int64_t M, int64_t N, int64_t ldd, int64_t elem_bytes) {
 //     11.2, at 1800 16.7 and 16.0, 1100 x 3000 x 1800 15.6 and 16.4); more than one
 //     tile to a CU goes to eight waves (1100 x 4096 x 4096 36.9 us, eight waves 28.2).
 enum I8Tile { I8_64, I8_128, I8_128X8, I8_256X128, I8_256 };
-I8Tile i8_tile_choice(int64_t M, int64_t N, int64_t K) {
+I8Tile i8_tile_choice(int64_t M, int64_t N, int64_t K, int64_t ldd, mdnn_dtype_t d_type) {
   auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(M, bm) * ceil_div(N, bn); };
   auto rounds = [](int64_t n) { return ceil_div(n, (int64_t)256); };
   const int64_t t256 = tiles(256, 256), t = tiles(256, 128), t128 = tiles(128, 128);
-  const bool padded = 5 * t256 > 3 * t;
+  const bool padded = 5 * t256 > 3 * t, slow = d_type == MDNN_BF16 || (d_type == MDNN_F32 && N < M && ldd % 1024 == 0);
+  const int line = K > 1024 ? 30 : K > 512 ? 33 : slow ? 99 : 37;  // tenths of a round of 128 x 128
   if (t128 <= (K <= 2048 ? 160 : 128)) return I8_64;
-  if (t > 256 && !padded && K > 512 && 3 * rounds(t128) >= (K > 1024 ? 9 : 10) * rounds(t256)) return I8_256;
+  if (t > 256 && !padded && 10 * rounds(t128) >= line * rounds(t256)) return I8_256;
   if (t > 160 && (t <= 256 || padded) && K > 1536) return I8_256X128;
   return t128 <= 256 && K > 1536 ? I8_128 : I8_128X8;
 }
@@ -846,7 +853,7 @@ mdnn_status_t run_i8(I8Args g, void* ws, size_t ws_bytes, hipStream_t st) {
       launch_any<TileI64x8, 2>(g, st);
     return check_launch("gemm_i8_any_kernel");
   }
-  switch (i8_tile_choice(g.M, g.N, g.K)) {
+  switch (i8_tile_choice(g.M, g.N, g.K, g.ldd, (mdnn_dtype_t)g.d_type)) {
     case I8_64: launch_i8<TileI64, 3>(g, st); break;
     case I8_128: launch_i8<TileI128, 3>(g, st); break;
     case I8_128X8: launch_i8<TileI128x8, 2>(g, st); break;

@@ -114,10 +114,13 @@ def test_int8_tile_order_by_the_size_of_d(lib):
 I8_64, I8_128, I8_128X8, I8_256X128, I8_256 = range(5)
 
 
-def _i8_choice(lib, *size):
-    f = lib["_ZN4mdnn14i8_tile_choiceElll"]
-    f.argtypes, f.restype = [C.c_int64] * 3, C.c_int
-    return f(*size)
+F32, F16, BF16 = range(3)
+
+
+def _i8_choice(lib, M, N, K, d_type=F16):
+    f = lib["_ZN4mdnn14i8_tile_choiceEllll12mdnn_dtype_t"]
+    f.argtypes, f.restype = [C.c_int64] * 4 + [C.c_int], C.c_int
+    return f(M, N, K, N, d_type)
 
 
 @pytest.mark.parametrize("size,tile", [
@@ -129,8 +132,13 @@ def _i8_choice(lib, *size):
     # 160 tiles of 256 x 128 and more, 256 and more
     ((1024, 5120, 4096), I8_128X8), ((1100, 4099, 1536), I8_128X8), ((1100, 4099, 1537), I8_256X128),
     ((2048, 4096, 4096), I8_256X128), ((2500, 2500, 1152), I8_128X8), ((30000, 300, 1537), I8_256X128),
-    # whole rounds of 256 x 256 tiles; four steps and one byte more
-    ((4096, 4096, 512), I8_128X8), ((4096, 4096, 513), I8_256), ((16384, 8192, 8192), I8_256),
+    # whole rounds of 256 x 256 tiles, and nearly whole ones; four steps and one byte more
+    ((4096, 4096, 128), I8_256), ((16384, 8192, 8192), I8_256), ((13000, 13000, 320), I8_256),
+    ((9600, 13952, 512), I8_128X8), ((9600, 13952, 513), I8_256), ((14000, 5000, 512), I8_128X8),
+    # bf16, and tall fp32 D in rows of whole pages, up to four steps; wide, other rows, more steps
+    ((4096, 4096, 512, BF16), I8_128X8), ((4096, 4096, 513, BF16), I8_256),
+    ((10240, 8192, 512, F32), I8_128X8), ((10240, 8192, 513, F32), I8_256), ((8192, 8192, 512, F32), I8_256),
+    ((14176, 6848, 128, F32), I8_256), ((10240, 8192, 512, F16), I8_256),
     # five, six and seven rounds of 128 x 128 for two of 256 x 256, below and above K = 1024
     ((4100, 4100, 4096), I8_128X8), ((5184, 4544, 1024), I8_128X8), ((5184, 4544, 1025), I8_256),
     ((5000, 5500, 640), I8_256)])
