@@ -33,20 +33,22 @@ template <> struct Mfma<I8> {
 // 4096 11.5 and 9.4, 1000 x 1001 x 4001 on any byte 18.7 and 16.0).  Which tiles
 // run at once also decides which pieces of D are written together, and a D of
 // hundreds of MB whose rows are whole multiples of 4 KB is slow to write down its
-// columns: such a D wants wider groups, 16 tile columns from 256 MB on (4096 x
+// columns: where the writes count, 16 tile columns, that is from 256 MB on (4096 x
 // 65536 x 1024 fp32 451 us, groups of 8 485; 16384 x 16384 x 2048 fp16 565 and 571,
 // groups of 8 tile rows 619; at 128 MB 8 columns still lead: 8192 x 8192 x 2048 fp16
-// 130 us, 16 133; 4096 x 8192 x 1024 fp32 52 and 54).  Taller ones take groups of 4
-// tile rows on such rows (16384 x 8192 x 4096 420 us, 8 tile rows 476; 32768 x 8192 x
-// 2048 523 and 569) and 8 on others (12000 x 5000 x 3200 176, 4 183) and far above N
-// (65536 x 4096 x 1024 363, 4 379).
+// 130 us, 16 133; 4096 x 8192 x 1024 fp32 52 and 54) and up to four steps (8192 x 8192 x
+// 128 bf16 48.7 and 50.7, 4096 x 8192 x 320 fp32 35.3 and 36.5).  Taller ones take
+// groups of 4 tile rows on such rows (16384 x 8192 x 4096 420 us, 8 tile rows 476;
+// 32768 x 8192 x 2048 523 and 569) and 8 on others (12000 x 5000 x 3200 176, 4 183) and
+// far above N (65536 x 4096 x 1024 363, 4 379).
 struct I8Order {
   bool by_cols;
   uint32_t group;
 };
-I8Order i8_tile_order(int64_t M, int64_t N, int64_t ldd, int64_t elem_bytes) {
-  const bool by_cols = N >= M, pages = ldd * elem_bytes % 4096 == 0, large = M >= ((int64_t)1 << 28) / elem_bytes / N;
-  return {by_cols, by_cols ? (large ? 16u : 8u) : pages && M / 8 < N ? 4u : 8u};
+I8Order i8_tile_order(int64_t M, int64_t N, int64_t K, int64_t ldd, int64_t elem_bytes) {
+  const bool by_cols = N >= M, pages = ldd * elem_bytes % 4096 == 0;
+  const bool writes = K <= 512 || M >= ((int64_t)1 << 28) / elem_bytes / N;
+  return {by_cols, by_cols ? (writes ? 16u : 8u) : pages && M / 8 < N ? 4u : 8u};
 }
 
 // The tile of rows on 16 bytes.
@@ -894,7 +896,7 @@ extern "C" mdnn_status_t mdnn_gemm_i8(int64_t M, int64_t N, int64_t K, const int
   g.a = A, g.b = B, g.a_scale = a_scale, g.b_scale = b_scale, g.bias = bias, g.d = D;
   g.M = M, g.N = N, g.K = K, g.lda = lda, g.ldb = ldb, g.ldd = ldd, g.act = act;
   g.d_type = d_type, g.pairs = d_type != MDNN_F32;
-  const I8Order order = i8_tile_order(M, N, ldd, (int64_t)dtype_size(d_type));
+  const I8Order order = i8_tile_order(M, N, K, ldd, (int64_t)dtype_size(d_type));
   g.by_cols = order.by_cols, g.group = order.group;
   clear_error();
   return run_i8(g, workspace, ws_bytes, as_stream(stream));

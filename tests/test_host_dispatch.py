@@ -70,10 +70,10 @@ class _I8Order(C.Structure):
     _fields_ = [("by_cols", C.c_bool), ("group", C.c_uint32)]
 
 
-def _i8_order(lib, M, N, ldd, elem_bytes):
-    f = lib["_ZN4mdnn13i8_tile_orderEllll"]
-    f.argtypes, f.restype = [C.c_int64] * 4, _I8Order
-    return f(M, N, ldd, elem_bytes)
+def _i8_order(lib, M, N, ldd, elem_bytes, K=4096):
+    f = lib["_ZN4mdnn13i8_tile_orderElllll"]
+    f.argtypes, f.restype = [C.c_int64] * 5, _I8Order
+    return f(M, N, K, ldd, elem_bytes)
 
 
 def _walk(order, tiles_m, tiles_n):
@@ -99,12 +99,13 @@ def test_int8_tiles_of_an_xcd_share_their_panels(lib, M, N):
 
 
 def test_int8_tile_order_by_the_size_of_d(lib):
-    """Wide D: 8 tile columns below 256 MB, 16 from there on; tall D: 4 tile rows where its rows are whole pages and
+    """Wide D: 8 tile columns below 256 MB, 16 from there on and up to four steps; tall D: 4 tile rows where its rows are whole pages and
     it is not far above N, 8 elsewhere."""
     for es, n in ((2, 1 << 14), (4, 1 << 13)):
         at = (1 << 28) // es // n
         assert (_i8_order(lib, at - 1, n, n, es).by_cols, _i8_order(lib, at - 1, n, n, es).group) == (True, 8)
         assert (_i8_order(lib, at, n, n, es).by_cols, _i8_order(lib, at, n, n, es).group) == (True, 16)
+        assert (_i8_order(lib, at - 1, n, n, es, 512).group, _i8_order(lib, at - 1, n, n, es, 513).group) == (16, 8)
     for args, group in (((16384, 8192, 8192, 2), 4), ((65536, 4096, 4096, 2), 8), ((12000, 5000, 5000, 2), 8),
                         ((20, 10, 10, 4), 8)):
         o = _i8_order(lib, *args)
