@@ -425,11 +425,11 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a) {
 // straight from memory to LDS.  A K that is no multiple of the step reads
 // through a range-checked buffer, whole 16-byte chunks past K as zeros; its
 // last K % 16 bytes are one more fragment step from registers.  Large products
-// keep the matrix cores busy in 56-69% of the cycles: 4096^3 55 us at the 2.1 GHz that
+// keep the matrix cores busy in 56-72% of the cycles: 4096^3 55 us at the 2.1 GHz that
 // half-zero codes leave under the power limit, 58 at the 1.7 of normal ones, so
 // what fills the rest does not follow the clock (tiles on their way from beyond L2:
-// waves are at waits 30% of their cycles); 16384 x 8192 x 8192 820-900 us at 1.7 GHz,
-// 2.4-2.7 POPS.  LDS reads take 26% of the cycles.  64 x 64 tiles wait for their
+// waves are at waits 30% of their cycles); 16384 x 8192 x 8192 820-965 us at 1.5-1.7
+// GHz, 2.3-2.7 POPS.  LDS reads take 26% of the cycles.  64 x 64 tiles wait for their
 // loads: 256 x 4096 x 4096, one tile a CU, 10.1 us, 730 cycles a step against 128 of
 // matrix work and as many of LDS reads; an L2 read takes 460.
 struct I8Operand {
