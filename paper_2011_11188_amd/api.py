@@ -10,9 +10,11 @@ Ordering the two streams is the caller's, as with torch's own operations.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import inspect
 from typing import Optional, Sequence
 
-from . import (ACT_NONE, BF16, F16, F32, LAYER_CONV, LAYER_FC, LAYER_MAXPOOL2, LOSS_MSE, LOSS_XENT,
+from . import (_s, ACT_NONE, BF16, F16, F32, LAYER_CONV, LAYER_FC, LAYER_MAXPOOL2, LOSS_MSE, LOSS_XENT,
                NN, NT, TN, ConvShape, LayerDesc, Scaler, TrainCfg, dtype_of, mdnn_conv2d_bwd_data,
                mdnn_conv2d_bwd_filter, mdnn_conv2d_bwd_filter_workspace, mdnn_conv2d_fwd,
                mdnn_gemm_mixed, mdnn_gemm_mixed_ws, mdnn_gemm_workspace, mdnn_gemm_split3,
@@ -34,38 +36,34 @@ def torch_dtype(code: int):
     return {F32: torch.float32, F16: torch.float16, BF16: torch.bfloat16}[code]
 
 
-def _torch_stream(stream):
-    """torch's object of a call's stream.  The handle 0 is the default stream
-    (an ExternalStream of 0 would be one of torch's pool of side streams)."""
-    import torch
-    if not isinstance(stream, int):
-        return stream
-    return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+def _on_its_stream(wrapper):
+    """A wrapper whose call on a given stream is made with that stream current:
+    what it allocates is that stream's memory, which no pending work of another
+    one still uses.  Its results are kept, besides, until the work that the
+    caller's own stream has at their release is done."""
+    names = list(inspect.signature(wrapper).parameters)
+    at = names.index("stream")
+
+    @functools.wraps(wrapper)
+    def call(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None or (stream if isinstance(stream, int) else stream.cuda_stream) == _s(None):
+            return wrapper(*args, **kw)
+        import torch
+        own = torch.cuda.current_stream()
+        if isinstance(stream, int):  # (0 is the default stream; an ExternalStream of 0 would be one of torch's pool)
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+        with torch.cuda.stream(stream):
+            results = wrapper(*args, **kw)
+        for t in results if isinstance(results, tuple) else (results,):
+            if t is not None:
+                t.record_stream(own)
+        return results
+
+    return call
 
 
-def _scratch(n: int, device, stream):
-    """A workspace of n bytes that belongs to the call's stream: released when
-    the wrapper returns, it goes to later work of that stream only."""
-    import torch
-    if stream is None:
-        return torch.empty((n,), dtype=torch.uint8, device=device)
-    with torch.cuda.stream(_torch_stream(stream)):
-        return torch.empty((n,), dtype=torch.uint8, device=device)
-
-
-def _empty(shape, dtype, device, stream):
-    """Memory for a result of a call on `stream`: that stream's own, which no
-    pending work of another one still uses, and not handed out again before
-    the work that the caller's current stream has by its release is done."""
-    import torch
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(_torch_stream(stream)):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    t.record_stream(torch.cuda.current_stream())
-    return t
-
-
+@_on_its_stream
 def gemm(layout: int, A, B, out_dtype=None, bias=None, act: int = ACT_NONE, mask=None,
          alpha: float = 1.0, beta: float = 0.0, Cm=None, out=None, stream=None, workspace=None,
          nonfinite=None):
@@ -81,7 +79,7 @@ def gemm(layout: int, A, B, out_dtype=None, bias=None, act: int = ACT_NONE, mask
         M, K = A.shape
     N = B.shape[0] if layout == NT else B.shape[1]
     if out is None:
-        out = _empty((M, N), out_dtype or torch.float32, A.device, stream)
+        out = torch.empty((M, N), dtype=out_dtype or torch.float32, device=A.device)
     args = (layout, M, N, K, alpha, A, A.stride(0), B, B.stride(0), dtype_of(A), beta, Cm,
             Cm.stride(0) if Cm is not None else 0, out, out.stride(0), dtype_of(out), bias,
             act, mask, mask.stride(0) if mask is not None else 0)
@@ -90,12 +88,13 @@ def gemm(layout: int, A, B, out_dtype=None, bias=None, act: int = ACT_NONE, mask
         return out
     if workspace is True:
         nb = mdnn_gemm_workspace(dtype_of(A), M, N, K)
-        workspace = _scratch(max(nb, 16), A.device, stream)
+        workspace = torch.empty((max(nb, 16),), dtype=torch.uint8, device=A.device)
     mdnn_gemm_mixed_ws(*args, workspace, workspace.numel() if workspace is not None else 0, stream,
                        nonfinite=nonfinite)
     return out
 
 
+@_on_its_stream
 def split_f16(x, scale: float = 1.0, stream=None, scale_out=None):
     """(hi, lo) fp16 tensors of the two-term split of a 2-D fp32 tensor.
     scale 0 lets the library choose the power of two on the device; it is
@@ -103,14 +102,15 @@ def split_f16(x, scale: float = 1.0, stream=None, scale_out=None):
     not given, returned as the third value)."""
     import torch
     rows, cols = x.shape
-    hi = _empty((rows, cols), torch.float16, x.device, stream)
-    lo = _empty((rows, cols), torch.float16, x.device, stream)
+    hi = torch.empty((rows, cols), dtype=torch.float16, device=x.device)
+    lo = torch.empty((rows, cols), dtype=torch.float16, device=x.device)
     if scale == 0.0 and scale_out is None:
-        scale_out = _empty((1,), torch.float32, x.device, stream)
+        scale_out = torch.empty((1,), dtype=torch.float32, device=x.device)
     mdnn_split_f16(rows, cols, x, x.stride(0), scale, scale_out, hi, cols, lo, cols, stream)
     return (hi, lo, scale_out) if scale == 0.0 else (hi, lo)
 
 
+@_on_its_stream
 def gemm_split3(layout: int, A, B, a_scale: float = 1.0, b_scale: float = 1.0, alpha: float = 1.0,
                 beta: float = 0.0, Cm=None, out=None, stream=None):
     """fp32 D = alpha op(A) op(B) + beta C through three fp16 MFMA products
@@ -122,9 +122,9 @@ def gemm_split3(layout: int, A, B, a_scale: float = 1.0, b_scale: float = 1.0, a
         M, K = A.shape
     N = B.shape[0] if layout == NT else B.shape[1]
     if out is None:
-        out = _empty((M, N), torch.float32, A.device, stream)
+        out = torch.empty((M, N), dtype=torch.float32, device=A.device)
     ws_bytes = mdnn_gemm_split3_workspace(M, N, K)
-    ws = _scratch(max(ws_bytes, 256), A.device, stream)
+    ws = torch.empty((max(ws_bytes, 256),), dtype=torch.uint8, device=A.device)
     mdnn_gemm_split3(layout, M, N, K, alpha, A, A.stride(0), a_scale, B, B.stride(0), b_scale, beta, Cm,
                      Cm.stride(0) if Cm is not None else 0, out, out.stride(0), ws, ws_bytes, stream)
     return out
@@ -135,63 +135,72 @@ def conv_shape(x_shape: Sequence[int], c_out: int, r: int, s: int, pad: int) -> 
     return ConvShape(n, h, w, c, c_out, r, s, pad)
 
 
+@_on_its_stream
 def conv2d_fwd(x, w, pad: int, bias=None, act: int = ACT_NONE, out_dtype=None, stream=None):
+    import torch
     k, r, s, c = w.shape
     sh = conv_shape(x.shape, k, r, s, pad)
     ho, wo = sh.h + 2 * pad - r + 1, sh.w + 2 * pad - s + 1
-    y = _empty((sh.n, ho, wo, k), out_dtype or x.dtype, x.device, stream)
+    y = torch.empty((sh.n, ho, wo, k), dtype=out_dtype or x.dtype, device=x.device)
     mdnn_conv2d_fwd(sh, x, w, dtype_of(x), bias, act, y, dtype_of(y), stream)
     return y
 
 
+@_on_its_stream
 def conv2d_fwd_algo(x, w, pad: int, algo: int, bias=None, act: int = ACT_NONE, out_dtype=None, workspace=None,
                     stream=None):
     """conv2d_fwd through a chosen algorithm (CONV_AUTO: the library's
     per-layer choice for the given workspace; a workspace of the algorithm's
     size is allocated when none is given)."""
+    import torch
     k, r, s, c = w.shape
     sh = conv_shape(x.shape, k, r, s, pad)
     ho, wo = sh.h + 2 * pad - r + 1, sh.w + 2 * pad - s + 1
-    y = _empty((sh.n, ho, wo, k), out_dtype or x.dtype, x.device, stream)
+    y = torch.empty((sh.n, ho, wo, k), dtype=out_dtype or x.dtype, device=x.device)
     io = dtype_of(x)
     if workspace is None:
         need = mdnn_conv2d_fwd_algo_workspace(sh, io, algo)
-        workspace = _scratch(max(need, 256), x.device, stream)
+        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=x.device)
     mdnn_conv2d_fwd_algo(sh, x, w, io, bias, act, y, dtype_of(y), algo, workspace, workspace.numel(), stream)
     return y
 
 
+@_on_its_stream
 def conv2d_fwd_winograd(x, w, pad: int, bias=None, act: int = ACT_NONE, out_dtype=None, workspace=None,
                         stream=None):
     """conv2d_fwd through Winograd F(2x2, 3x3) (3x3 filters, fp16 / bf16)."""
+    import torch
     k, r, s, c = w.shape
     sh = conv_shape(x.shape, k, r, s, pad)
     ho, wo = sh.h + 2 * pad - r + 1, sh.w + 2 * pad - s + 1
-    y = _empty((sh.n, ho, wo, k), out_dtype or x.dtype, x.device, stream)
+    y = torch.empty((sh.n, ho, wo, k), dtype=out_dtype or x.dtype, device=x.device)
     nb = mdnn_conv2d_fwd_winograd_workspace(sh, dtype_of(x))
     if workspace is None:
-        workspace = _scratch(max(nb, 256), x.device, stream)
+        workspace = torch.empty((max(nb, 256),), dtype=torch.uint8, device=x.device)
     mdnn_conv2d_fwd_winograd(sh, x, w, dtype_of(x), bias, act, y, dtype_of(y), workspace, workspace.numel(), stream)
     return y
 
 
+@_on_its_stream
 def conv2d_bwd_data(dy, w, pad: int, h: int, wd: int, mask=None, out_dtype=None, stream=None):
+    import torch
     k, r, s, c = w.shape
     sh = ConvShape(dy.shape[0], h, wd, c, k, r, s, pad)
-    dx = _empty((sh.n, h, wd, c), out_dtype or dy.dtype, dy.device, stream)
+    dx = torch.empty((sh.n, h, wd, c), dtype=out_dtype or dy.dtype, device=dy.device)
     mdnn_conv2d_bwd_data(sh, dy, w, dtype_of(dy), mask, dx, dtype_of(dx), stream)
     return dx
 
 
+@_on_its_stream
 def conv2d_bwd_filter(x, dy, r: int, s: int, pad: int, with_db: bool = True, stream=None):
     import torch
     n, h, wd, c = x.shape
     k = dy.shape[3]
     sh = ConvShape(n, h, wd, c, k, r, s, pad)
-    dw = _empty((k, r, s, c), torch.float32, x.device, stream)
-    db = _empty((k,), torch.float32, x.device, stream) if with_db else None
+    dw = torch.empty((k, r, s, c), dtype=torch.float32, device=x.device)
+    db = torch.empty((k,), dtype=torch.float32, device=x.device) if with_db else None
     ws_bytes = mdnn_conv2d_bwd_filter_workspace(sh, dtype_of(x))
-    ws = _scratch(max(ws_bytes, 16), x.device, stream)
+    ws = torch.empty((max(ws_bytes, 16),), dtype=torch.uint8, device=x.device)
     mdnn_conv2d_bwd_filter(sh, x, dy, dtype_of(x), dw, db, ws, ws_bytes, stream)
     return dw, db
 
@@ -229,11 +238,11 @@ def _like(t, x, name: str):
     return t, _rows_of(t, name)[2]
 
 
-def _codes_like(q, rows: int, cols: int, device, stream):
+def _codes_like(q, rows: int, cols: int, device):
     """Room for [rows, cols] codes; allocated rows start on 128 bytes (a cache line)."""
     import torch
     if q is None:
-        q = _empty((rows, (cols + 127) // 128 * 128), torch.int8, device, stream)[:, :cols]
+        q = torch.empty((rows, (cols + 127) // 128 * 128), dtype=torch.int8, device=device)[:, :cols]
     elif q.dtype != torch.int8 or tuple(q.shape) != (rows, cols):
         raise ValueError(f"q must be int8 [{rows}, {cols}]")
     return q, _rows_of(q, "q")[2]
@@ -249,6 +258,7 @@ def _bytes_of(ws):
     return ws, ws.numel()
 
 
+@_on_its_stream
 def quantize_i8(x, transpose: bool = False, q=None, scale=None, workspace=None, stream=None):
     """(codes, scales) of a 2-D tensor: int8 codes with an fp32 scale for each
     row, or with transpose for each column, the codes stored [cols, rows] (a
@@ -256,17 +266,19 @@ def quantize_i8(x, transpose: bool = False, q=None, scale=None, workspace=None, 
     import torch
     rows, cols, ldx = _rows_of(x, "x")
     n = cols if transpose else rows
-    q, ldq = _codes_like(q, n, rows if transpose else cols, x.device, stream)
-    scale = _empty((n,), torch.float32, x.device, stream) if scale is None else _vector_of(scale, n, "scale")
+    q, ldq = _codes_like(q, n, rows if transpose else cols, x.device)
+    scale = torch.empty((n,), dtype=torch.float32, device=x.device) if scale is None else _vector_of(scale, n, "scale")
     if not transpose:
         mdnn_quantize_i8(rows, cols, x, ldx, dtype_of(x), q, ldq, scale, stream)
         return q, scale
     if workspace is None:
-        workspace = _scratch(max(mdnn_quantize_i8_t_workspace(rows, cols), 16), x.device, stream)
+        need = mdnn_quantize_i8_t_workspace(rows, cols)
+        workspace = torch.empty((max(need, 16),), dtype=torch.uint8, device=x.device)
     mdnn_quantize_i8_t(rows, cols, x, ldx, dtype_of(x), q, ldq, scale, *_bytes_of(workspace), stream)
     return q, scale
 
 
+@_on_its_stream
 def gemm_i8(A, a_scale, B, b_scale, bias=None, act: int = ACT_NONE, out_dtype=None, out=None, workspace=None,
             stream=None):
     """D = act((A B^T) * a_scale[:, None] * b_scale + bias) of int8 codes A [M, K],
@@ -279,30 +291,33 @@ def gemm_i8(A, a_scale, B, b_scale, bias=None, act: int = ACT_NONE, out_dtype=No
         raise ValueError("A and B must be int8 codes of one depth")
     _vector_of(a_scale, M, "a_scale"), _vector_of(b_scale, N, "b_scale"), _vector_of(bias, N, "bias")
     if out is None:
-        out = _empty((M, N), out_dtype or torch.float32, A.device, stream)
+        out = torch.empty((M, N), dtype=out_dtype or torch.float32, device=A.device)
     elif tuple(out.shape) != (M, N):
         raise ValueError(f"out must be [{M}, {N}]")
     if workspace is True:
-        workspace = _scratch(max(mdnn_gemm_i8_workspace(M, N, K), 16), A.device, stream)
+        workspace = torch.empty((max(mdnn_gemm_i8_workspace(M, N, K), 16),), dtype=torch.uint8, device=A.device)
     mdnn_gemm_i8(M, N, K, A, lda, a_scale, B, ldb, b_scale, bias, act, out, _rows_of(out, "out")[2], dtype_of(out),
                  *_bytes_of(workspace), stream)
     return out
 
 
+@_on_its_stream
 def rmsnorm(x, gamma=None, residual=None, eps: float = 1e-6, h_out=None, out=None, stream=None):
     """y = h * gamma / sqrt(mean(h^2) + eps) of the rows of h = x + residual.
     Returns y, or (y, h) with a residual (h_out is allocated then)."""
+    import torch
     rows, cols, ldx = _rows_of(x, "x")
     residual, ldr = _like(residual, x, "residual")
     if residual is not None and h_out is None:
-        h_out = _empty((rows, cols), x.dtype, x.device, stream)
+        h_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
     h_out, ldh = _like(h_out, x, "h_out")
-    out, ldy = _like(_empty((rows, cols), x.dtype, x.device, stream) if out is None else out, x, "out")
+    out, ldy = _like(torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out, x, "out")
     mdnn_rmsnorm_fwd(rows, cols, x, ldx, residual, ldr, _vector_of(gamma, cols, "gamma"), eps, h_out, ldh, out, ldy,
                      dtype_of(x), stream)
     return (out, h_out) if h_out is not None else out
 
 
+@_on_its_stream
 def rmsnorm_i8(x, gamma=None, residual=None, eps: float = 1e-6, h_out=None, q=None, scale=None, stream=None):
     """rmsnorm with its result as int8 codes and an fp32 scale for each row.
     Returns (q, scale), or (q, scale, h) with a residual."""
@@ -310,15 +325,17 @@ def rmsnorm_i8(x, gamma=None, residual=None, eps: float = 1e-6, h_out=None, q=No
     rows, cols, ldx = _rows_of(x, "x")
     residual, ldr = _like(residual, x, "residual")
     if residual is not None and h_out is None:
-        h_out = _empty((rows, cols), x.dtype, x.device, stream)
+        h_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
     h_out, ldh = _like(h_out, x, "h_out")
-    q, ldq = _codes_like(q, rows, cols, x.device, stream)
-    scale = _empty((rows,), torch.float32, x.device, stream) if scale is None else _vector_of(scale, rows, "scale")
+    q, ldq = _codes_like(q, rows, cols, x.device)
+    scale = (torch.empty((rows,), dtype=torch.float32, device=x.device) if scale is None
+             else _vector_of(scale, rows, "scale"))
     mdnn_rmsnorm_i8_fwd(rows, cols, x, ldx, residual, ldr, _vector_of(gamma, cols, "gamma"), eps, h_out, ldh, q, ldq,
                         scale, dtype_of(x), stream)
     return (q, scale, h_out) if h_out is not None else (q, scale)
 
 
+@_on_its_stream
 def rmsnorm_bwd(dy, h, gamma=None, eps: float = 1e-6, dres=None, dx=None, with_dgamma: bool = True, dgamma=None,
                 workspace=None, stream=None):
     """(dx, dgamma) of rmsnorm at the stored h; dres is the gradient that
@@ -329,15 +346,16 @@ def rmsnorm_bwd(dy, h, gamma=None, eps: float = 1e-6, dres=None, dx=None, with_d
         raise ValueError("h is required")
     h, ldh = _like(h, dy, "h")
     dres, lddr = _like(dres, dy, "dres")
-    dx, lddx = _like(_empty((rows, cols), dy.dtype, dy.device, stream) if dx is None else dx, dy, "dx")
+    dx, lddx = _like(torch.empty((rows, cols), dtype=dy.dtype, device=dy.device) if dx is None else dx, dy, "dx")
     if not with_dgamma:
         dgamma = None
     elif dgamma is None:
-        dgamma = _empty((cols,), torch.float32, dy.device, stream)
+        dgamma = torch.empty((cols,), dtype=torch.float32, device=dy.device)
     else:
         _vector_of(dgamma, cols, "dgamma")
     if with_dgamma and workspace is None:
-        workspace = _scratch(max(mdnn_rmsnorm_bwd_workspace(rows, cols), 256), dy.device, stream)
+        need = mdnn_rmsnorm_bwd_workspace(rows, cols)
+        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=dy.device)
     mdnn_rmsnorm_bwd(rows, cols, dy, lddy, h, ldh, _vector_of(gamma, cols, "gamma"), eps, dres, lddr, dx, lddx, dgamma,
                      dtype_of(dy), *_bytes_of(workspace), stream)
     return dx, dgamma

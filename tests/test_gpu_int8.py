@@ -425,19 +425,24 @@ def test_api_refuses(mdnn):
         mdnn.gemm_i8(a, one, a, one, workspace=torch.zeros(33, dtype=torch.uint8, device="cuda")[1:])
 
 
-def test_own_workspaces_on_the_default_streams_handle(mdnn):
-    """The default stream given as its handle, which is 0: the workspace lies in that stream's memory, and the results
-    are those of the call without a stream."""
+def test_wrappers_on_the_default_streams_handle(mdnn):
+    """The default stream given as its handle, which is 0, from another current stream: what is allocated lies in the
+    default stream's memory, and the results are those of the call without a stream."""
     import torch
-    from paper_2011_11188_amd import api
     assert torch.cuda.default_stream().cuda_stream == 0
-    ws = api._scratch(3 << 20, "cuda", 0)
-    owner = [g["stream"] for g in torch.cuda.memory_snapshot()
-             if g["address"] <= ws.data_ptr() < g["address"] + g["total_size"]]
-    assert owner == [0]
     x, dy = torch.randn(2000, 500, device="cuda"), torch.randn(2000, 500, device="cuda")
+    side = torch.cuda.Stream()
     for call in (lambda **k: mdnn.quantize_i8(x, transpose=True, **k), lambda **k: mdnn.rmsnorm_bwd(dy, x, **k)):
-        assert all(torch.equal(a, b) for a, b in zip(call(), call(stream=0)))
+        want = call()
+        with torch.cuda.stream(side):
+            got = call(stream=0)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        for t in got:
+            at = t.untyped_storage().data_ptr()
+            owner = [g["stream"] for g in torch.cuda.memory_snapshot()
+                     if g["address"] <= at < g["address"] + g["total_size"]]
+            assert owner == [0]
 
 
 @pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
