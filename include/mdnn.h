@@ -534,6 +534,115 @@ mdnn_status_t mdnn_rmsnorm_bwd(int64_t rows, int64_t cols, const void* dy, int64
                                mdnn_stream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Dropout, its mask never stored, and layer norm with the residual's addition
+ * and that dropout in its pass (a training step's regularised residual block).
+ *
+ * Dropout of element (r, c): dropped where its 16 bits are below t =
+ * floor(p 2^16 + 1/2), else multiplied by s = 2^16 / (2^16 - t).  The bits come
+ * from Philox 4x32 with ten rounds (Salmon, Moraes, Dror and Shaw, 2011) under
+ * the key `seed` at the counter (c / 8, r, step, site): 128 bits for eight
+ * columns, the lowest 16 bits of the first word first.  rng: device memory of
+ * two 64-bit numbers, {seed, step} (of step the lowest 32 bits count), read
+ * when the call runs: a captured step draws anew at each replay if the program
+ * advances step in between, and the backward call, given the same rng, site
+ * and p, draws the same bits.  site tells the places of a program apart.
+ * p in [0, 1]; where t is 0 nothing is drawn and rng may be NULL; where t is
+ * 2^16 all is dropped.  rows <= 2^32 with t > 0.
+ *   mdnn_dropout_fwd   y = residual + dropout(x)     (residual NULL: without it)
+ *   mdnn_dropout_bwd   dx = dropout(dy)
+ *   mdnn_layernorm_fwd h = residual + dropout(x)     (fp32)
+ *     y = (h - mean h) / sqrt(var h + eps) * gamma + beta
+ *     gamma (ones) and beta (zeros) NULL or fp32 [cols]; eps > 0.  h_out (NULL
+ *     allowed) receives h rounded to dtype, the bits of mdnn_dropout_fwd; y is
+ *     computed from the unrounded h and rounded once.
+ *   mdnn_layernorm_bwd gradients at the stored h (x itself where there was
+ *     neither residual nor dropout), with r = 1 / sqrt(var h + eps), xh =
+ *     (h - mean h) r, g = dy gamma:
+ *     dh = r (g - mean g - xh mean(g xh)) + dres   (dres NULL: without it; it
+ *          is the gradient that reaches h along the residual)
+ *     dx = dropout(dh), from the unrounded dh
+ *     dgamma[c] = sum over rows of dy xh, dbeta[c] = sum over rows of dy
+ *          (fp32, overwritten; rows == 0: zeros)
+ *     dx, dh, dgamma and dbeta may each be NULL.  workspace:
+ *     mdnn_layernorm_bwd_workspace(rows, cols) bytes, 256-byte aligned, when
+ *     dgamma or dbeta is asked for (else, and where that is 0, NULL is
+ *     allowed); scratch.
+ * Rows of `dtype`, any leading dimensions >= cols, buffers aligned to their
+ * elements.  cols >= 1 (dropout: >= 0) and <= 2^29, any rows >= 0.  Statistics
+ * are fp32, partly 64-bit in rows longer than the registers hold; sums in a
+ * fixed order (deterministic).  A row that holds Inf or NaN, or whose sums pass
+ * fp32's range, gives NaN in all of y; an element that is dropped counts as 0
+ * whatever it holds.  Outputs may lie exactly in place of an input of dtype
+ * (same address and leading dimension), two outputs never in the same place;
+ * otherwise outputs must not overlap inputs or each other.
+ * Errors: MDNN_ERR_SHAPE (also p and eps), _DTYPE, _NULL, _LAYOUT,
+ * _MISALIGNED, _WORKSPACE, _LAUNCH.
+ * ------------------------------------------------------------------------- */
+mdnn_status_t mdnn_dropout_fwd(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual,
+                               int64_t ldr, float p, const void* rng, uint32_t site, void* y, int64_t ldy,
+                               mdnn_dtype_t dtype, mdnn_stream_t stream);
+mdnn_status_t mdnn_dropout_bwd(int64_t rows, int64_t cols, const void* dy, int64_t lddy, float p, const void* rng,
+                               uint32_t site, void* dx, int64_t lddx, mdnn_dtype_t dtype, mdnn_stream_t stream);
+mdnn_status_t mdnn_layernorm_fwd(int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* residual,
+                                 int64_t ldr, float p, const void* rng, uint32_t site, const float* gamma,
+                                 const float* beta, float eps, void* h_out, int64_t ldh, void* y, int64_t ldy,
+                                 mdnn_dtype_t dtype, mdnn_stream_t stream);
+size_t mdnn_layernorm_bwd_workspace(int64_t rows, int64_t cols);
+mdnn_status_t mdnn_layernorm_bwd(int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* h, int64_t ldh,
+                                 const float* gamma, float eps, const void* dres, int64_t lddr, float p,
+                                 const void* rng, uint32_t site, void* dx, int64_t lddx, void* dh, int64_t lddh,
+                                 float* dgamma, float* dbeta, mdnn_dtype_t dtype, void* workspace, size_t ws_bytes,
+                                 mdnn_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * A last layer z = x W + bias of many classes and its softmax cross entropy,
+ * in pieces of the classes: neither the logits nor their gradients of all
+ * classes are kept (mdnn_softmax_xent takes stored logits of up to 1024).
+ *   x [M, K], ldx >= K; W of the same dtype, layout MDNN_NN: W[K, N], ldw >= N
+ *   (this library's FC weights), MDNN_NT: W[N, K], ldw >= K (a table by
+ *   classes).  bias NULL or fp32 [N] (-Inf masks a class).  labels int32 [M]:
+ *   a class, or `ignored` (any value, also one that is a class): such a row
+ *   counts nowhere.  Any other label outside [0, N) is data: the row's loss and
+ *   gradient are NaN.
+ *   lse_i = log sum_j exp(z_ij);  row_loss_i = lse_i - z_i,label (0: ignored)
+ *   loss = sum of row_loss / number of rows not ignored (0 where none counts)
+ * mdnn_linear_xent_fwd writes loss (fp32), row_loss and lse (fp32 [M], lse of
+ *   every row), each NULL allowed.  A row whose logits are all -Inf has lse
+ *   -Inf and no loss (NaN).
+ * mdnn_linear_xent_bwd takes lse as the forward call left it, computes each
+ *   piece's logits again, and with G_ij = exp(z_ij - lse_i) - [j = label_i] (0 in
+ *   ignored rows, whatever x and lse hold there) and a = S / counted rows, S =
+ *   *loss_scale (device fp32; NULL means 1), writes
+ *     dx [M, lddx >= K] = a G W^T      of dtype,
+ *     dw = a x^T G, stored as W is, lddw as ldw, of dw_type (fp32 or dtype),
+ *     db [N] = a * column sums of G    fp32;
+ *   each NULL allowed, all overwritten.  G is rounded to dtype between the
+ *   products (fp16: times 2^15, so that small probabilities keep their bits; S
+ *   does not change it); db is summed before that rounding.
+ * M >= 0 and <= 2^24 (0: loss, dw and db are 0), N and K from 1 to 2^31 - 1, any
+ * leading dimensions and element-aligned buffers; 16-byte aligned ones with
+ * leading dimensions multiples of 8 are fastest.  workspace: the bytes that the
+ * _workspace function gives for the same layout, sizes and dtype (0 where M is
+ * 0), 256-byte aligned; scratch, overwritten; calls that share one must be
+ * ordered on one stream.  Outputs must not overlap inputs or each other.
+ * Products are accumulated in fp32, the exponentials' sums in fp32, the loss
+ * over rows in 64 bits; all orders are fixed (deterministic).
+ * Errors: MDNN_ERR_SHAPE, _DTYPE, _NULL, _LAYOUT (also layout TN),
+ * _MISALIGNED, _WORKSPACE, _LAUNCH.
+ * ------------------------------------------------------------------------- */
+size_t mdnn_linear_xent_fwd_workspace(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t dtype);
+mdnn_status_t mdnn_linear_xent_fwd(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx,
+                                   const void* w, int64_t ldw, mdnn_dtype_t dtype, const float* bias,
+                                   const int32_t* labels, int32_t ignored, float* loss, float* row_loss, float* lse,
+                                   void* workspace, size_t ws_bytes, mdnn_stream_t stream);
+size_t mdnn_linear_xent_bwd_workspace(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t dtype);
+mdnn_status_t mdnn_linear_xent_bwd(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx,
+                                   const void* w, int64_t ldw, mdnn_dtype_t dtype, const float* bias,
+                                   const int32_t* labels, int32_t ignored, const float* lse, const float* loss_scale,
+                                   void* dx, int64_t lddx, void* dw, int64_t lddw, mdnn_dtype_t dw_type, float* db,
+                                   void* workspace, size_t ws_bytes, mdnn_stream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Train step of a fixed layer chain (section 2.1 compute graph, fixed here;
  * section 3.1 minibatch SGD).  One call = forward, loss, backpropagation and
  * update of one minibatch, all enqueued on one stream with no host sync.

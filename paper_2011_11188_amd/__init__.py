@@ -67,7 +67,7 @@ class TrainCfg(C.Structure):
                 ("fuse_update", C.c_int32)]
 
 
-_vp, _i64, _f, _i = C.c_void_p, C.c_int64, C.c_float, C.c_int
+_vp, _i64, _f, _i, _u32 = C.c_void_p, C.c_int64, C.c_float, C.c_int, C.c_uint32
 
 _SIGS = {
     "mdnn_gemm_mixed": [_i, _i64, _i64, _i64, _f, _vp, _i64, _vp, _i64, _i, _f, _vp, _i64, _vp,
@@ -106,6 +106,15 @@ _SIGS = {
     "mdnn_rmsnorm_i8_fwd": [_i64, _i64, _vp, _i64, _vp, _i64, _vp, _f, _vp, _i64, _vp, _i64, _vp, _i, _vp],
     "mdnn_rmsnorm_bwd": [_i64, _i64, _vp, _i64, _vp, _i64, _vp, _f, _vp, _i64, _vp, _i64, _vp, _i, _vp, C.c_size_t,
                          _vp],
+    "mdnn_dropout_fwd": [_i64, _i64, _vp, _i64, _vp, _i64, _f, _vp, _u32, _vp, _i64, _i, _vp],
+    "mdnn_dropout_bwd": [_i64, _i64, _vp, _i64, _f, _vp, _u32, _vp, _i64, _i, _vp],
+    "mdnn_layernorm_fwd": [_i64, _i64, _vp, _i64, _vp, _i64, _f, _vp, _u32, _vp, _vp, _f, _vp, _i64, _vp, _i64, _i, _vp],
+    "mdnn_layernorm_bwd": [_i64, _i64, _vp, _i64, _vp, _i64, _vp, _f, _vp, _i64, _f, _vp, _u32, _vp, _i64, _vp, _i64,
+                           _vp, _vp, _i, _vp, C.c_size_t, _vp],
+    "mdnn_linear_xent_fwd": [_i, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i, _vp, _vp, C.c_int32, _vp, _vp, _vp, _vp,
+                             C.c_size_t, _vp],
+    "mdnn_linear_xent_bwd": [_i, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i, _vp, _vp, C.c_int32, _vp, _vp, _vp, _i64,
+                             _vp, _i64, _i, _vp, _vp, C.c_size_t, _vp],
     "mdnn_train_graph_create": [_vp, _vp, _vp, _vp, _vp],
     "mdnn_graph_launch": [_vp, _vp],
 }
@@ -135,6 +144,12 @@ _lib.mdnn_gemm_i8_workspace.argtypes = [_i64, _i64, _i64]
 _lib.mdnn_gemm_i8_workspace.restype = C.c_size_t
 _lib.mdnn_rmsnorm_bwd_workspace.argtypes = [_i64, _i64]
 _lib.mdnn_rmsnorm_bwd_workspace.restype = C.c_size_t
+_lib.mdnn_layernorm_bwd_workspace.argtypes = [_i64, _i64]
+_lib.mdnn_layernorm_bwd_workspace.restype = C.c_size_t
+_lib.mdnn_linear_xent_fwd_workspace.argtypes = [_i, _i64, _i64, _i64, _i]
+_lib.mdnn_linear_xent_fwd_workspace.restype = C.c_size_t
+_lib.mdnn_linear_xent_bwd_workspace.argtypes = [_i, _i64, _i64, _i64, _i]
+_lib.mdnn_linear_xent_bwd_workspace.restype = C.c_size_t
 _lib.mdnn_last_error.restype = C.c_char_p
 _lib.mdnn_version.restype = C.c_char_p
 _lib.mdnn_net_activation.argtypes = [_vp, C.c_int32]
@@ -209,7 +224,8 @@ def exported_symbols():
                                  "mdnn_gemm_split3_workspace", "mdnn_gemm_workspace",
                                  "mdnn_conv2d_fwd_winograd_workspace", "mdnn_conv2d_fwd_algo_workspace",
                                  "mdnn_conv2d_fwd_choose", "mdnn_quantize_i8_t_workspace",
-                                 "mdnn_gemm_i8_workspace", "mdnn_rmsnorm_bwd_workspace",
+                                 "mdnn_gemm_i8_workspace", "mdnn_rmsnorm_bwd_workspace", "mdnn_layernorm_bwd_workspace",
+                                 "mdnn_linear_xent_fwd_workspace", "mdnn_linear_xent_bwd_workspace",
                                  "mdnn_last_error",
                                  "mdnn_version", "mdnn_net_activation", "mdnn_net_output_grad", "mdnn_net_destroy",
                                  "mdnn_graph_destroy", "mdnn_set_gemm_tile"])
@@ -407,6 +423,52 @@ def mdnn_rmsnorm_bwd(rows, cols, dy, lddy, h, ldh, gamma, eps, dres, lddr, dx, l
                      ws_bytes=0, stream=None):
     return _call("mdnn_rmsnorm_bwd", rows, cols, _p(dy), lddy, _p(h), ldh, _p(gamma), eps, _p(dres), lddr, _p(dx), lddx,
                  _p(dgamma), dtype, _p(workspace), ws_bytes, _s(stream))
+
+
+def mdnn_dropout_fwd(rows, cols, x, ldx, residual, ldr, p, rng, site, y, ldy, dtype, stream=None):
+    return _call("mdnn_dropout_fwd", rows, cols, _p(x), ldx, _p(residual), ldr, p, _p(rng), site, _p(y), ldy, dtype,
+                 _s(stream))
+
+
+def mdnn_dropout_bwd(rows, cols, dy, lddy, p, rng, site, dx, lddx, dtype, stream=None):
+    return _call("mdnn_dropout_bwd", rows, cols, _p(dy), lddy, p, _p(rng), site, _p(dx), lddx, dtype, _s(stream))
+
+
+def mdnn_layernorm_fwd(rows, cols, x, ldx, residual, ldr, p, rng, site, gamma, beta, eps, h_out, ldh, y, ldy, dtype,
+                       stream=None):
+    return _call("mdnn_layernorm_fwd", rows, cols, _p(x), ldx, _p(residual), ldr, p, _p(rng), site, _p(gamma), _p(beta),
+                 eps, _p(h_out), ldh, _p(y), ldy, dtype, _s(stream))
+
+
+def mdnn_layernorm_bwd_workspace(rows, cols) -> int:
+    return _lib.mdnn_layernorm_bwd_workspace(rows, cols)
+
+
+def mdnn_layernorm_bwd(rows, cols, dy, lddy, h, ldh, gamma, eps, dres, lddr, p, rng, site, dx, lddx, dh, lddh, dgamma,
+                       dbeta, dtype, workspace=None, ws_bytes=0, stream=None):
+    return _call("mdnn_layernorm_bwd", rows, cols, _p(dy), lddy, _p(h), ldh, _p(gamma), eps, _p(dres), lddr, p, _p(rng),
+                 site, _p(dx), lddx, _p(dh), lddh, _p(dgamma), _p(dbeta), dtype, _p(workspace), ws_bytes, _s(stream))
+
+
+def mdnn_linear_xent_fwd_workspace(layout, M, N, K, dtype) -> int:
+    return _lib.mdnn_linear_xent_fwd_workspace(layout, M, N, K, dtype)
+
+
+def mdnn_linear_xent_fwd(layout, M, N, K, x, ldx, w, ldw, dtype, bias, labels, ignored, loss, row_loss, lse,
+                         workspace=None, ws_bytes=0, stream=None):
+    return _call("mdnn_linear_xent_fwd", layout, M, N, K, _p(x), ldx, _p(w), ldw, dtype, _p(bias), _p(labels), ignored,
+                 _p(loss), _p(row_loss), _p(lse), _p(workspace), ws_bytes, _s(stream))
+
+
+def mdnn_linear_xent_bwd_workspace(layout, M, N, K, dtype) -> int:
+    return _lib.mdnn_linear_xent_bwd_workspace(layout, M, N, K, dtype)
+
+
+def mdnn_linear_xent_bwd(layout, M, N, K, x, ldx, w, ldw, dtype, bias, labels, ignored, lse, loss_scale, dx, lddx, dw,
+                         lddw, dw_type, db, workspace=None, ws_bytes=0, stream=None):
+    return _call("mdnn_linear_xent_bwd", layout, M, N, K, _p(x), ldx, _p(w), ldw, dtype, _p(bias), _p(labels), ignored,
+                 _p(lse), _p(loss_scale), _p(dx), lddx, _p(dw), lddw, dw_type, _p(db), _p(workspace), ws_bytes,
+                 _s(stream))
 
 
 def mdnn_net_create(layers, batch: int, cfg: TrainCfg) -> int:

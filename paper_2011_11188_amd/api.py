@@ -24,11 +24,14 @@ from . import (_s, ACT_NONE, BF16, F16, F32, LAYER_CONV, LAYER_FC, LAYER_MAXPOOL
                mdnn_conv2d_fwd_winograd_workspace, mdnn_conv2d_fwd_algo, mdnn_conv2d_fwd_algo_workspace,
                mdnn_quantize_i8, mdnn_quantize_i8_t, mdnn_quantize_i8_t_workspace, mdnn_gemm_i8,
                mdnn_gemm_i8_workspace, mdnn_rmsnorm_fwd, mdnn_rmsnorm_i8_fwd, mdnn_rmsnorm_bwd,
-               mdnn_rmsnorm_bwd_workspace)
+               mdnn_rmsnorm_bwd_workspace, mdnn_dropout_fwd, mdnn_dropout_bwd, mdnn_layernorm_fwd, mdnn_layernorm_bwd,
+               mdnn_layernorm_bwd_workspace, mdnn_linear_xent_fwd, mdnn_linear_xent_fwd_workspace, mdnn_linear_xent_bwd,
+               mdnn_linear_xent_bwd_workspace)
 
 __all__ = ["torch_dtype", "gemm", "split_f16", "gemm_split3", "conv_shape", "conv2d_fwd",
            "conv2d_fwd_winograd", "conv2d_fwd_algo", "conv2d_bwd_data", "conv2d_bwd_filter", "make_scaler", "read_scaler", "Net", "StepGraph",
-           "quantize_i8", "gemm_i8", "rmsnorm", "rmsnorm_i8", "rmsnorm_bwd"]
+           "quantize_i8", "gemm_i8", "rmsnorm", "rmsnorm_i8", "rmsnorm_bwd", "make_rng", "dropout", "dropout_bwd",
+           "layernorm", "layernorm_bwd", "linear_xent", "linear_xent_bwd"]
 
 
 def torch_dtype(code: int):
@@ -359,6 +362,151 @@ def rmsnorm_bwd(dy, h, gamma=None, eps: float = 1e-6, dres=None, dx=None, with_d
     mdnn_rmsnorm_bwd(rows, cols, dy, lddy, h, ldh, _vector_of(gamma, cols, "gamma"), eps, dres, lddr, dx, lddx, dgamma,
                      dtype_of(dy), *_bytes_of(workspace), stream)
     return dx, dgamma
+
+
+def make_rng(seed: int, step: int = 0, device="cuda"):
+    """The device state {seed, step} that dropout draws from.  Advance the step between training steps (rng[1] += 1, also
+    between replays of a captured one), after the backward pass, which draws the same bits again."""
+    import torch
+    wrap = lambda v: (int(v) + 2 ** 63) % 2 ** 64 - 2 ** 63  # noqa: E731
+    return torch.tensor([wrap(seed), wrap(step)], dtype=torch.int64, device=device)
+
+
+def _rng_of(rng, p: float):
+    """The generator's state, needed where p drops anything."""
+    import torch
+    if rng is None:
+        if p > 0.0:
+            raise ValueError("rng is required with p > 0")
+        return None
+    if rng.dtype != torch.int64 or rng.numel() != 2 or not rng.is_contiguous():
+        raise ValueError("rng must be two contiguous int64 values")
+    if not rng.is_cuda or rng.device.index != torch.cuda.current_device():
+        raise ValueError("rng is not on the current GPU")
+    return rng
+
+
+@_on_its_stream
+def dropout(x, p: float, rng=None, site: int = 0, residual=None, out=None, stream=None):
+    """residual + dropout(x): elements dropped with chance p, the others times its inverse; no mask is stored."""
+    import torch
+    rows, cols, ldx = _rows_of(x, "x")
+    residual, ldr = _like(residual, x, "residual")
+    out, ldy = _like(torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out, x, "out")
+    mdnn_dropout_fwd(rows, cols, x, ldx, residual, ldr, p, _rng_of(rng, p), site, out, ldy, dtype_of(x), stream)
+    return out
+
+
+@_on_its_stream
+def dropout_bwd(dy, p: float, rng=None, site: int = 0, dx=None, stream=None):
+    """The gradient of dropout's x, with the bits that dropout drew for the same rng and site."""
+    import torch
+    rows, cols, lddy = _rows_of(dy, "dy")
+    dx, lddx = _like(torch.empty((rows, cols), dtype=dy.dtype, device=dy.device) if dx is None else dx, dy, "dx")
+    mdnn_dropout_bwd(rows, cols, dy, lddy, p, _rng_of(rng, p), site, dx, lddx, dtype_of(dy), stream)
+    return dx
+
+
+@_on_its_stream
+def layernorm(x, gamma=None, beta=None, residual=None, eps: float = 1e-5, p: float = 0.0, rng=None, site: int = 0,
+              h_out=None, out=None, stream=None):
+    """Layer norm of the rows of h = residual + dropout(x).  Returns y, or (y, h) with a residual or dropout (h_out is
+    allocated then)."""
+    import torch
+    rows, cols, ldx = _rows_of(x, "x")
+    residual, ldr = _like(residual, x, "residual")
+    if (residual is not None or p > 0.0) and h_out is None:
+        h_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    h_out, ldh = _like(h_out, x, "h_out")
+    out, ldy = _like(torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out, x, "out")
+    mdnn_layernorm_fwd(rows, cols, x, ldx, residual, ldr, p, _rng_of(rng, p), site, _vector_of(gamma, cols, "gamma"),
+                       _vector_of(beta, cols, "beta"), eps, h_out, ldh, out, ldy, dtype_of(x), stream)
+    return (out, h_out) if h_out is not None else out
+
+
+@_on_its_stream
+def layernorm_bwd(dy, h, gamma=None, eps: float = 1e-5, dres=None, p: float = 0.0, rng=None, site: int = 0, dx=None,
+                  dh=None, with_sums: bool = True, dgamma=None, dbeta=None, workspace=None, stream=None):
+    """(dx, dh, dgamma, dbeta) of layernorm at the stored h; dres is the gradient that reaches h along the residual.  dh,
+    the residual's gradient, is dx itself without dropout (a dh given is written all the same); dgamma and dbeta are None
+    without with_sums."""
+    import torch
+    rows, cols, lddy = _rows_of(dy, "dy")
+    if h is None:
+        raise ValueError("h is required")
+    h, ldh = _like(h, dy, "h")
+    dres, lddr = _like(dres, dy, "dres")
+    dx, lddx = _like(torch.empty((rows, cols), dtype=dy.dtype, device=dy.device) if dx is None else dx, dy, "dx")
+    if p > 0.0 and dh is None:
+        dh = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device)
+    dh, lddh = _like(dh, dy, "dh")
+    if not with_sums:
+        dgamma = dbeta = None
+    else:
+        dgamma, dbeta = (torch.empty((cols,), dtype=torch.float32, device=dy.device) if t is None
+                         else _vector_of(t, cols, n) for t, n in ((dgamma, "dgamma"), (dbeta, "dbeta")))
+    if with_sums and workspace is None:
+        need = mdnn_layernorm_bwd_workspace(rows, cols)
+        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=dy.device)
+    mdnn_layernorm_bwd(rows, cols, dy, lddy, h, ldh, _vector_of(gamma, cols, "gamma"), eps, dres, lddr, p,
+                       _rng_of(rng, p), site, dx, lddx, dh, lddh, dgamma, dbeta, dtype_of(dy), *_bytes_of(workspace),
+                       stream)
+    return dx, dx if dh is None else dh, dgamma, dbeta
+
+
+def _xent_args(x, w, labels, bias, layout):
+    """Sizes, leading dimensions and checked operands of the last layer."""
+    import torch
+    M, K, ldx = _rows_of(x, "x")
+    if layout not in (NN, NT):
+        raise ValueError("layout must be NN (w [in, classes]) or NT (w [classes, in])")
+    k, N = w.shape if layout == NN else w.shape[::-1]
+    if k != K or w.dtype != x.dtype:
+        raise ValueError("w must have x's type and width")
+    if labels.dtype != torch.int32 or labels.shape != (M,) or not labels.is_contiguous():
+        raise ValueError("labels must be one contiguous int32 for each row")
+    if not labels.is_cuda or labels.device.index != torch.cuda.current_device():
+        raise ValueError("labels are not on the current GPU")
+    return M, N, K, ldx, _rows_of(w, "w")[2], _vector_of(bias, N, "bias")
+
+
+@_on_its_stream
+def linear_xent(x, w, labels, bias=None, layout: int = NN, ignored: int = -1, workspace=None, stream=None):
+    """(loss, row_loss, lse) of a last layer x w + bias of many classes: the mean cross entropy over the rows whose label
+    is not `ignored`, each row's, and the logarithm of each row's sum of exponentials, which the gradients need.  w:
+    [in, classes] (NN) or [classes, in] (NT); the logits of all classes are never stored."""
+    import torch
+    M, N, K, ldx, ldw, bias = _xent_args(x, w, labels, bias, layout)
+    loss, row_loss, lse = (torch.empty((n,), dtype=torch.float32, device=x.device) for n in (1, M, M))
+    if workspace is None:
+        need = mdnn_linear_xent_fwd_workspace(layout, M, N, K, dtype_of(x))
+        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=x.device)
+    mdnn_linear_xent_fwd(layout, M, N, K, x, ldx, w, ldw, dtype_of(x), bias, labels, ignored, loss, row_loss, lse,
+                         *_bytes_of(workspace), stream)
+    return loss, row_loss, lse
+
+
+@_on_its_stream
+def linear_xent_bwd(x, w, labels, lse, bias=None, layout: int = NN, ignored: int = -1, loss_scale=None, dw_dtype=None,
+                    dx=None, dw=None, db=None, workspace=None, stream=None):
+    """(dx, dw, db) of linear_xent's loss times loss_scale (a device fp32; None: 1) from its lse.  dw is stored as w is, in
+    dw_dtype (fp32 by default, or w's type); db is None without a bias."""
+    import torch
+    M, N, K, ldx, ldw, bias = _xent_args(x, w, labels, bias, layout)
+    dx, lddx = _like(torch.empty((M, K), dtype=x.dtype, device=x.device) if dx is None else dx, x, "dx")
+    if dw is None:
+        dw = torch.empty(tuple(w.shape), dtype=torch.float32 if dw_dtype is None else dw_dtype, device=x.device)
+    elif dw.shape != w.shape or (dw_dtype is not None and dw.dtype != dw_dtype):
+        raise ValueError("dw must have w's shape")
+    if bias is not None and db is None:
+        db = torch.empty((N,), dtype=torch.float32, device=x.device)
+    if workspace is None:
+        need = mdnn_linear_xent_bwd_workspace(layout, M, N, K, dtype_of(x))
+        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=x.device)
+    mdnn_linear_xent_bwd(layout, M, N, K, x, ldx, w, ldw, dtype_of(x), bias, labels, ignored, _vector_of(lse, M, "lse"),
+                         _vector_of(loss_scale, 1, "loss_scale"), dx, lddx, dw, _rows_of(dw, "dw")[2], dtype_of(dw),
+                         _vector_of(db, N, "db"), *_bytes_of(workspace), stream)
+    return dx, dw, db
 
 
 def make_scaler(scale: float, growth_interval: int = 2000, growth: float = 2.0,

@@ -18,85 +18,14 @@
 // so every load is unconditional and lies inside the row.  Rows longer than
 // the registers hold, or below eight elements, take the two-pass kernels.
 #include <cmath>
-#include <type_traits>
 
-#include "gemm_core.h"
 #include "internal.h"
+#include "row_chunk.h"
 
 namespace mdnn {
 namespace {
 
 constexpr float A_MIN = 0x1p-100f;  // smallest row maximum the codes resolve (127 / a stays finite)
-
-// Eight consecutive elements at any element address.
-typedef uint32_t u4v_a2 __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u4v_a4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u2v_a1 __attribute__((ext_vector_type(2), aligned(1)));
-#define MDNN_GLOBAL __attribute__((address_space(1)))
-
-template <class T>
-struct Chunk {
-  static constexpr bool H = sizeof(typename T::storage) == 2;
-  typedef typename T::storage S;
-  uint32_t w[H ? 4 : 8];
-  __device__ __forceinline__ void load(const S* p) {
-    if constexpr (H) {
-      const u4v_a2 v = *(const MDNN_GLOBAL u4v_a2*)p;
-      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-    } else {
-      const u4v_a4 v = *(const MDNN_GLOBAL u4v_a4*)p, u = *(const MDNN_GLOBAL u4v_a4*)(p + 4);
-      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w, w[4] = u.x, w[5] = u.y, w[6] = u.z, w[7] = u.w;
-    }
-  }
-  __device__ __forceinline__ float get(int e) const {
-    if constexpr (H)
-      return to_f<T>((uint16_t)(w[e >> 1] >> ((e & 1) * 16)));
-    else
-      return __builtin_bit_cast(float, w[e]);
-  }
-  // clears elements 0 .. lo - 1
-  __device__ __forceinline__ void clear(int lo) {
-    asm("" : "+v"(lo));  // (the tests of lo stay here: hoisted out of a loop over rows they fill the scalar registers)
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < lo) w[H ? e >> 1 : e] &= H && !(e & 1) ? 0xffff0000u : 0u;
-  }
-  __device__ __forceinline__ void set(const float (&v)[8]) {
-    if constexpr (H) {
-      // (a vector conversion is one instruction for two elements)
-      typedef float f2 __attribute__((ext_vector_type(2)));
-      typedef std::conditional_t<T::id == MDNN_F16, _Float16, __bf16> E;
-      typedef E e2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[2 * e], v[2 * e + 1]}, e2));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = __builtin_bit_cast(uint32_t, v[e]);
-    }
-  }
-  // elements lo .. 7 (lo = 0: one vector store)
-  __device__ __forceinline__ void store(S* p, int lo) const {
-    if (lo == 0) {
-      if constexpr (H) {
-        *(MDNN_GLOBAL u4v_a2*)p = (u4v_a2){w[0], w[1], w[2], w[3]};
-      } else {
-        *(MDNN_GLOBAL u4v_a4*)p = (u4v_a4){w[0], w[1], w[2], w[3]};
-        *(MDNN_GLOBAL u4v_a4*)(p + 4) = (u4v_a4){w[4], w[5], w[6], w[7]};
-      }
-    } else {
-      asm("" : "+v"(lo));
-#pragma unroll
-      for (int e = 1; e < 8; ++e)
-        if (e >= lo) {
-          if constexpr (H)
-            p[e] = (uint16_t)(w[e >> 1] >> ((e & 1) * 16));
-          else
-            p[e] = __builtin_bit_cast(float, w[e]);
-        }
-    }
-  }
-};
 
 // Codes of four values: fl(t * inv) rounded to the nearest even integer (by
 // adding 1.5 * 2^23, whose last place is 1), the low bytes packed.  The
@@ -109,14 +38,6 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, f
   const uint32_t uc = __float_as_uint(pc + MAGIC), ud = __float_as_uint(pd + MAGIC);
   const uint32_t lo = __builtin_amdgcn_perm(ub, ua, 0x0c0c0400u), hi = __builtin_amdgcn_perm(ud, uc, 0x0c0c0400u);
   return lo | (hi << 16);
-}
-__device__ __forceinline__ float mul_rn(float a, float b) {
-#pragma clang fp contract(off)
-  return a * b;
-}
-__device__ __forceinline__ float add_rn(float a, float b) {
-#pragma clang fp contract(off)
-  return a + b;
 }
 __device__ __forceinline__ void store_codes(int8_t* p, uint32_t lo4, uint32_t hi4, int lo) {
   if (lo == 0) {
@@ -181,28 +102,6 @@ __device__ __forceinline__ SumMax row_reduce(SumMax v, SumMax (*buf)[TPR / 64 + 
   }
   return v;
 }
-struct Sum2 {
-  float a, b;
-};
-template <int TPR, int RPB>
-__device__ __forceinline__ Sum2 row_reduce(Sum2 v, Sum2 (*buf)[RPB][TPR / 64 + 1], int flip) {
-  constexpr int W = TPR < 64 ? TPR : 64;
-#pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1) {
-    v.a += __shfl_xor(v.a, o, W);
-    v.b += __shfl_xor(v.b, o, W);
-  }
-  if constexpr (TPR > 64) {
-    const int r = threadIdx.x / TPR;
-    if ((threadIdx.x & 63) == 0) buf[flip][r][threadIdx.x % TPR >> 6] = v;
-    __syncthreads();
-    v = buf[flip][r][0];
-#pragma unroll
-    for (int w = 1; w < TPR / 64; ++w) v.a += buf[flip][r][w].a, v.b += buf[flip][r][w].b;
-  }
-  return v;
-}
-
 enum RowMode { QUANT = 0, NORM = 1, NORM_I8 = 2 };
 
 struct RowArgs {
@@ -215,16 +114,6 @@ struct RowArgs {
   int32_t cols;
   float eps;
 };
-
-// Where this thread's chunk c of a row lies: its first element, and how many
-// of its leading elements are not its own (8: none is).
-struct ChunkPos {
-  int start, lo;
-};
-__device__ __forceinline__ ChunkPos chunk_pos(int c, int cols) {
-  const int at = c * 8, last = cols - 8;
-  return {at < last ? at : last, at <= last ? 0 : at < cols ? at - last : 8};
-}
 
 template <class T, int MODE, int TPR, int NCH>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_kernel(RowArgs a) {
@@ -395,9 +284,6 @@ __global__ void __launch_bounds__(1024) row_long_kernel(RowArgs a) {
     }
   }
 }
-
-// One launch holds fewer than 2^32 threads: blocks beyond this many rows loop.
-constexpr int64_t MAX_BLOCKS = 1 << 20;
 
 template <class T, int MODE, int TPR, int NCH>
 void launch_rows(const RowArgs& a, hipStream_t st) {
