@@ -276,7 +276,7 @@ BwdPlan bwd_plan(int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
   p.rows = h ? ceil_div(M, 64) * 64 : M;
   p.kc = h ? ceil_div(K, 8) * 8 : ceil_div(K, 4) * 4;
   p.ldg = h ? ceil_div(p.nc, 64) * 64 : ceil_div(p.nc, 4) * 4;
-  p.blocks = ceil_div(M, 32);
+  p.blocks = ceil_div(p.rows, 32);  // (of xent_grad_kernel, padding rows too)
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at += pad256(n); return o; };
   p.alpha = take(4);
