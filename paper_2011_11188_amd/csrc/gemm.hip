@@ -768,10 +768,11 @@ template <class T, class OutT>
 static mdnn_status_t gemm_dispatch16(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
                                      const void* A, int64_t lda, bool va, const void* B,
                                      int64_t ldb, bool vb, const Epilogue& ep_in, void* ws, size_t ws_bytes,
-                                     hipStream_t st) {
+                                     hipStream_t st, int64_t ext_a, int64_t ext_b) {
   const uint16_t* a = (const uint16_t*)A;
   const uint16_t* b = (const uint16_t*)B;
-  const LdsOperand la{A, lda, M, layout != MDNN_TN}, lb{B, ldb, N, layout == MDNN_NT};
+  const LdsOperand la{A, lda, layout == MDNN_TN && ext_a > M ? ext_a : M, layout != MDNN_TN};
+  const LdsOperand lb{B, ldb, layout != MDNN_NT && ext_b > N ? ext_b : N, layout == MDNN_NT};
   // split K over the workspace when the grid is small (partials in fp32,
   // then the epilogue in a fixed-order reduction)
   Epilogue ep = ep_in;
@@ -921,7 +922,7 @@ mdnn_status_t mdnn::gemm_mixed_ws(mdnn_layout_t layout, int64_t M, int64_t N, in
                                   float beta, const void* C, int64_t ldc, void* D, int64_t ldd,
                                   mdnn_dtype_t d_type, const float* bias, mdnn_act_t act, const void* mask_src,
                                   int64_t ldm, void* ws, size_t ws_bytes, mdnn_stream_t stream,
-                                  int32_t* nonfinite, const float* alpha_dev) {
+                                  int32_t* nonfinite, const float* alpha_dev, int64_t ext_a, int64_t ext_b) {
   if (layout != MDNN_NN && layout != MDNN_NT && layout != MDNN_TN)
     return fail(MDNN_ERR_LAYOUT, "gemm: unknown layout %d", (int)layout);
   if (M < 0 || N < 0 || K < 0) return fail(MDNN_ERR_SHAPE, "gemm: negative size");
@@ -976,12 +977,12 @@ mdnn_status_t mdnn::gemm_mixed_ws(mdnn_layout_t layout, int64_t M, int64_t N, in
   const bool vb = aligned(B, 16) && ldb % 8 == 0;
   if (ab_type == MDNN_F16) {
     if (d_type == MDNN_F32)
-      return gemm_dispatch16<F16, F32>(layout, M, N, K, A, lda, va, B, ldb, vb, ep, ws, ws_bytes, st);
-    return gemm_dispatch16<F16, F16>(layout, M, N, K, A, lda, va, B, ldb, vb, ep, ws, ws_bytes, st);
+      return gemm_dispatch16<F16, F32>(layout, M, N, K, A, lda, va, B, ldb, vb, ep, ws, ws_bytes, st, ext_a, ext_b);
+    return gemm_dispatch16<F16, F16>(layout, M, N, K, A, lda, va, B, ldb, vb, ep, ws, ws_bytes, st, ext_a, ext_b);
   }
   if (d_type == MDNN_F32)
-    return gemm_dispatch16<BF16, F32>(layout, M, N, K, A, lda, va, B, ldb, vb, ep, ws, ws_bytes, st);
-  return gemm_dispatch16<BF16, BF16>(layout, M, N, K, A, lda, va, B, ldb, vb, ep, ws, ws_bytes, st);
+    return gemm_dispatch16<BF16, F32>(layout, M, N, K, A, lda, va, B, ldb, vb, ep, ws, ws_bytes, st, ext_a, ext_b);
+  return gemm_dispatch16<BF16, BF16>(layout, M, N, K, A, lda, va, B, ldb, vb, ep, ws, ws_bytes, st, ext_a, ext_b);
 }
 
 int mdnn::gemm_lp_splits(int64_t M, int64_t N, int64_t K) { return lp_split_plan(M, N, K, 128).splits; }

@@ -129,14 +129,17 @@ mdnn_status_t column_sums_partial_batch(const StripBatch& b, mdnn_dtype_t t, int
 // mdnn_gemm_mixed with an optional workspace (NULL / too small: same as
 // mdnn_gemm_mixed).  With one, fp32 problems whose grid would be a handful of
 // tiles over a long K split K across workgroups and reduce the fp32
-// partials in split order (deterministic) before the epilogue.
+// partials in split order (deterministic) before the epilogue.  ext_a, ext_b:
+// elements that rows of a 16-bit M- or N-contiguous operand have memory for
+// where those are more than M or N (0: not): a padded copy takes the pipelined
+// kernel whatever the size.
 size_t gemm_ws_bytes(mdnn_dtype_t ab_type, int64_t M, int64_t N, int64_t K);
 mdnn_status_t gemm_mixed_ws(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, float alpha, const void* A,
                             int64_t lda, const void* B, int64_t ldb, mdnn_dtype_t ab_type, float beta,
                             const void* C, int64_t ldc, void* D, int64_t ldd, mdnn_dtype_t d_type,
                             const float* bias, mdnn_act_t act, const void* mask_src, int64_t ldm, void* ws,
                             size_t ws_bytes, mdnn_stream_t stream, int32_t* nonfinite = nullptr,
-                            const float* alpha_dev = nullptr);
+                            const float* alpha_dev = nullptr, int64_t ext_a = 0, int64_t ext_b = 0);
 
 // K splits of a 16-bit product given a large enough workspace (1: none).
 int gemm_lp_splits(int64_t M, int64_t N, int64_t K);

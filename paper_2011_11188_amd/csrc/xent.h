@@ -2,6 +2,7 @@
 #pragma once
 
 #include "common.h"
+#include "internal.h"
 
 namespace mdnn {
 
@@ -17,5 +18,37 @@ __device__ __forceinline__ Pair join(Pair a, Pair b) {
   const float m = fmaxf(a.m, b.m), ref = pair_ref(m);
   return {m, a.s * __expf(a.m - ref) + b.s * __expf(b.m - ref)};
 }
+
+// What a tile of a piece's logits turns into in place of being stored.
+struct XentTile {
+  const float* bias;  // the piece's, or null
+  const int32_t* labels;
+  int32_t ignored;
+  int64_t n0, classes;  // the piece's first class; all classes
+  // forward: tile column t leaves a pair for each row at pairs[t * M + row], the label's column its logit
+  Pair* pairs;
+  float* zlab;
+  // backward: G times `scale` in the operands' type, rows of ldg elements (a multiple of 64), zeros in rows M .. rows - 1
+  // and columns past the piece; part: column sums of tile row t at part[t * classes + n0 + column], or null
+  const float* lse;
+  float scale;
+  void* g;
+  int64_t ldg, rows;
+  float* part;
+};
+
+// The products whose tiles end so (16-bit operands, x K-contiguous, W
+// K-contiguous or, w_kc false, class-contiguous), with the preconditions of the
+// pipelined kernel: K a multiple of 64, 16-byte aligned rows, an extent of
+// class-contiguous rows (ext, >= N) that is a multiple of 8.
+struct XentProduct {
+  const void *x, *w;
+  int64_t ldx, ldw, M, N, K, ext;
+  bool w_kc, backward;
+};
+// 256, 128 or 64: the side of the tiles, by the sizes.
+int xent_tile(int64_t M, int64_t N);
+template <class T>
+mdnn_status_t xent_tiles(const XentProduct& p, const XentTile& x, hipStream_t st);
 
 }  // namespace mdnn

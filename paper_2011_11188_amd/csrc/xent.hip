@@ -5,22 +5,36 @@
 //   G_ij = exp(z_ij - lse_i) - [j = label(i)]      (0 in ignored rows)
 //   dx = a G W^T,  dW = a x^T G,  db = a sum_i G_i,  a = S / counted rows
 //
-// The classes are taken in pieces.  Forward, a piece leaves each row's maximum
-// m and the sum of exp(z - m); the pairs of all pieces are joined at the end.
+// The classes are taken in pieces.  Forward, tiles of a piece leave each row's
+// maximum m and the sum of exp(z - m); the pairs of all tiles are joined.
 // Backward, lse is known, so a piece's G follows from its logits alone and goes
 // into the two products at once.
+//
+// Tiled (16 bits): the logits never leave the tile's registers (xent_pipe.h), and
+// all products run on the pipelined kernel.  Operands that it cannot read (sizes
+// that are no multiples of 64, rows off 16 bytes) are copied to padded rows, W by
+// pieces, where there are rows enough to pay for that.  Otherwise, and in fp32, a
+// piece's fp32 logits go through the workspace.
 //
 // In 16 bits G is stored as 2^15 G for fp16 (probabilities of 1e-5 are subnormal
 // there, those of 1e-8 nothing; times 2^15 the least normal one is 1.9e-9) and
 // G for bf16: one rounding of the same size as a result's own.  The factor a
 // comes after the products, in fp32, so the loss scale does not move G.
 #include <cmath>
+#include <type_traits>
 
 #include "gemm_core.h"
 #include "internal.h"
 #include "xent.h"
 
 namespace mdnn {
+
+int xent_tile(int64_t M, int64_t N) {
+  auto tiles = [&](int64_t side) { return ceil_div(M, side) * ceil_div(N, side); };
+  if (M > 128 && tiles(256) >= 256) return 256;
+  return M > 64 && tiles(128) >= 256 ? 128 : 64;
+}
+
 namespace {
 
 // ---------------------------------------------------------------- forward
@@ -35,9 +49,10 @@ xent_stats_kernel(const float* z, int64_t ldz, int64_t M, int64_t nc, int64_t n0
     const int64_t at = (int64_t)labels[row] - n0;
     Pair v = {-INFINITY, 0.0f};
     for (int64_t c = threadIdx.x * 4; c < nc; c += 1024) {
+      const float4_t q = *(const float4_t*)(p + c);  // (rows of whole quads)
       float e[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) e[k] = c + k < nc ? p[c + k] : -INFINITY;
+      for (int k = 0; k < 4; ++k) e[k] = c + k < nc ? q[k] : -INFINITY;
       float m = fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
       m = fmaxf(m, v.m);
       const float ref = pair_ref(m);
@@ -61,17 +76,20 @@ struct Tally {
   int64_t count;
 };
 
-// Pairs of all pieces to lse and the rows' losses: 64 rows a block, 16 groups
-// of pieces, joined in their order.  A block leaves its losses' sum and the
-// number of its rows that count; a single block writes the mean.
+// The pairs of a piece's tiles, and those of the pieces before it (`before`, or
+// null), joined: 64 rows a block, 16 groups of tiles, joined in their order.  To
+// `after` (which may be `before`) where more pieces follow, else to lse and the
+// rows' losses: a block leaves its losses' sum and the number of its rows that
+// count; a single block writes the mean.
 __global__ void __launch_bounds__(1024)
-xent_rows_kernel(const Pair* pairs, int64_t pieces, int64_t M, int64_t N, const float* zlab, const int32_t* labels,
+xent_rows_kernel(const Pair* pairs, int64_t pieces, const Pair* before, Pair* after, int64_t M, int64_t N, const float* zlab, const int32_t* labels,
                  int32_t ignored, float* lse, float* row_loss, float* loss, Tally* tally) {
   __shared__ Pair buf[16][64];
   const int r = threadIdx.x & 63, g = threadIdx.x >> 6;
   const int64_t row = (int64_t)blockIdx.x * 64 + r, at = row < M ? row : M - 1;
   const int64_t per = ceil_div(pieces, 16), p0 = g * per, p1 = p0 + per < pieces ? p0 + per : pieces;
   Pair v = {-INFINITY, 0.0f};
+  if (before && g == 0) v = before[at];
   for (int64_t p = p0; p < p1; p += 8) {
     Pair u[8];
 #pragma unroll
@@ -85,6 +103,10 @@ xent_rows_kernel(const Pair* pairs, int64_t pieces, int64_t M, int64_t N, const 
   if (g > 0) return;
 #pragma unroll
   for (int k = 1; k < 16; ++k) v = join(v, buf[k][r]);
+  if (after) {
+    if (row < M) after[row] = v;
+    return;
+  }
   Tally t = {0.0, 0};
   if (row < M) {
     const float l = v.m + logf(v.s);
@@ -125,6 +147,43 @@ __global__ void __launch_bounds__(1024) xent_mean_kernel(const Tally* tally, int
 
 // --------------------------------------------------------------- backward
 
+typedef uint32_t chunk_a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t chunk_a4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// 16 bytes of a row from element c on, at any element address; zeros from
+// element `cols` on.
+template <class S>
+__device__ __forceinline__ uint4 chunk16(const S* row, int64_t c, int64_t cols) {
+  typedef std::conditional_t<sizeof(S) == 2, chunk_a2, chunk_a4> V;
+  constexpr int E = 16 / sizeof(S);
+  if (c + E <= cols) {
+    const V v = *(const __attribute__((address_space(1))) V*)(row + c);
+    return make_uint4(v.x, v.y, v.z, v.w);
+  }
+  struct {
+    S e[E];
+  } v;
+#pragma unroll
+  for (int k = 0; k < E; ++k) v.e[k] = c + k < cols ? row[c + k] : (S)0;
+  return __builtin_bit_cast(uint4, v);
+}
+
+// [rows][cols] of 16-bit elements at any address to rows of ldc (a multiple of
+// 8), zeros past cols and in rows .. all - 1.
+__global__ void __launch_bounds__(256)
+xent_pack_kernel(const uint16_t* src, int64_t ld, int64_t rows, int64_t cols, uint16_t* dst, int64_t all, int64_t ldc) {
+  const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
+  if (c >= ldc) return;
+  for (int64_t r0 = ((int64_t)blockIdx.y * 4 + (threadIdx.x >> 6)) * 4; r0 < all; r0 += (int64_t)gridDim.y * 16) {
+    uint4 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = r0 + k < rows ? chunk16(src + (r0 + k) * ld, c, cols) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (r0 + k < all) *(uint4*)(dst + (r0 + k) * ldc + c) = v[k];
+  }
+}
+
 // Block 0 counts the rows with a label that is not ignored and leaves
 // a = S / count, times `scale`; the others copy x to rows of ldc elements,
 // ignored rows, rows past M and columns past K as zeros (what an ignored row
@@ -160,41 +219,54 @@ xent_prepare_kernel(const typename T::storage* x, int64_t ldx, int64_t M, int64_
     const bool live = row < M && labels[row < M ? row : 0] != ignored;
     const typename T::storage* p = x + row * ldx;
     for (int64_t c = threadIdx.x; c < per; c += 256) {
-      typename T::storage v[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = live && c * E + e < K ? p[c * E + e] : (typename T::storage)0;
-      *(uint4*)(copy + row * ldc + c * E) = __builtin_bit_cast(uint4, v);
+      *(uint4*)(copy + row * ldc + c * E) = live ? chunk16(p, c * E, K) : make_uint4(0, 0, 0, 0);
     }
   }
 }
 
 // Logits of a piece to G (type T, rows of ldg elements; z and G may be the
-// same memory in fp32): 32 rows a block, four columns a thread.  Rows past M and
-// columns past nc become zeros.  part: the block's column sums, or null.
+// same memory in fp32): 32 rows a block, four columns a thread, four rows in
+// flight.  Rows past M and columns past nc become zeros.  part: the block's
+// column sums, or null.
 template <class T>
 __global__ void __launch_bounds__(256)
-xent_grad_kernel(const float* z, int64_t ldz, int64_t M, int64_t rows, int64_t nc, int64_t n0, const int32_t* labels,
-                 int32_t ignored, int64_t N, const float* lse, float scale, typename T::storage* g, int64_t ldg,
-                 float* part) {
+xent_grad_kernel(const float* z, int64_t M, int64_t rows, int64_t nc, int64_t n0, const int32_t* labels, int32_t ignored,
+                 int64_t N, const float* lse, float scale, typename T::storage* g, int64_t ldg, float* part) {
+  typedef typename T::storage S;
   const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= ldg) return;
   for (int64_t b = blockIdx.y; b * 32 < rows; b += gridDim.y) {
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     const int64_t r1 = b * 32 + 32 < rows ? b * 32 + 32 : rows;
-    for (int64_t r = b * 32; r < r1; ++r) {
-      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      const int32_t label = r < M ? labels[r] : ignored;
-      if (r < M && label != ignored) {
-        const float l = label >= 0 && label < N ? lse[r] : __builtin_nanf("");
-        const int64_t at = (int64_t)label - n0 - c;
+    for (int64_t r0 = b * 32; r0 < r1; r0 += 4) {
+      float4_t q[4];
+      int32_t label[4];
+      float l[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (c + e < nc) v[e] = __expf(z[r * ldz + c + e] - l) - (e == at ? 1.0f : 0.0f);
+      for (int k = 0; k < 4; ++k) {
+        const int64_t r = r0 + k < M ? r0 + k : M - 1;
+        q[k] = *(const float4_t*)(z + r * ldg + c);
+        label[k] = labels[r], l[k] = lse[r];
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        sum[e] += v[e];
-        if (c + e < ldg) g[r * ldg + c + e] = from_f<T>(v[e] * scale);
+      for (int k = 0; k < 4; ++k) {
+        if (r0 + k >= r1) break;
+        const bool live = r0 + k < M && label[k] != ignored;
+        const float at_l = label[k] >= 0 && label[k] < N ? l[k] : __builtin_nanf("");
+        const int64_t at = (int64_t)label[k] - n0 - c;
+        S o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float v = __expf(q[k][e] - at_l) - (e == at ? 1.0f : 0.0f);
+          v = live && c + e < nc ? v : 0.0f;
+          sum[e] += v;
+          o[e] = from_f<T>(v * scale);
+        }
+        S* d = g + (r0 + k) * ldg + c;
+        if constexpr (sizeof(S) == 2)
+          *(uint2*)d = make_uint2((uint32_t)o[0] | ((uint32_t)o[1] << 16), (uint32_t)o[2] | ((uint32_t)o[3] << 16));
+        else
+          *(float4_t*)d = (float4_t){o[0], o[1], o[2], o[3]};
       }
     }
     if (part) {
@@ -205,20 +277,25 @@ xent_grad_kernel(const float* z, int64_t ldz, int64_t M, int64_t rows, int64_t n
   }
 }
 
-// db from the row blocks' column sums, in their order.
+// db from the row blocks' column sums: 64 columns a block, four groups of row
+// blocks (eight loads in flight), joined in their order.
 __global__ void __launch_bounds__(256)
-xent_db_kernel(const float* part, int64_t blocks, int64_t N, const float* alpha, float scale, float* db) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= N) return;
+xent_db_kernel(const float* part, int64_t blocks, int64_t ldp, int64_t cols, const float* alpha, float scale, float* db) {
+  __shared__ double buf[4][64];
+  const int cx = threadIdx.x & 63, r = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + cx, at = c < cols ? c : cols - 1;
+  const int64_t per = ceil_div(blocks, 4), b1 = (r + 1) * per < blocks ? (r + 1) * per : blocks;
   double s = 0.0;
-  for (int64_t b = 0; b < blocks; b += 8) {
+  for (int64_t b = r * per; b < b1; b += 8) {
     float v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = b + k < blocks ? part[(b + k) * N + c] : 0.0f;
+    for (int k = 0; k < 8; ++k) v[k] = part[(b + k < b1 ? b + k : b) * ldp + at];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s += (double)v[k];
+    for (int k = 0; k < 8; ++k) s += b + k < b1 ? (double)v[k] : 0.0;
   }
-  db[c] = (float)s * (*alpha * scale);
+  buf[r][cx] = s;
+  __syncthreads();
+  if (r == 0 && c < cols) db[c] = (float)(((buf[0][cx] + buf[1][cx]) + buf[2][cx]) + buf[3][cx]) * (*alpha * scale);
 }
 
 template <class T>
@@ -231,69 +308,134 @@ xent_round_kernel(const float* src, int64_t rows, int64_t cols, typename T::stor
 
 // ------------------------------------------------------------------- plans
 
-size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
+int64_t up(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
 
-// Classes of a piece: as many as `bytes` of M rows hold, in whole multiples of
-// 256, at least one.
-int64_t piece_classes(int64_t M, int64_t N, size_t elem, size_t bytes) {
-  int64_t nc = (int64_t)(bytes / elem) / M / 256 * 256;
-  nc = nc < 256 ? 256 : nc;
-  return nc < N ? nc : N;
+// Classes of a piece: as many as `elems` elements of `rows` a class hold, in
+// whole multiples of 256, at least one.
+int64_t piece_classes(int64_t N, int64_t rows, int64_t elems) {
+  const int64_t nc = elems / rows / 256 * 256;
+  return nc < 256 ? (N < 256 ? N : 256) : nc < N ? nc : N;
 }
 
-struct FwdPlan {
-  int64_t nc, pieces, blocks;
-  size_t pairs, zlab, tally, z, gemm, gemm_bytes, bytes;
-};
-FwdPlan fwd_plan(int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
-  FwdPlan p;
-  p.nc = piece_classes(M, N, 4, (size_t)64 << 20);
-  p.pieces = ceil_div(N, p.nc);
-  p.blocks = ceil_div(M, 64);
+// How a call runs.  By the sizes alone it may run tiled (TILED: operands as
+// they are; PACKED: copies in the workspace) or general; the caller's workspace
+// holds any that its sizes allow.
+enum Way { GENERAL, TILED, PACKED };
+
+// Rows from which copying W pays (two passes over it at memory speed against
+// products at about twice the register-staged kernel's rate).
+bool pack_pays(int64_t M, bool backward) { return M >= (backward ? 256 : 512); }
+
+Way way_by_size(int64_t M, int64_t N, int64_t K, mdnn_dtype_t t, bool backward) {
+  if (t == MDNN_F32 || M * up(K, 64) >= (int64_t)1 << 31) return GENERAL;  // (32-bit offsets reach every row of x)
+  if (N % 64 == 0 && K % 64 == 0) return TILED;
+  if (!backward && K % 64 == 0 && N % 8 == 0) return TILED;
+  return pack_pays(M, backward) ? PACKED : GENERAL;
+}
+
+struct Space {
   size_t at = 0;
-  auto take = [&](size_t n) { const size_t o = at; at += pad256(n); return o; };
-  p.pairs = take((size_t)p.pieces * M * sizeof(Pair));
-  p.zlab = take((size_t)M * 4);
-  p.tally = take((size_t)p.blocks * sizeof(Tally));
-  p.z = take((size_t)M * p.nc * 4);
-  const size_t a = gemm_ws_bytes(t, M, p.nc, K), b = gemm_ws_bytes(t, M, N - (p.pieces - 1) * p.nc, K);
-  p.gemm_bytes = a > b ? a : b;
-  p.gemm = take(p.gemm_bytes);
-  p.bytes = at;
+  size_t take(size_t n) {
+    const size_t o = at;
+    at += (n + 255) / 256 * 256;
+    return o;
+  }
+};
+
+struct FwdPlan {
+  int64_t nc, pieces, blocks, kc, ldw;
+  size_t pairs, run, zlab, tally, z, copy, pack, gemm, gemm_bytes, bytes;
+};
+FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
+  FwdPlan p = {};
+  Space s;
+  p.blocks = ceil_div(M, 64);
+  p.kc = up(K, 64);
+  if (way == GENERAL) {
+    p.nc = piece_classes(N, M, (int64_t)16 << 20);
+  } else {
+    p.nc = piece_classes(N, ceil_div(M, 64), (int64_t)32 << 20);  // pairs of 64 columns at least
+    if (way == PACKED) {
+      const int64_t most = piece_classes(N, p.kc, (int64_t)128 << 20);
+      p.nc = p.nc < most ? p.nc : most;
+    }
+  }
+  p.pieces = ceil_div(N, p.nc);
+  const int64_t last = N - (p.pieces - 1) * p.nc;
+  int64_t tiles = 1;
+  if (way != GENERAL)
+    for (int64_t n : {p.nc, last}) {
+      const int64_t k = ceil_div(n, xent_tile(M, n));
+      tiles = k > tiles ? k : tiles;
+    }
+  p.pairs = s.take((size_t)tiles * M * sizeof(Pair));
+  p.run = s.take(p.pieces > 1 ? (size_t)M * sizeof(Pair) : 0);
+  p.zlab = s.take((size_t)M * 4);
+  p.tally = s.take((size_t)p.blocks * sizeof(Tally));
+  if (way == GENERAL) {
+    p.z = s.take((size_t)M * up(p.nc, 4) * 4);
+    const size_t a = gemm_ws_bytes(t, M, p.nc, K), b = gemm_ws_bytes(t, M, last, K);
+    p.gemm_bytes = a > b ? a : b;
+    p.gemm = s.take(p.gemm_bytes);
+  } else {
+    p.copy = s.take((size_t)M * p.kc * 2);  // x, where its rows are not as the tiles read them
+    p.ldw = layout == MDNN_NN ? up(p.nc, 64) : p.kc;
+    p.pack = s.take(way == PACKED ? (size_t)(layout == MDNN_NN ? p.kc : up(p.nc, 64)) * p.ldw * 2 : 0);
+  }
+  p.bytes = s.at;
   return p;
 }
 
 struct BwdPlan {
-  int64_t nc, pieces, rows, kc, ldg, blocks;
-  size_t alpha, copy, z, g, part, acc, gemm, gemm_bytes, bytes;
+  int64_t nc, pieces, rows, kc, ldg, blocks, ldw;
+  size_t alpha, copy, z, g, part, acc, pack, gemm, gemm_bytes, bytes;
 };
-BwdPlan bwd_plan(int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
-  BwdPlan p;
+BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
+  BwdPlan p = {};
+  Space s;
   const bool h = t != MDNN_F32;
   const size_t es = dtype_size(t);
-  p.nc = piece_classes(M, N, 4, (size_t)256 << 20);
+  p.rows = h ? up(M, 64) : M;
+  p.kc = h ? up(K, 64) : up(K, 4);
+  p.nc = piece_classes(N, way == GENERAL ? M : p.rows, (way == GENERAL ? (int64_t)32 : (int64_t)128) << 20);
+  if (way == PACKED) {
+    const int64_t most = piece_classes(N, p.kc, (int64_t)128 << 20);
+    p.nc = p.nc < most ? p.nc : most;
+  }
   p.pieces = ceil_div(N, p.nc);
-  p.rows = h ? ceil_div(M, 64) * 64 : M;
-  p.kc = h ? ceil_div(K, 8) * 8 : ceil_div(K, 4) * 4;
-  p.ldg = h ? ceil_div(p.nc, 64) * 64 : ceil_div(p.nc, 4) * 4;
-  p.blocks = ceil_div(p.rows, 32);  // (of xent_grad_kernel, padding rows too)
-  size_t at = 0;
-  auto take = [&](size_t n) { const size_t o = at; at += pad256(n); return o; };
-  p.alpha = take(4);
-  p.copy = take((size_t)p.rows * p.kc * es);
-  p.z = take((size_t)M * p.ldg * 4);
-  p.g = h ? take((size_t)p.rows * p.ldg * 2) : p.z;
-  p.part = take((size_t)p.blocks * N * 4);
-  p.acc = take(h && p.pieces > 1 ? (size_t)M * K * 4 : 0);
+  p.ldg = up(p.nc, h ? 64 : 4);
   const int64_t last = N - (p.pieces - 1) * p.nc;
-  p.gemm_bytes = 0;
+  // row blocks that leave column sums
+  p.blocks = ceil_div(p.rows, 32);
+  if (way != GENERAL) {
+    p.blocks = 1;
+    for (int64_t n : {p.nc, last}) {
+      const int64_t b = ceil_div(M, xent_tile(M, n));
+      p.blocks = b > p.blocks ? b : p.blocks;
+    }
+  }
+  p.alpha = s.take(4);
+  p.copy = s.take((size_t)p.rows * p.kc * es);
+  if (way == GENERAL) p.z = s.take((size_t)M * p.ldg * 4);
+  p.g = h ? s.take((size_t)p.rows * p.ldg * 2) : p.z;
+  p.part = s.take((size_t)p.blocks * N * 4);
+  p.acc = s.take(h && p.pieces > 1 ? (size_t)M * K * 4 : 0);
+  p.ldw = layout == MDNN_NN ? p.ldg : p.kc;
+  p.pack = s.take(way == PACKED ? (size_t)(layout == MDNN_NN ? p.kc : p.ldg) * p.ldw * 2 : 0);
   for (int64_t n : {p.nc, last})
-    for (size_t b : {gemm_ws_bytes(t, M, n, K), gemm_ws_bytes(t, M, K, n), gemm_ws_bytes(t, n, K, p.rows),
-                     gemm_ws_bytes(t, K, n, p.rows)})
+    for (size_t b : {gemm_ws_bytes(t, M, n, K), gemm_ws_bytes(t, M, K, n), gemm_ws_bytes(t, M, K, up(n, 64)),
+                     gemm_ws_bytes(t, n, K, p.rows), gemm_ws_bytes(t, K, n, p.rows)})
       p.gemm_bytes = b > p.gemm_bytes ? b : p.gemm_bytes;
-  p.gemm = take(p.gemm_bytes);
-  p.bytes = at;
+  p.gemm = s.take(p.gemm_bytes);
+  p.bytes = s.at;
   return p;
+}
+
+// Whether the tiles read W as it is: rows on 16 bytes, 32-bit offsets over a
+// piece's rows.
+bool w_fits(mdnn_layout_t layout, const void* w, int64_t ldw, int64_t nc) {
+  return aligned(w, 16) && ldw % 8 == 0 &&
+         (layout == MDNN_NN ? 64 * ldw + nc : (nc + 255) * ldw) < (int64_t)1 << 31;
 }
 
 constexpr int64_t MAX_ROWS = (int64_t)1 << 24, MAX_N = 0x7fffffff;
@@ -326,15 +468,92 @@ const void* w_piece(mdnn_layout_t layout, const void* w, int64_t ldw, int64_t n0
 
 unsigned capped(int64_t n, int64_t most) { return (unsigned)(n < most ? n : most); }
 
+mdnn_status_t pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t all, int64_t ldc,
+                   hipStream_t st) {
+  hipLaunchKernelGGL(xent_pack_kernel, dim3((unsigned)ceil_div(ldc, 512), capped(ceil_div(all, 16), 65535)), dim3(256), 0,
+                     st, (const uint16_t*)src, ld, rows, cols, (uint16_t*)dst, all, ldc);
+  return check_launch("xent_pack_kernel");
+}
+
+// Classes n0 .. n0 + nc - 1 of W as the tiles read them: in place, or copied to
+// rows of ldc, zeros past the sizes (the depth to kc, classes to a multiple of 64).
+struct Piece {
+  const void* w;
+  int64_t ldw, ext;  // ext: classes that class-contiguous rows have memory for
+};
+mdnn_status_t take_piece(Way way, mdnn_layout_t layout, const void* w, int64_t ldw, int64_t n0, int64_t nc, int64_t K,
+                         int64_t kc, void* room, int64_t ldc, Piece& out, hipStream_t st) {
+  const void* p = w_piece(layout, w, ldw, n0, 2);
+  if (way != PACKED) {
+    out = {p, ldw, nc};
+    return MDNN_SUCCESS;
+  }
+  const int64_t all = up(nc, 64);
+  out = {room, ldc, all};
+  return layout == MDNN_NN ? pack(p, ldw, K, nc, room, kc, ldc, st) : pack(p, ldw, nc, K, room, all, ldc, st);
+}
+
 template <class T>
-mdnn_status_t run_bwd(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* w,
-                      int64_t ldw, const float* bias, const int32_t* labels, int32_t ignored, const float* lse,
-                      const float* loss_scale, void* dx, int64_t lddx, void* dw, int64_t lddw, mdnn_dtype_t dw_type,
-                      float* db, char* ws, hipStream_t st) {
+mdnn_status_t tiles(const XentProduct& p, const XentTile& x, hipStream_t st) {
+  if constexpr (T::id != MDNN_F32)
+    return xent_tiles<T>(p, x, st);
+  else
+    return fail(MDNN_ERR_STATE, "linear_xent: no tiles in fp32");
+}
+
+template <class T>
+mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx,
+                      const void* w, int64_t ldw, const float* bias, const int32_t* labels, int32_t ignored, float* loss,
+                      float* row_loss, float* lse, char* ws, hipStream_t st) {
+  const mdnn_dtype_t t = T::id;
+  const FwdPlan p = fwd_plan(way, layout, M, N, K, t);
+  Pair *pairs = (Pair*)(ws + p.pairs), *run = (Pair*)(ws + p.run);
+  float *zlab = (float*)(ws + p.zlab), *z = (float*)(ws + p.z);
+  Tally* tally = (Tally*)(ws + p.tally);
+  if (way != GENERAL && !(aligned(x, 16) && ldx % 8 == 0 && K % 64 == 0 && (M + 255) * ldx < (int64_t)1 << 31)) {
+    MDNN_TRY(pack(x, ldx, M, K, ws + p.copy, M, p.kc, st));
+    x = ws + p.copy, ldx = p.kc;
+  }
+  for (int64_t i = 0; i < p.pieces; ++i) {
+    const int64_t n0 = i * p.nc, nc = n0 + p.nc < N ? p.nc : N - n0;
+    const float* b = bias ? bias + n0 : nullptr;
+    int64_t n = 1;
+    if (way == GENERAL) {
+      const int64_t ldz = up(p.nc, 4);
+      MDNN_TRY(gemm_mixed_ws(layout, M, nc, K, 1.0f, x, ldx, w_piece(layout, w, ldw, n0, dtype_size(t)), ldw, t, 0.0f,
+                             nullptr, 0, z, ldz, MDNN_F32, b, MDNN_ACT_NONE, nullptr, 0, ws + p.gemm, p.gemm_bytes, st));
+      hipLaunchKernelGGL(xent_stats_kernel, dim3(capped(M, 1 << 20)), dim3(256), 0, st, z, ldz, M, nc, n0, labels, pairs,
+                         zlab);
+      MDNN_TRY(check_launch("xent_stats_kernel"));
+    } else {
+      Piece q;
+      MDNN_TRY(take_piece(way, layout, w, ldw, n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
+      XentProduct a = {x, q.w, ldx, q.ldw, M, nc, p.kc, q.ext, layout == MDNN_NT, false};
+      XentTile e = {};
+      e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.pairs = pairs, e.zlab = zlab;
+      MDNN_TRY(tiles<T>(a, e, st));
+      n = ceil_div(nc, xent_tile(M, nc));
+    }
+    hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)p.blocks), dim3(1024), 0, st, pairs, n, i > 0 ? run : nullptr,
+                       i + 1 < p.pieces ? run : nullptr, M, N, zlab, labels, ignored, lse, row_loss, loss, tally);
+    MDNN_TRY(check_launch("xent_rows_kernel"));
+  }
+  if (loss && p.blocks > 1) {
+    hipLaunchKernelGGL(xent_mean_kernel, dim3(1), dim3(1024), 0, st, tally, p.blocks, loss);
+    MDNN_TRY(check_launch("xent_mean_kernel"));
+  }
+  return MDNN_SUCCESS;
+}
+
+template <class T>
+mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx,
+                      const void* w, int64_t ldw, const float* bias, const int32_t* labels, int32_t ignored,
+                      const float* lse, const float* loss_scale, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                      mdnn_dtype_t dw_type, float* db, char* ws, hipStream_t st) {
   typedef typename T::storage S;
   constexpr bool H = sizeof(S) == 2;
   const mdnn_dtype_t t = T::id;
-  const BwdPlan p = bwd_plan(M, N, K, t);
+  const BwdPlan p = bwd_plan(way, layout, M, N, K, t);
   const float scale = t == MDNN_F16 ? 32768.0f : 1.0f;
   float* alpha = (float*)(ws + p.alpha);
   S* copy = (S*)(ws + p.copy);
@@ -349,41 +568,55 @@ mdnn_status_t run_bwd(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, con
   MDNN_TRY(check_launch("xent_prepare_kernel"));
   for (int64_t n0 = 0; n0 < N; n0 += p.nc) {
     const int64_t nc = n0 + p.nc < N ? p.nc : N - n0;
-    const void* wp = w_piece(layout, w, ldw, n0, sizeof(S));
-    MDNN_TRY(gemm_mixed_ws(layout, M, nc, K, 1.0f, copy, p.kc, wp, ldw, t, 0.0f, nullptr, 0, z, p.ldg, MDNN_F32,
-                           bias ? bias + n0 : nullptr, MDNN_ACT_NONE, nullptr, 0, gw, p.gemm_bytes, st));
-    hipLaunchKernelGGL((xent_grad_kernel<T>), dim3((unsigned)ceil_div(p.ldg, 1024), capped(ceil_div(p.rows, 32), 65535)),
-                       dim3(256), 0, st, z, p.ldg, M, p.rows, nc, n0, labels, ignored, N, lse, scale, g, p.ldg, part);
-    MDNN_TRY(check_launch("xent_grad_kernel"));
+    const float* b = bias ? bias + n0 : nullptr;
+    Piece q = {w_piece(layout, w, ldw, n0, sizeof(S)), ldw, nc};
+    int64_t blocks = p.blocks;
+    if (way == GENERAL) {
+      MDNN_TRY(gemm_mixed_ws(layout, M, nc, K, 1.0f, copy, p.kc, q.w, ldw, t, 0.0f, nullptr, 0, z, p.ldg, MDNN_F32, b,
+                             MDNN_ACT_NONE, nullptr, 0, gw, p.gemm_bytes, st));
+      hipLaunchKernelGGL((xent_grad_kernel<T>),
+                         dim3((unsigned)ceil_div(p.ldg, 1024), capped(ceil_div(p.rows, 32), 65535)), dim3(256), 0, st, z, M,
+                         p.rows, nc, n0, labels, ignored, N, lse, scale, g, p.ldg, part);
+      MDNN_TRY(check_launch("xent_grad_kernel"));
+    } else {
+      MDNN_TRY(take_piece(way, layout, w, ldw, n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
+      XentProduct a = {copy, q.w, p.kc, q.ldw, M, nc, p.kc, q.ext, layout == MDNN_NT, true};
+      XentTile e = {};
+      e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.lse = lse, e.scale = scale;
+      e.g = g, e.ldg = p.ldg, e.rows = p.rows, e.part = part;
+      MDNN_TRY(tiles<T>(a, e, st));
+      blocks = ceil_div(M, xent_tile(M, nc));
+    }
+    if (db) {
+      hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(nc, 64)), dim3(256), 0, st, part + n0, blocks, N, nc, alpha,
+                         scale, db + n0);
+      MDNN_TRY(check_launch("xent_db_kernel"));
+    }
     if (dx) {
       const mdnn_layout_t back = layout == MDNN_NN ? MDNN_NT : MDNN_NN;
       void* d = joined ? (void*)acc : dx;
       const int64_t ldd = joined ? K : lddx;
-      MDNN_TRY(gemm_mixed_ws(back, M, K, nc, 1.0f, g, p.ldg, wp, ldw, t, n0 > 0 ? 1.0f : 0.0f, d, ldd, d, ldd,
-                             joined ? MDNN_F32 : t, nullptr, MDNN_ACT_NONE, nullptr, 0, gw, p.gemm_bytes, st, nullptr,
-                             alpha));
+      // (a copied piece's padding is zeros on both sides: whole steps)
+      MDNN_TRY(gemm_mixed_ws(back, M, K, way == PACKED ? up(nc, 64) : nc, 1.0f, g, p.ldg, q.w, q.ldw, t,
+                             n0 > 0 ? 1.0f : 0.0f, d, ldd, d, ldd, joined ? MDNN_F32 : t, nullptr, MDNN_ACT_NONE, nullptr,
+                             0, gw, p.gemm_bytes, st, nullptr, alpha, 0, way == PACKED ? p.kc : 0));
     }
     if (dw) {
       const size_t ds = dtype_size(dw_type);
       if (layout == MDNN_NN)
         MDNN_TRY(gemm_mixed_ws(MDNN_TN, K, nc, p.rows, 1.0f, copy, p.kc, g, p.ldg, t, 0.0f, nullptr, 0,
                                (char*)dw + n0 * ds, lddw, dw_type, nullptr, MDNN_ACT_NONE, nullptr, 0, gw, p.gemm_bytes,
-                               st, nullptr, alpha));
+                               st, nullptr, alpha, p.kc, up(nc, 8)));
       else
         MDNN_TRY(gemm_mixed_ws(MDNN_TN, nc, K, p.rows, 1.0f, g, p.ldg, copy, p.kc, t, 0.0f, nullptr, 0,
                                (char*)dw + n0 * lddw * ds, lddw, dw_type, nullptr, MDNN_ACT_NONE, nullptr, 0, gw,
-                               p.gemm_bytes, st, nullptr, alpha));
+                               p.gemm_bytes, st, nullptr, alpha, up(nc, 8), p.kc));
     }
   }
   if (dx && joined) {
     hipLaunchKernelGGL((xent_round_kernel<T>), dim3(capped(ceil_div(K, 256), 1024), capped(M, 65535)), dim3(256), 0, st,
                        acc, M, K, (S*)dx, lddx);
     MDNN_TRY(check_launch("xent_round_kernel"));
-  }
-  if (db) {
-    hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(N, 256)), dim3(256), 0, st, part, p.blocks, N, alpha,
-                       scale, db);
-    MDNN_TRY(check_launch("xent_db_kernel"));
   }
   return MDNN_SUCCESS;
 }
@@ -393,10 +626,21 @@ mdnn_status_t run_bwd(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, con
 
 using namespace mdnn;
 
+static size_t fwd_bytes(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
+  const Way way = way_by_size(M, N, K, t, false);
+  const size_t a = fwd_plan(way, layout, M, N, K, t).bytes, b = way == TILED ? fwd_plan(GENERAL, layout, M, N, K, t).bytes : 0;
+  return a > b ? a : b;
+}
+static size_t bwd_bytes(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
+  const Way way = way_by_size(M, N, K, t, true);
+  const size_t a = bwd_plan(way, layout, M, N, K, t).bytes, b = way == TILED ? bwd_plan(GENERAL, layout, M, N, K, t).bytes : 0;
+  return a > b ? a : b;
+}
+
 extern "C" size_t mdnn_linear_xent_fwd_workspace(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
                                                  mdnn_dtype_t dtype) {
   if ((layout != MDNN_NN && layout != MDNN_NT) || !sizes_ok(M, N, K) || !dtype_ok(dtype) || M == 0) return 0;
-  return fwd_plan(M, N, K, dtype).bytes;
+  return fwd_bytes(layout, M, N, K, dtype);
 }
 
 extern "C" mdnn_status_t mdnn_linear_xent_fwd(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, const void* x,
@@ -412,36 +656,26 @@ extern "C" mdnn_status_t mdnn_linear_xent_fwd(mdnn_layout_t layout, int64_t M, i
   clear_error();
   if (M == 0) return loss ? fill_zero(loss, 4, st) : MDNN_SUCCESS;
   if (!loss && !row_loss && !lse) return MDNN_SUCCESS;
-  const FwdPlan p = fwd_plan(M, N, K, dtype);
-  if (!workspace || ws_bytes < p.bytes || !aligned(workspace, 256))
-    return fail(MDNN_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) required", who, p.bytes);
+  const size_t need = fwd_bytes(layout, M, N, K, dtype);
+  if (!workspace || ws_bytes < need || !aligned(workspace, 256))
+    return fail(MDNN_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) required", who, need);
+  Way way = way_by_size(M, N, K, dtype, false);
+  if (way == TILED && !w_fits(layout, w, ldw, fwd_plan(TILED, layout, M, N, K, dtype).nc)) way = GENERAL;
   char* ws = (char*)workspace;
-  Pair* pairs = (Pair*)(ws + p.pairs);
-  float *zlab = (float*)(ws + p.zlab), *z = (float*)(ws + p.z);
-  Tally* tally = (Tally*)(ws + p.tally);
-  for (int64_t i = 0; i < p.pieces; ++i) {
-    const int64_t n0 = i * p.nc, nc = n0 + p.nc < N ? p.nc : N - n0;
-    MDNN_TRY(gemm_mixed_ws(layout, M, nc, K, 1.0f, x, ldx, w_piece(layout, w, ldw, n0, dtype_size(dtype)), ldw, dtype,
-                           0.0f, nullptr, 0, z, p.nc, MDNN_F32, bias ? bias + n0 : nullptr, MDNN_ACT_NONE, nullptr, 0,
-                           ws + p.gemm, p.gemm_bytes, stream));
-    hipLaunchKernelGGL(xent_stats_kernel, dim3(capped(M, 1 << 20)), dim3(256), 0, st, z, p.nc, M, nc, n0, labels,
-                       pairs + i * M, zlab);
-    MDNN_TRY(check_launch("xent_stats_kernel"));
+  switch (dtype) {
+    case MDNN_F32:
+      return run_fwd<F32>(way, layout, M, N, K, x, ldx, w, ldw, bias, labels, ignored, loss, row_loss, lse, ws, st);
+    case MDNN_F16:
+      return run_fwd<F16>(way, layout, M, N, K, x, ldx, w, ldw, bias, labels, ignored, loss, row_loss, lse, ws, st);
+    default:
+      return run_fwd<BF16>(way, layout, M, N, K, x, ldx, w, ldw, bias, labels, ignored, loss, row_loss, lse, ws, st);
   }
-  hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)p.blocks), dim3(1024), 0, st, pairs, p.pieces, M, N, zlab, labels,
-                     ignored, lse, row_loss, loss, tally);
-  MDNN_TRY(check_launch("xent_rows_kernel"));
-  if (loss && p.blocks > 1) {
-    hipLaunchKernelGGL(xent_mean_kernel, dim3(1), dim3(1024), 0, st, tally, p.blocks, loss);
-    MDNN_TRY(check_launch("xent_mean_kernel"));
-  }
-  return MDNN_SUCCESS;
 }
 
 extern "C" size_t mdnn_linear_xent_bwd_workspace(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
                                                  mdnn_dtype_t dtype) {
   if ((layout != MDNN_NN && layout != MDNN_NT) || !sizes_ok(M, N, K) || !dtype_ok(dtype) || M == 0) return 0;
-  return bwd_plan(M, N, K, dtype).bytes;
+  return bwd_bytes(layout, M, N, K, dtype);
 }
 
 extern "C" mdnn_status_t mdnn_linear_xent_bwd(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, const void* x,
@@ -472,20 +706,22 @@ extern "C" mdnn_status_t mdnn_linear_xent_bwd(mdnn_layout_t layout, int64_t M, i
   if (dx && lddx < K) return fail(MDNN_ERR_LAYOUT, "%s: leading dimension below the width", who);
   if (!aligned(lse, 4) || !aligned(loss_scale, 4) || (dx && !aligned(dx, dtype_size(dtype))))
     return fail(MDNN_ERR_MISALIGNED, "%s: misaligned buffer", who);
-  const size_t need = bwd_plan(M, N, K, dtype).bytes;
+  const size_t need = bwd_bytes(layout, M, N, K, dtype);
   if (!workspace || ws_bytes < need || !aligned(workspace, 256))
     return fail(MDNN_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) required", who, need);
   clear_error();
+  Way way = way_by_size(M, N, K, dtype, true);
+  if (way == TILED && !w_fits(layout, w, ldw, bwd_plan(TILED, layout, M, N, K, dtype).nc)) way = GENERAL;
   char* ws = (char*)workspace;
   switch (dtype) {
     case MDNN_F32:
-      return run_bwd<F32>(layout, M, N, K, x, ldx, w, ldw, bias, labels, ignored, lse, loss_scale, dx, lddx, dw, lddw,
+      return run_bwd<F32>(way, layout, M, N, K, x, ldx, w, ldw, bias, labels, ignored, lse, loss_scale, dx, lddx, dw, lddw,
                           dw_type, db, ws, st);
     case MDNN_F16:
-      return run_bwd<F16>(layout, M, N, K, x, ldx, w, ldw, bias, labels, ignored, lse, loss_scale, dx, lddx, dw, lddw,
+      return run_bwd<F16>(way, layout, M, N, K, x, ldx, w, ldw, bias, labels, ignored, lse, loss_scale, dx, lddx, dw, lddw,
                           dw_type, db, ws, st);
     default:
-      return run_bwd<BF16>(layout, M, N, K, x, ldx, w, ldw, bias, labels, ignored, lse, loss_scale, dx, lddx, dw, lddw,
+      return run_bwd<BF16>(way, layout, M, N, K, x, ldx, w, ldw, bias, labels, ignored, lse, loss_scale, dx, lddx, dw, lddw,
                            dw_type, db, ws, st);
   }
 }

@@ -429,3 +429,30 @@ def test_a_block_and_its_loss_together(mdnn, dtype):
     assert abs(float(loss) - want) <= 10 * HALF[dtype] * abs(want) + 2e-5
     for a, b in ((dy, dyv), (dw, dwv.T), (dx, keep * dhv), (dh, dhv), (dg, dgv), (db, dbv)):
         assert near(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", [(1, 1, 1), (5, 300, 333), (64, 1024, 128), (300, 1031, 40), (600, 777, 200),
+                                  (4100, 9000, 64), (600, 70001, 72), (9000, 20011, 32)])
+def test_the_workspace_is_enough(mdnn, size, dtype):
+    """Nothing is written past the bytes that the query names."""
+    import torch
+    m, n, k = size
+    code = {"f32": 0, "f16": 1, "bf16": 2}[dtype]
+    for layout in (mdnn.NN, mdnn.NT):
+        x = torch.randn(m, k, device="cuda").to(_t(dtype))
+        w = torch.randn(*((k, n) if layout == mdnn.NN else (n, k)), device="cuda").to(_t(dtype))
+        labels = torch.randint(0, n, (m,), device="cuda", dtype=torch.int32)
+        loss, row, lse = torch.empty(1, device="cuda"), torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(n, device="cuda")
+        for backward in (False, True):
+            f = mdnn.mdnn_linear_xent_bwd_workspace if backward else mdnn.mdnn_linear_xent_fwd_workspace
+            need = f(layout, m, n, k, code)
+            ws = torch.full((need + (1 << 20),), 0xA5, dtype=torch.uint8, device="cuda")
+            if backward:
+                mdnn.mdnn_linear_xent_bwd(layout, m, n, k, x, k, w, w.shape[1], code, None, labels, -1, lse, None, dx, k, dw,
+                                          w.shape[1], code, db, ws, need)
+            else:
+                mdnn.mdnn_linear_xent_fwd(layout, m, n, k, x, k, w, w.shape[1], code, None, labels, -1, loss, row, lse, ws,
+                                          need)
+            assert bool((ws[need:] == 0xA5).all())
