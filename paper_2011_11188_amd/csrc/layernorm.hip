@@ -454,28 +454,39 @@ struct LnBwdArgs {
 // block's rows, are added over its row groups in their order and written once;
 // sums_kernel adds the blocks' in order.
 template <class T, bool DROP, int TPR, int NCH>
-__global__ void __launch_bounds__(512) layernorm_bwd_kernel(LnBwdArgs a) {
+__global__ void __launch_bounds__(512, NCH <= 2 && !(DROP && !Chunk<T>::H) ? 4 : 2) layernorm_bwd_kernel(LnBwdArgs a) {
   typedef typename T::storage S;
   constexpr int NT = 512, RPB = NT / TPR, WIDE = TPR * NCH * 8;
   __shared__ RowSums<3, TPR, RPB> buf;
   __shared__ float part[RPB > 1 ? RPB * WIDE : 1];
+  __shared__ float4_t gamma[WIDE / 4];
   const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
   DropKey key = {};
   if (DROP) key = drop_key(a.d);
   ChunkPos pos[NCH];
-  float dg[NCH][8], db[NCH][8], gamma[NCH][8];
+  float dg[NCH][8], db[NCH][8];
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
     pos[i] = chunk_pos(t + i * TPR, a.cols);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dg[i][e] = db[i][e] = 0.0f, gamma[i][e] = 1.0f;
+    for (int e = 0; e < 8; ++e) dg[i][e] = db[i][e] = 0.0f;
+    // (each row group writes the same)
+    float4_t g[2] = {{1.0f, 1.0f, 1.0f, 1.0f}, {1.0f, 1.0f, 1.0f, 1.0f}};
     if (a.gamma) {
-      Chunk<F32> g;
-      g.load(a.gamma + pos[i].start);
+      Chunk<F32> c;
+      c.load(a.gamma + pos[i].start);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) gamma[i][e] = g.get(e);
+      for (int e = 0; e < 8; ++e) g[e >> 2][e & 3] = c.get(e);
     }
+    gamma[(t + i * TPR) * 2] = g[0], gamma[(t + i * TPR) * 2 + 1] = g[1];
   }
+  __syncthreads();
+  // this thread's chunk of gamma, read again where it is needed: 8 NCH registers less
+  auto scale = [&](int i, float (&g)[8]) {
+    const float4_t u = gamma[(t + i * TPR) * 2], v = gamma[(t + i * TPR) * 2 + 1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) g[e] = u[e], g[4 + e] = v[e];
+  };
   const float cols = (float)a.cols;
   for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB) {
     const bool live = r0 + grp < a.rows;
@@ -494,9 +505,11 @@ __global__ void __launch_bounds__(512) layernorm_bwd_kernel(LnBwdArgs a) {
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
+      float g[8];
+      scale(i, g);
       if (pos[i].lo > 0) ch[i].clear(pos[i].lo), cd[i].clear(pos[i].lo);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[0] += ch[i].get(e), s[1] += cd[i].get(e) * gamma[i][e];
+      for (int e = 0; e < 8; ++e) s[0] += ch[i].get(e), s[1] += cd[i].get(e) * g[e];
     }
     row_sums<0>(s, buf);
     const float mean = s[0] / cols;
@@ -504,12 +517,15 @@ __global__ void __launch_bounds__(512) layernorm_bwd_kernel(LnBwdArgs a) {
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       hold(ch[i]), hold(cd[i]);
+      asm volatile("" ::: "memory");  // (gamma is read again)
+      float g[8];
+      scale(i, g);
       int lo = pos[i].lo;
       asm("" : "+v"(lo));
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float d = e < lo ? 0.0f : ch[i].get(e) - mean;
-        q[0] += d, q[1] = fmaf(d, d, q[1]), q[2] = fmaf(cd[i].get(e) * gamma[i][e], d, q[2]);
+        q[0] += d, q[1] = fmaf(d, d, q[1]), q[2] = fmaf(cd[i].get(e) * g[e], d, q[2]);
       }
     }
     row_sums<1>(q, buf);
@@ -519,11 +535,14 @@ __global__ void __launch_bounds__(512) layernorm_bwd_kernel(LnBwdArgs a) {
     for (int i = 0; i < NCH; ++i) {
       if (!live || pos[i].lo == 8) continue;
       hold(ch[i]), hold(cd[i]);
-      float o[8];
+      asm volatile("" ::: "memory");
+      if (DROP) __builtin_amdgcn_sched_barrier(0);  // (one chunk's bits at a time)
+      float o[8], g[8];
+      scale(i, g);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float xh = ((ch[i].get(e) - mean) - k.c) * k.rstd, d = cd[i].get(e);
-        o[e] = k.rstd * ((d * gamma[i][e] - mg) - xh * mgx);
+        o[e] = k.rstd * ((d * g[e] - mg) - xh * mgx);
         if (a.dres) o[e] += cr[i].get(e);
         dg[i][e] = fmaf(d, xh, dg[i][e]);
         db[i][e] += d;
