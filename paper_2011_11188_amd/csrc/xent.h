@@ -51,4 +51,11 @@ int xent_tile(int64_t M, int64_t N);
 template <class T>
 mdnn_status_t xent_tiles(const XentProduct& p, const XentTile& x, hipStream_t st);
 
+// The same by the register-staged kernel: any type, element address and
+// leading dimension that xent_reg_ok takes (ext is not used); tiles of 128 or 64.
+int xent_reg_tile(int64_t M, int64_t N);
+bool xent_reg_ok(mdnn_dtype_t t, const XentProduct& p);
+template <class T>
+mdnn_status_t xent_reg(const XentProduct& p, const XentTile& x, hipStream_t st);
+
 }  // namespace mdnn

@@ -10,11 +10,13 @@
 // Backward, lse is known, so a piece's G follows from its logits alone and goes
 // into the two products at once.
 //
-// Tiled (16 bits): the logits never leave the tile's registers (xent_pipe.h), and
-// all products run on the pipelined kernel.  Operands that it cannot read (sizes
-// that are no multiples of 64, rows off 16 bytes) are copied to padded rows, W by
-// pieces, where there are rows enough to pay for that.  Otherwise, and in fp32, a
-// piece's fp32 logits go through the workspace.
+// The logits never leave a tile's registers: tiled (16 bits), all products run on
+// the pipelined kernel (xent_pipe.h).  Operands that it cannot read (sizes that
+// are no multiples of 64, rows off 16 bytes) are copied to padded rows, W by
+// pieces, where there are rows enough to pay for that; otherwise, and in fp32, the
+// register-staged kernel takes them as they are (xent_reg.hip).  Where neither
+// can (contiguous extents below 16 bytes), or so few tiles over a long K that K
+// has to be split, a piece's fp32 logits go through the workspace.
 //
 // In 16 bits G is stored as 2^15 G for fp16 (probabilities of 1e-5 are subnormal
 // there, those of 1e-8 nothing; times 2^15 the least normal one is 1.9e-9) and
@@ -317,21 +319,31 @@ int64_t piece_classes(int64_t N, int64_t rows, int64_t elems) {
   return nc < 256 ? (N < 256 ? N : 256) : nc < N ? nc : N;
 }
 
-// How a call runs.  By the sizes alone it may run tiled (TILED: operands as
-// they are; PACKED: copies in the workspace) or general; the caller's workspace
-// holds any that its sizes allow.
-enum Way { GENERAL, TILED, PACKED };
+// How a call runs: the tiles read the operands as they are (TILED) or copies in
+// the workspace (PACKED), or the register-staged tiles do (STAGED), or a piece's
+// logits go through the workspace (GENERAL).  The sizes alone name the way; rows
+// that it cannot read (addresses, leading dimensions) fall back to the next, and
+// the caller's workspace holds every way that its sizes allow.
+enum Way { TILED, PACKED, STAGED, GENERAL };
 
 // Rows from which copying W pays (two passes over it at memory speed against
 // products at about twice the register-staged kernel's rate).
 bool pack_pays(int64_t M, bool backward) { return M >= (backward ? 256 : 512); }
 
 Way way_by_size(int64_t M, int64_t N, int64_t K, mdnn_dtype_t t, bool backward) {
-  if (t == MDNN_F32 || M * up(K, 64) >= (int64_t)1 << 31) return GENERAL;  // (32-bit offsets reach every row of x)
-  if (N % 64 == 0 && K % 64 == 0) return TILED;
-  if (!backward && K % 64 == 0 && N % 8 == 0) return TILED;
-  return pack_pays(M, backward) ? PACKED : GENERAL;
+  // (a grid of less than half the chip's CUs over a long K: split in the general product)
+  const bool split = ceil_div(M, 64) * ceil_div(N, 64) < 128 && K > 512;
+  if (t != MDNN_F32 && M * up(K, 64) < (int64_t)1 << 31) {  // (32-bit offsets reach every row of x)
+    if ((N % 64 == 0 || (!backward && N % 8 == 0)) && K % 64 == 0 && !split) return TILED;
+    if (pack_pays(M, backward)) return PACKED;
+  }
+  const int64_t e = 16 / (int64_t)dtype_size(t);
+  return K >= e && N >= e && !split ? STAGED : GENERAL;
 }
+Way way_below(Way w) { return w == TILED ? STAGED : GENERAL; }
+
+// The tile that a way's products take.
+int way_tile(Way w, int64_t M, int64_t N) { return w == STAGED ? xent_reg_tile(M, N) : xent_tile(M, N); }
 
 struct Space {
   size_t at = 0;
@@ -365,7 +377,7 @@ FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   int64_t tiles = 1;
   if (way != GENERAL)
     for (int64_t n : {p.nc, last}) {
-      const int64_t k = ceil_div(n, xent_tile(M, n));
+      const int64_t k = ceil_div(n, way_tile(way, M, n));
       tiles = k > tiles ? k : tiles;
     }
   p.pairs = s.take((size_t)tiles * M * sizeof(Pair));
@@ -377,7 +389,7 @@ FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
     const size_t a = gemm_ws_bytes(t, M, p.nc, K), b = gemm_ws_bytes(t, M, last, K);
     p.gemm_bytes = a > b ? a : b;
     p.gemm = s.take(p.gemm_bytes);
-  } else {
+  } else if (way != STAGED) {
     p.copy = s.take((size_t)M * p.kc * 2);  // x, where its rows are not as the tiles read them
     p.ldw = layout == MDNN_NN ? up(p.nc, 64) : p.kc;
     p.pack = s.take(way == PACKED ? (size_t)(layout == MDNN_NN ? p.kc : up(p.nc, 64)) * p.ldw * 2 : 0);
@@ -397,7 +409,7 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   const size_t es = dtype_size(t);
   p.rows = h ? up(M, 64) : M;
   p.kc = h ? up(K, 64) : up(K, 4);
-  p.nc = piece_classes(N, way == GENERAL ? M : p.rows, (way == GENERAL ? (int64_t)32 : (int64_t)128) << 20);
+  p.nc = piece_classes(N, way == GENERAL ? M : p.rows, (way == GENERAL ? (int64_t)32 : h ? (int64_t)128 : (int64_t)64) << 20);
   if (way == PACKED) {
     const int64_t most = piece_classes(N, p.kc, (int64_t)128 << 20);
     p.nc = p.nc < most ? p.nc : most;
@@ -410,14 +422,14 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   if (way != GENERAL) {
     p.blocks = 1;
     for (int64_t n : {p.nc, last}) {
-      const int64_t b = ceil_div(M, xent_tile(M, n));
+      const int64_t b = ceil_div(M, way_tile(way, M, n));
       p.blocks = b > p.blocks ? b : p.blocks;
     }
   }
   p.alpha = s.take(4);
   p.copy = s.take((size_t)p.rows * p.kc * es);
   if (way == GENERAL) p.z = s.take((size_t)M * p.ldg * 4);
-  p.g = h ? s.take((size_t)p.rows * p.ldg * 2) : p.z;
+  p.g = way == GENERAL && !h ? p.z : s.take((size_t)p.rows * p.ldg * es);
   p.part = s.take((size_t)p.blocks * N * 4);
   p.acc = s.take(h && p.pieces > 1 ? (size_t)M * K * 4 : 0);
   p.ldw = layout == MDNN_NN ? p.ldg : p.kc;
@@ -431,11 +443,18 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   return p;
 }
 
-// Whether the tiles read W as it is: rows on 16 bytes, 32-bit offsets over a
-// piece's rows.
-bool w_fits(mdnn_layout_t layout, const void* w, int64_t ldw, int64_t nc) {
-  return aligned(w, 16) && ldw % 8 == 0 &&
-         (layout == MDNN_NN ? 64 * ldw + nc : (nc + 255) * ldw) < (int64_t)1 << 31;
+// Whether W's rows are as the tiles read them: on 16 bytes, 32-bit offsets over
+// a piece's rows; or as the register-staged tiles do.
+bool w_fits(Way way, mdnn_layout_t layout, int64_t M, int64_t K, const void* x, int64_t ldx, const void* w, int64_t ldw,
+            int64_t N, int64_t nc, mdnn_dtype_t t) {
+  if (way == TILED)
+    return aligned(w, 16) && ldw % 8 == 0 && (layout == MDNN_NN ? 64 * ldw + nc : (nc + 255) * ldw) < (int64_t)1 << 31;
+  if (way == STAGED) {
+    const int64_t last = N - (N - 1) / nc * nc;
+    return xent_reg_ok(t, XentProduct{x, w, ldx, ldw, M, nc, K, nc, layout == MDNN_NT, false}) &&
+           xent_reg_ok(t, XentProduct{x, w, ldx, ldw, M, last, K, last, layout == MDNN_NT, false});
+  }
+  return true;
 }
 
 constexpr int64_t MAX_ROWS = (int64_t)1 << 24, MAX_N = 0x7fffffff;
@@ -481,9 +500,9 @@ struct Piece {
   const void* w;
   int64_t ldw, ext;  // ext: classes that class-contiguous rows have memory for
 };
-mdnn_status_t take_piece(Way way, mdnn_layout_t layout, const void* w, int64_t ldw, int64_t n0, int64_t nc, int64_t K,
-                         int64_t kc, void* room, int64_t ldc, Piece& out, hipStream_t st) {
-  const void* p = w_piece(layout, w, ldw, n0, 2);
+mdnn_status_t take_piece(Way way, mdnn_layout_t layout, const void* w, int64_t ldw, size_t es, int64_t n0, int64_t nc,
+                         int64_t K, int64_t kc, void* room, int64_t ldc, Piece& out, hipStream_t st) {
+  const void* p = w_piece(layout, w, ldw, n0, es);
   if (way != PACKED) {
     out = {p, ldw, nc};
     return MDNN_SUCCESS;
@@ -494,11 +513,11 @@ mdnn_status_t take_piece(Way way, mdnn_layout_t layout, const void* w, int64_t l
 }
 
 template <class T>
-mdnn_status_t tiles(const XentProduct& p, const XentTile& x, hipStream_t st) {
-  if constexpr (T::id != MDNN_F32)
-    return xent_tiles<T>(p, x, st);
-  else
-    return fail(MDNN_ERR_STATE, "linear_xent: no tiles in fp32");
+mdnn_status_t tiles(Way way, const XentProduct& p, const XentTile& x, hipStream_t st) {
+  if constexpr (T::id != MDNN_F32) {
+    if (way != STAGED) return xent_tiles<T>(p, x, st);
+  }
+  return xent_reg<T>(p, x, st);
 }
 
 template <class T>
@@ -510,7 +529,7 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
   Pair *pairs = (Pair*)(ws + p.pairs), *run = (Pair*)(ws + p.run);
   float *zlab = (float*)(ws + p.zlab), *z = (float*)(ws + p.z);
   Tally* tally = (Tally*)(ws + p.tally);
-  if (way != GENERAL && !(aligned(x, 16) && ldx % 8 == 0 && K % 64 == 0 && (M + 255) * ldx < (int64_t)1 << 31)) {
+  if (way < STAGED && !(aligned(x, 16) && ldx % 8 == 0 && K % 64 == 0 && (M + 255) * ldx < (int64_t)1 << 31)) {
     MDNN_TRY(pack(x, ldx, M, K, ws + p.copy, M, p.kc, st));
     x = ws + p.copy, ldx = p.kc;
   }
@@ -527,12 +546,12 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       MDNN_TRY(check_launch("xent_stats_kernel"));
     } else {
       Piece q;
-      MDNN_TRY(take_piece(way, layout, w, ldw, n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
-      XentProduct a = {x, q.w, ldx, q.ldw, M, nc, p.kc, q.ext, layout == MDNN_NT, false};
+      MDNN_TRY(take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
+      XentProduct a = {x, q.w, ldx, q.ldw, M, nc, way == STAGED ? K : p.kc, q.ext, layout == MDNN_NT, false};
       XentTile e = {};
       e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.pairs = pairs, e.zlab = zlab;
-      MDNN_TRY(tiles<T>(a, e, st));
-      n = ceil_div(nc, xent_tile(M, nc));
+      MDNN_TRY(tiles<T>(way, a, e, st));
+      n = ceil_div(nc, way_tile(way, M, nc));
     }
     hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)p.blocks), dim3(1024), 0, st, pairs, n, i > 0 ? run : nullptr,
                        i + 1 < p.pieces ? run : nullptr, M, N, zlab, labels, ignored, lse, row_loss, loss, tally);
@@ -579,13 +598,13 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
                          p.rows, nc, n0, labels, ignored, N, lse, scale, g, p.ldg, part);
       MDNN_TRY(check_launch("xent_grad_kernel"));
     } else {
-      MDNN_TRY(take_piece(way, layout, w, ldw, n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
-      XentProduct a = {copy, q.w, p.kc, q.ldw, M, nc, p.kc, q.ext, layout == MDNN_NT, true};
+      MDNN_TRY(take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
+      XentProduct a = {copy, q.w, p.kc, q.ldw, M, nc, way == STAGED ? K : p.kc, q.ext, layout == MDNN_NT, true};
       XentTile e = {};
       e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.lse = lse, e.scale = scale;
       e.g = g, e.ldg = p.ldg, e.rows = p.rows, e.part = part;
-      MDNN_TRY(tiles<T>(a, e, st));
-      blocks = ceil_div(M, xent_tile(M, nc));
+      MDNN_TRY(tiles<T>(way, a, e, st));
+      blocks = ceil_div(M, way_tile(way, M, nc));
     }
     if (db) {
       hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(nc, 64)), dim3(256), 0, st, part + n0, blocks, N, nc, alpha,
@@ -626,15 +645,22 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
 
 using namespace mdnn;
 
+// Bytes of a call's workspace: the most that a way open to its sizes takes.
 static size_t fwd_bytes(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
-  const Way way = way_by_size(M, N, K, t, false);
-  const size_t a = fwd_plan(way, layout, M, N, K, t).bytes, b = way == TILED ? fwd_plan(GENERAL, layout, M, N, K, t).bytes : 0;
-  return a > b ? a : b;
+  size_t most = 0;
+  for (Way w = way_by_size(M, N, K, t, false);; w = way_below(w)) {
+    const size_t b = fwd_plan(w, layout, M, N, K, t).bytes;
+    most = b > most ? b : most;
+    if (w == GENERAL || w == PACKED) return most;
+  }
 }
 static size_t bwd_bytes(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
-  const Way way = way_by_size(M, N, K, t, true);
-  const size_t a = bwd_plan(way, layout, M, N, K, t).bytes, b = way == TILED ? bwd_plan(GENERAL, layout, M, N, K, t).bytes : 0;
-  return a > b ? a : b;
+  size_t most = 0;
+  for (Way w = way_by_size(M, N, K, t, true);; w = way_below(w)) {
+    const size_t b = bwd_plan(w, layout, M, N, K, t).bytes;
+    most = b > most ? b : most;
+    if (w == GENERAL || w == PACKED) return most;
+  }
 }
 
 extern "C" size_t mdnn_linear_xent_fwd_workspace(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
@@ -660,7 +686,7 @@ extern "C" mdnn_status_t mdnn_linear_xent_fwd(mdnn_layout_t layout, int64_t M, i
   if (!workspace || ws_bytes < need || !aligned(workspace, 256))
     return fail(MDNN_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) required", who, need);
   Way way = way_by_size(M, N, K, dtype, false);
-  if (way == TILED && !w_fits(layout, w, ldw, fwd_plan(TILED, layout, M, N, K, dtype).nc)) way = GENERAL;
+  while (!w_fits(way, layout, M, K, x, ldx, w, ldw, N, fwd_plan(way, layout, M, N, K, dtype).nc, dtype)) way = way_below(way);
   char* ws = (char*)workspace;
   switch (dtype) {
     case MDNN_F32:
@@ -711,7 +737,10 @@ extern "C" mdnn_status_t mdnn_linear_xent_bwd(mdnn_layout_t layout, int64_t M, i
     return fail(MDNN_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) required", who, need);
   clear_error();
   Way way = way_by_size(M, N, K, dtype, true);
-  if (way == TILED && !w_fits(layout, w, ldw, bwd_plan(TILED, layout, M, N, K, dtype).nc)) way = GENERAL;
+  for (;; way = way_below(way)) {
+    const BwdPlan p = bwd_plan(way, layout, M, N, K, dtype);
+    if (w_fits(way, layout, M, K, workspace, p.kc, w, ldw, N, p.nc, dtype)) break;
+  }
   char* ws = (char*)workspace;
   switch (dtype) {
     case MDNN_F32:

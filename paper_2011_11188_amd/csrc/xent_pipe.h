@@ -11,7 +11,7 @@
 #pragma once
 
 #include "gemm_launch.h"
-#include "xent.h"
+#include "xent_end.h"
 
 namespace mdnn {
 namespace {
@@ -30,9 +30,7 @@ xent_tile_kernel(lds::MatArgs aa, lds::MatArgs ba, int64_t M, int64_t N, int64_t
   __shared__ __attribute__((aligned(NS > 2 ? 1024 : 1))) char lds_b2[NS > 2 ? TL::B_BYTES : 1];
   __shared__ __attribute__((aligned(NS > 3 ? 1024 : 1))) char lds_a3[NS > 3 ? TL::A_BYTES : 1];
   __shared__ __attribute__((aligned(NS > 3 ? 1024 : 1))) char lds_b3[NS > 3 ? TL::B_BYTES : 1];
-  __shared__ float col_bias[TL::BN];
-  __shared__ int32_t row_label[TL::BM];
-  __shared__ float row_lse[BWD ? TL::BM : 1];
+  __shared__ XentNumbers<TL, BWD> rn;
   char* const all_a[4] = {lds_a0, lds_a1, lds_a2, lds_a3};
   char* const all_b[4] = {lds_b0, lds_b1, lds_b2, lds_b3};
   lds::Stages<NS> st;
@@ -52,12 +50,7 @@ xent_tile_kernel(lds::MatArgs aa, lds::MatArgs ba, int64_t M, int64_t N, int64_t
   la.init(aa, m0, 0, wave, lane);
   lb.init(ba, n0, 0, wave, lane);
   const uint32_t wa = (uint32_t)(wave * TL::LA) * 1024u, wb = (uint32_t)(wave * TL::LB) * 1024u;
-  // the rows' and columns' own numbers, for the tile's end (published by the mainloop's barriers)
-  for (int i = tid; i < TL::BN; i += TL::NT) col_bias[i] = x.bias && n0 + i < N ? x.bias[n0 + i] : 0.0f;
-  for (int i = tid; i < TL::BM; i += TL::NT) {
-    row_label[i] = m0 + i < M ? x.labels[m0 + i] : x.ignored;
-    if constexpr (BWD) row_lse[i] = m0 + i < M ? x.lse[m0 + i] : 0.0f;
-  }
+  rn.load(x, M, N, m0, n0, tid);  // (published by the mainloop's barriers)
 
   float4_t acc[FM][FN];
 #pragma unroll
@@ -85,117 +78,7 @@ xent_tile_kernel(lds::MatArgs aa, lds::MatArgs ba, int64_t M, int64_t N, int64_t
   for (; t < nk; t += U)
     lds::pipeline_round<T, TL, NS, LA, LB, 0, U, true>(t, nk, st, wave, fa_l, fb_l, wm, wn, la, lb, f0, f1, acc);
 
-  // lane holds rows mw + 16 i, columns nw + 16 j + e of the tile
-  const int mw = wm * TL::WTM + (lane & 15), nw = wn * TL::WTN + 4 * (lane >> 4);
-  float4_t bq[FN];
-#pragma unroll
-  for (int j = 0; j < FN; ++j) bq[j] = *(const float4_t*)&col_bias[nw + j * 16];
-  const bool edge = n0 + TL::BN > N;  // columns past the piece: no logits
-  __syncthreads();                    // (the mainloop's last fragment reads are done)
-
-  if constexpr (!BWD) {
-    Pair* red = (Pair*)lds_a0;  // [WN][BM]
-    static_assert(TL::WN * TL::BM * sizeof(Pair) <= TL::A_BYTES, "room for the pairs");
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      Pair v = {-INFINITY, 0.0f};
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float z = acc[i][j][e] + bq[j][e];
-          if (edge) z = n0 + nw + j * 16 + e < N ? z : -INFINITY;
-          acc[i][j][e] = z;
-          v.m = fmaxf(v.m, z);
-        }
-      v.m = fmaxf(v.m, __shfl_xor(v.m, 16, 64));
-      v.m = fmaxf(v.m, __shfl_xor(v.m, 32, 64));
-      const float ref = pair_ref(v.m);
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v.s += __expf(acc[i][j][e] - ref);
-      v.s += __shfl_xor(v.s, 16, 64);
-      v.s += __shfl_xor(v.s, 32, 64);
-      const int row = mw + i * 16;
-      const int64_t at = (int64_t)row_label[row] - x.n0 - n0 - nw;
-      if (at >= 0 && at < TL::WTN && (at & 15) < 4 && m0 + row < M) {
-        float z = 0.0f;
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) z = at == j * 16 + e ? acc[i][j][e] : z;
-        x.zlab[m0 + row] = z;
-      }
-      if (lane < 16) red[wn * TL::BM + row] = v;
-    }
-    __syncthreads();
-    for (int r = tid; r < TL::BM; r += TL::NT) {
-      if (m0 + r >= M) break;
-      Pair v = red[r];
-#pragma unroll
-      for (int w = 1; w < TL::WN; ++w) v = join(v, red[w * TL::BM + r]);
-      x.pairs[tn * M + m0 + r] = v;
-    }
-  } else {
-    float sum[FN][4];
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[j][e] = 0.0f;
-    typedef typename T::storage S;
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int row = mw + i * 16;
-      const int32_t label = row_label[row];
-      const bool live = label != x.ignored && m0 + row < M;
-      const float l = label >= 0 && label < x.classes ? row_lse[row] : __builtin_nanf("");
-      const int64_t far = (int64_t)label - x.n0 - n0 - nw;
-      const int at = far >= 0 && far < TL::WTN ? (int)far : -1;
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int64_t n = n0 + nw + j * 16;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = __expf(acc[i][j][e] + bq[j][e] - l);
-          v[e] = at == j * 16 + e ? v[e] - 1.0f : v[e];
-          v[e] = live && (!edge || n + e < N) ? v[e] : 0.0f;
-          sum[j][e] += v[e];
-        }
-        if (m0 + row < x.rows && n < x.ldg) {
-          uint2 q;
-          q.x = (uint32_t)from_f<T>(v[0] * x.scale) | ((uint32_t)from_f<T>(v[1] * x.scale) << 16);
-          q.y = (uint32_t)from_f<T>(v[2] * x.scale) | ((uint32_t)from_f<T>(v[3] * x.scale) << 16);
-          *(uint2*)((S*)x.g + (m0 + row) * x.ldg + n) = q;
-        }
-      }
-    }
-    if (x.part) {
-      // over the 16 rows of the lanes, then the tile's wave rows in order
-      float* red = (float*)lds_a0;  // [WM][BN]
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-#pragma unroll
-          for (int o = 1; o < 16; o <<= 1) sum[j][e] += __shfl_xor(sum[j][e], o, 64);
-        }
-      if ((lane & 15) == 0) {
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-          *(float4_t*)&red[wm * TL::BN + nw + j * 16] = (float4_t){sum[j][0], sum[j][1], sum[j][2], sum[j][3]};
-      }
-      __syncthreads();
-      for (int c = tid; c < TL::BN; c += TL::NT) {
-        if (n0 + c >= N) break;
-        float s = red[c];
-#pragma unroll
-        for (int w = 1; w < TL::WM; ++w) s += red[w * TL::BN + c];
-        x.part[tm * x.classes + x.n0 + n0 + c] = s;
-      }
-    }
-  }
+  xent_end<T, TL, BWD>(x, rn, M, N, m0, n0, tm, tn, wm, wn, tid, lds_a0, acc);
 }
 
 template <class T, class TL, int NS, bool B_KC, bool BWD>
