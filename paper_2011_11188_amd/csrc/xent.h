@@ -28,6 +28,7 @@ struct XentTile {
   // forward: tile column t leaves a pair for each row at pairs[t * M + row], the label's column its logit
   Pair* pairs;
   float* zlab;
+  uint32_t* done;  // cleared
   // backward: G times `scale` in the operands' type, rows of ldg elements (a multiple of 64), zeros in rows M .. rows - 1
   // and columns past the piece; part: column sums of tile row t at part[t * classes + n0 + column], or null
   const float* lse;
@@ -57,5 +58,25 @@ int xent_reg_tile(int64_t M, int64_t N);
 bool xent_reg_ok(mdnn_dtype_t t, const XentProduct& p);
 template <class T>
 mdnn_status_t xent_reg(const XentProduct& p, const XentTile& x, hipStream_t st);
+
+// dW and dx of up to eight rows in one pass over W (xent_few.hip).
+struct XentFew {
+  const void *x, *g, *w;  // x: ignored rows zero
+  void* dw;               // or null
+  float* part;            // few_plan's parts [parts][M][K], or null
+  const float* alpha;
+  int64_t M, N, K, ldx, ldg, ldw, lddw;
+  bool by_class;
+  int tx;       // set by xent_few
+  int64_t per;
+};
+struct FewPlan {
+  int tx;                              // threads across a row of W
+  int64_t strips, splits, per, parts;  // per: rows of W in a split
+};
+FewPlan few_plan(bool by_class, int64_t N, int64_t K);
+bool xent_few_ok(bool by_class, mdnn_dtype_t t, int64_t M, int64_t N, int64_t K);
+template <class T>
+mdnn_status_t xent_few(XentFew a, mdnn_dtype_t dw_type, void* dx, int64_t lddx, hipStream_t st);
 
 }  // namespace mdnn

@@ -25,7 +25,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "gemm_core.h"
+#include "gemm_launch.h"
 #include "internal.h"
 #include "xent.h"
 
@@ -41,20 +41,46 @@ namespace {
 
 // ---------------------------------------------------------------- forward
 
+// A row's piece of logits in the workspace: rows of ldz, or the parts of a split
+// product, `splits` of them one after another without their bias.
+struct Logits {
+  const float* z;
+  int64_t ldz, part;  // part: elements between parts
+  int32_t splits;
+  const float* bias;  // with parts: the piece's, or null
+  // element c of a row, the parts added in their order
+  __device__ __forceinline__ float at(int64_t row, int64_t c) const {
+    const float* p = z + row * ldz + c;
+    float v = *p;
+    for (int k = 1; k < splits; ++k) v += p[k * part];
+    return splits > 1 && bias ? v + bias[c] : v;
+  }
+  __device__ __forceinline__ void quad(int64_t row, int64_t c, int64_t nc, float (&e)[4]) const {
+    if (splits == 1) {
+      const float4_t q = *(const float4_t*)(z + row * ldz + c);  // (rows of whole quads)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) e[k] = q[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) e[k] = at(row, c + k < nc ? c + k : nc - 1);
+    }
+  }
+};
+
 // A row's piece of logits to its pair (m, sum exp(z - m)); the label's logit.
 __global__ void __launch_bounds__(256)
-xent_stats_kernel(const float* z, int64_t ldz, int64_t M, int64_t nc, int64_t n0, const int32_t* labels, Pair* pairs,
-                  float* zlab) {
+xent_stats_kernel(Logits z, int64_t M, int64_t nc, int64_t n0, const int32_t* labels, Pair* pairs, float* zlab,
+                  uint32_t* done) {
   __shared__ Pair buf[4];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *done = 0;
   for (int64_t row = blockIdx.x; row < M; row += gridDim.x) {
-    const float* p = z + row * ldz;
     const int64_t at = (int64_t)labels[row] - n0;
     Pair v = {-INFINITY, 0.0f};
     for (int64_t c = threadIdx.x * 4; c < nc; c += 1024) {
-      const float4_t q = *(const float4_t*)(p + c);  // (rows of whole quads)
       float e[4];
+      z.quad(row, c, nc, e);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) e[k] = c + k < nc ? q[k] : -INFINITY;
+      for (int k = 0; k < 4; ++k) e[k] = c + k < nc ? e[k] : -INFINITY;
       float m = fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
       m = fmaxf(m, v.m);
       const float ref = pair_ref(m);
@@ -67,7 +93,7 @@ xent_stats_kernel(const float* z, int64_t ldz, int64_t M, int64_t nc, int64_t n0
     __syncthreads();
     if (threadIdx.x == 0) {
       pairs[row] = join(join(buf[0], buf[1]), join(buf[2], buf[3]));
-      if (at >= 0 && at < nc) zlab[row] = p[at];
+      if (at >= 0 && at < nc) zlab[row] = z.at(row, at);
     }
     __syncthreads();
   }
@@ -82,10 +108,11 @@ struct Tally {
 // null), joined: 64 rows a block, 16 groups of tiles, joined in their order.  To
 // `after` (which may be `before`) where more pieces follow, else to lse and the
 // rows' losses: a block leaves its losses' sum and the number of its rows that
-// count; a single block writes the mean.
+// count, and the last one to do so (counted in `done`, which a kernel before
+// this one has cleared) adds all blocks' in their order for the mean.
 __global__ void __launch_bounds__(1024)
 xent_rows_kernel(const Pair* pairs, int64_t pieces, const Pair* before, Pair* after, int64_t M, int64_t N, const float* zlab, const int32_t* labels,
-                 int32_t ignored, float* lse, float* row_loss, float* loss, Tally* tally) {
+                 int32_t ignored, float* lse, float* row_loss, float* loss, Tally* tally, uint32_t* done) {
   __shared__ Pair buf[16][64];
   const int r = threadIdx.x & 63, g = threadIdx.x >> 6;
   const int64_t row = (int64_t)blockIdx.x * 64 + r, at = row < M ? row : M - 1;
@@ -124,27 +151,28 @@ xent_rows_kernel(const Pair* pairs, int64_t pieces, const Pair* before, Pair* af
     t.sum += __shfl_xor(t.sum, o, 64);
     t.count += __shfl_xor((long long)t.count, o, 64);
   }
-  if (r > 0) return;
-  if (gridDim.x > 1)
-    tally[blockIdx.x] = t;
-  else if (loss)
-    *loss = (float)(t.sum / (double)(t.count > 0 ? t.count : 1));
-}
-
-__global__ void __launch_bounds__(1024) xent_mean_kernel(const Tally* tally, int64_t n, float* loss) {
-  __shared__ Tally buf[16];
-  Tally t = {0.0, 0};
-  for (int64_t i = threadIdx.x; i < n; i += 1024) t.sum += tally[i].sum, t.count += tally[i].count;
+  if (!loss) return;
+  if (gridDim.x > 1) {
+    // (tallies cross the XCDs' caches: stores and loads at device scope)
+    uint32_t last = 0;
+    if (r == 0) {
+      __hip_atomic_store(&tally[blockIdx.x].sum, t.sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&tally[blockIdx.x].count, t.count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last = __hip_atomic_fetch_add(done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    }
+    if (!__shfl((int)last, 0, 64)) return;
+    t = {0.0, 0};
+    for (uint32_t b = r; b < gridDim.x; b += 64) {
+      t.sum += __hip_atomic_load(&tally[b].sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      t.count += __hip_atomic_load(&tally[b].count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    t.sum += __shfl_xor(t.sum, o, 64);
-    t.count += __shfl_xor((long long)t.count, o, 64);
+    for (int o = 32; o > 0; o >>= 1) {
+      t.sum += __shfl_xor(t.sum, o, 64);
+      t.count += __shfl_xor((long long)t.count, o, 64);
+    }
   }
-  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = t;
-  __syncthreads();
-  if (threadIdx.x > 0) return;
-  for (int w = 1; w < 16; ++w) t.sum += buf[w].sum, t.count += buf[w].count;
-  *loss = (float)(t.sum / (double)(t.count > 0 ? t.count : 1));
+  if (r == 0) *loss = (float)(t.sum / (double)(t.count > 0 ? t.count : 1));
 }
 
 // --------------------------------------------------------------- backward
@@ -226,28 +254,28 @@ xent_prepare_kernel(const typename T::storage* x, int64_t ldx, int64_t M, int64_
   }
 }
 
-// Logits of a piece to G (type T, rows of ldg elements; z and G may be the
-// same memory in fp32): 32 rows a block, four columns a thread, four rows in
-// flight.  Rows past M and columns past nc become zeros.  part: the block's
+// Logits of a piece to G (type T, rows of ldg elements): GRAD_ROWS rows a block, four columns a thread, four rows
+// in flight.  Rows past M and columns past nc become zeros.  part: the block's
 // column sums, or null.
+constexpr int GRAD_ROWS = 8;
 template <class T>
 __global__ void __launch_bounds__(256)
-xent_grad_kernel(const float* z, int64_t M, int64_t rows, int64_t nc, int64_t n0, const int32_t* labels, int32_t ignored,
+xent_grad_kernel(Logits z, int64_t M, int64_t rows, int64_t nc, int64_t n0, const int32_t* labels, int32_t ignored,
                  int64_t N, const float* lse, float scale, typename T::storage* g, int64_t ldg, float* part) {
   typedef typename T::storage S;
   const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= ldg) return;
-  for (int64_t b = blockIdx.y; b * 32 < rows; b += gridDim.y) {
+  for (int64_t b = blockIdx.y; b * GRAD_ROWS < rows; b += gridDim.y) {
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t r1 = b * 32 + 32 < rows ? b * 32 + 32 : rows;
-    for (int64_t r0 = b * 32; r0 < r1; r0 += 4) {
-      float4_t q[4];
+    const int64_t r1 = b * GRAD_ROWS + GRAD_ROWS < rows ? b * GRAD_ROWS + GRAD_ROWS : rows;
+    for (int64_t r0 = b * GRAD_ROWS; r0 < r1; r0 += 4) {
+      float q[4][4];
       int32_t label[4];
       float l[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int64_t r = r0 + k < M ? r0 + k : M - 1;
-        q[k] = *(const float4_t*)(z + r * ldg + c);
+        z.quad(r, c, nc, q[k]);
         label[k] = labels[r], l[k] = lse[r];
       }
 #pragma unroll
@@ -332,13 +360,13 @@ bool pack_pays(int64_t M, bool backward) { return M >= (backward ? 256 : 512); }
 
 Way way_by_size(int64_t M, int64_t N, int64_t K, mdnn_dtype_t t, bool backward) {
   // (a grid of less than half the chip's CUs over a long K: split in the general product)
-  const bool split = ceil_div(M, 64) * ceil_div(N, 64) < 128 && K > 512;
+  if (ceil_div(M, 64) * ceil_div(N, 64) < 128 && K > 512) return GENERAL;
   if (t != MDNN_F32 && M * up(K, 64) < (int64_t)1 << 31) {  // (32-bit offsets reach every row of x)
-    if ((N % 64 == 0 || (!backward && N % 8 == 0)) && K % 64 == 0 && !split) return TILED;
+    if ((N % 64 == 0 || (!backward && N % 8 == 0)) && K % 64 == 0) return TILED;
     if (pack_pays(M, backward)) return PACKED;
   }
   const int64_t e = 16 / (int64_t)dtype_size(t);
-  return K >= e && N >= e && !split ? STAGED : GENERAL;
+  return K >= e && N >= e ? STAGED : GENERAL;
 }
 Way way_below(Way w) { return w == TILED ? STAGED : GENERAL; }
 
@@ -354,9 +382,44 @@ struct Space {
   }
 };
 
+// K split of a general piece's logits where their tiles are few (1: the
+// product's own ways), at least 256 deep, parts of at most 32 MB.
+SplitPlan logit_splits(int64_t M, int64_t nc, int64_t K) {
+  SplitPlan p{1, K};
+  const int64_t tiles = ceil_div(M, 64) * ceil_div(nc, 64);
+  int64_t n = tiles < 128 ? ceil_div((int64_t)512, tiles) : 1;
+  n = n < K / 256 ? n : K / 256;
+  const int64_t most = ((int64_t)8 << 20) / (M * nc);
+  n = n < most ? n : most;
+  if (n < 2) return p;
+  p.k_per_split = up(ceil_div(K, n), 64);
+  p.splits = (int)ceil_div(K, p.k_per_split);
+  return p;
+}
+
+// A general piece's logits.
+mdnn_status_t general_logits(mdnn_layout_t layout, int64_t M, int64_t nc, int64_t K, const void* x, int64_t ldx,
+                             const void* w, int64_t ldw, mdnn_dtype_t t, const float* bias, float* z, int64_t ldz,
+                             void* gw, size_t gw_bytes, Logits& out, hipStream_t st) {
+  const SplitPlan s = logit_splits(M, nc, K);
+  if (s.splits > 1 && gemm_reg_ok(t, layout, M, nc, K, ldx, ldw, s.splits)) {
+    Epilogue ep{};
+    ep.alpha = 1.0f, ep.partial = z, ep.k_per_split = s.k_per_split;
+    out = {z, nc, M * nc, s.splits, bias};
+    return gemm_reg(t, MDNN_F32, layout, M, nc, K, x, ldx, w, ldw, ep, s.splits, st);
+  }
+  out = {z, ldz, 0, 1, nullptr};
+  return gemm_mixed_ws(layout, M, nc, K, 1.0f, x, ldx, w, ldw, t, 0.0f, nullptr, 0, z, ldz, MDNN_F32, bias, MDNN_ACT_NONE,
+                       nullptr, 0, gw, gw_bytes, st);
+}
+size_t logit_bytes(int64_t M, int64_t nc, int64_t K, int64_t ldz) {
+  const size_t a = (size_t)logit_splits(M, nc, K).splits * M * nc * 4, b = (size_t)M * ldz * 4;
+  return a > b ? a : b;
+}
+
 struct FwdPlan {
   int64_t nc, pieces, blocks, kc, ldw;
-  size_t pairs, run, zlab, tally, z, copy, pack, gemm, gemm_bytes, bytes;
+  size_t pairs, run, zlab, tally, done, z, copy, pack, gemm, gemm_bytes, bytes;
 };
 FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
   FwdPlan p = {};
@@ -384,8 +447,10 @@ FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   p.run = s.take(p.pieces > 1 ? (size_t)M * sizeof(Pair) : 0);
   p.zlab = s.take((size_t)M * 4);
   p.tally = s.take((size_t)p.blocks * sizeof(Tally));
+  p.done = s.take(4);
   if (way == GENERAL) {
-    p.z = s.take((size_t)M * up(p.nc, 4) * 4);
+    const size_t za = logit_bytes(M, p.nc, K, up(p.nc, 4)), zb = logit_bytes(M, last, K, up(p.nc, 4));
+    p.z = s.take(za > zb ? za : zb);
     const size_t a = gemm_ws_bytes(t, M, p.nc, K), b = gemm_ws_bytes(t, M, last, K);
     p.gemm_bytes = a > b ? a : b;
     p.gemm = s.take(p.gemm_bytes);
@@ -400,14 +465,16 @@ FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
 
 struct BwdPlan {
   int64_t nc, pieces, rows, kc, ldg, blocks, ldw;
-  size_t alpha, copy, z, g, part, acc, pack, gemm, gemm_bytes, bytes;
+  size_t alpha, copy, z, g, part, acc, pack, few, gemm, gemm_bytes, bytes;
+  bool is_few;
 };
 BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
   BwdPlan p = {};
   Space s;
   const bool h = t != MDNN_F32;
   const size_t es = dtype_size(t);
-  p.rows = h ? up(M, 64) : M;
+  // (fp32: a depth below 8 of dW's product would take a kernel for narrow operands: 4 rows, 30912 x 134, 35 us)
+  p.rows = h ? up(M, 64) : M < 8 ? 8 : M;
   p.kc = h ? up(K, 64) : up(K, 4);
   p.nc = piece_classes(N, way == GENERAL ? M : p.rows, (way == GENERAL ? (int64_t)32 : h ? (int64_t)128 : (int64_t)64) << 20);
   if (way == PACKED) {
@@ -418,7 +485,7 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   p.ldg = up(p.nc, h ? 64 : 4);
   const int64_t last = N - (p.pieces - 1) * p.nc;
   // row blocks that leave column sums
-  p.blocks = ceil_div(p.rows, 32);
+  p.blocks = ceil_div(p.rows, GRAD_ROWS);
   if (way != GENERAL) {
     p.blocks = 1;
     for (int64_t n : {p.nc, last}) {
@@ -428,8 +495,11 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   }
   p.alpha = s.take(4);
   p.copy = s.take((size_t)p.rows * p.kc * es);
-  if (way == GENERAL) p.z = s.take((size_t)M * p.ldg * 4);
-  p.g = way == GENERAL && !h ? p.z : s.take((size_t)p.rows * p.ldg * es);
+  if (way == GENERAL) {
+    const size_t za = logit_bytes(M, p.nc, K, p.ldg), zb = logit_bytes(M, last, K, p.ldg);
+    p.z = s.take(za > zb ? za : zb);
+  }
+  p.g = s.take((size_t)p.rows * p.ldg * es);
   p.part = s.take((size_t)p.blocks * N * 4);
   p.acc = s.take(h && p.pieces > 1 ? (size_t)M * K * 4 : 0);
   p.ldw = layout == MDNN_NN ? p.ldg : p.kc;
@@ -438,6 +508,8 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
     for (size_t b : {gemm_ws_bytes(t, M, n, K), gemm_ws_bytes(t, M, K, n), gemm_ws_bytes(t, M, K, up(n, 64)),
                      gemm_ws_bytes(t, n, K, p.rows), gemm_ws_bytes(t, K, n, p.rows)})
       p.gemm_bytes = b > p.gemm_bytes ? b : p.gemm_bytes;
+  p.is_few = p.pieces == 1 && xent_few_ok(layout == MDNN_NT, t, M, N, K);
+  p.few = s.take(p.is_few ? (size_t)few_plan(layout == MDNN_NT, N, K).parts * M * K * 4 : 0);
   p.gemm = s.take(p.gemm_bytes);
   p.bytes = s.at;
   return p;
@@ -529,6 +601,7 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
   Pair *pairs = (Pair*)(ws + p.pairs), *run = (Pair*)(ws + p.run);
   float *zlab = (float*)(ws + p.zlab), *z = (float*)(ws + p.z);
   Tally* tally = (Tally*)(ws + p.tally);
+  uint32_t* done = (uint32_t*)(ws + p.done);
   if (way < STAGED && !(aligned(x, 16) && ldx % 8 == 0 && K % 64 == 0 && (M + 255) * ldx < (int64_t)1 << 31)) {
     MDNN_TRY(pack(x, ldx, M, K, ws + p.copy, M, p.kc, st));
     x = ws + p.copy, ldx = p.kc;
@@ -539,27 +612,24 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
     int64_t n = 1;
     if (way == GENERAL) {
       const int64_t ldz = up(p.nc, 4);
-      MDNN_TRY(gemm_mixed_ws(layout, M, nc, K, 1.0f, x, ldx, w_piece(layout, w, ldw, n0, dtype_size(t)), ldw, t, 0.0f,
-                             nullptr, 0, z, ldz, MDNN_F32, b, MDNN_ACT_NONE, nullptr, 0, ws + p.gemm, p.gemm_bytes, st));
-      hipLaunchKernelGGL(xent_stats_kernel, dim3(capped(M, 1 << 20)), dim3(256), 0, st, z, ldz, M, nc, n0, labels, pairs,
-                         zlab);
+      Logits q;
+      MDNN_TRY(general_logits(layout, M, nc, K, x, ldx, w_piece(layout, w, ldw, n0, dtype_size(t)), ldw, t, b, z, ldz,
+                              ws + p.gemm, p.gemm_bytes, q, st));
+      hipLaunchKernelGGL(xent_stats_kernel, dim3(capped(M, 1 << 20)), dim3(256), 0, st, q, M, nc, n0, labels, pairs, zlab,
+                         done);
       MDNN_TRY(check_launch("xent_stats_kernel"));
     } else {
       Piece q;
       MDNN_TRY(take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
       XentProduct a = {x, q.w, ldx, q.ldw, M, nc, way == STAGED ? K : p.kc, q.ext, layout == MDNN_NT, false};
       XentTile e = {};
-      e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.pairs = pairs, e.zlab = zlab;
+      e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.pairs = pairs, e.zlab = zlab, e.done = done;
       MDNN_TRY(tiles<T>(way, a, e, st));
       n = ceil_div(nc, way_tile(way, M, nc));
     }
     hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)p.blocks), dim3(1024), 0, st, pairs, n, i > 0 ? run : nullptr,
-                       i + 1 < p.pieces ? run : nullptr, M, N, zlab, labels, ignored, lse, row_loss, loss, tally);
+                       i + 1 < p.pieces ? run : nullptr, M, N, zlab, labels, ignored, lse, row_loss, loss, tally, done);
     MDNN_TRY(check_launch("xent_rows_kernel"));
-  }
-  if (loss && p.blocks > 1) {
-    hipLaunchKernelGGL(xent_mean_kernel, dim3(1), dim3(1024), 0, st, tally, p.blocks, loss);
-    MDNN_TRY(check_launch("xent_mean_kernel"));
   }
   return MDNN_SUCCESS;
 }
@@ -591,10 +661,10 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
     Piece q = {w_piece(layout, w, ldw, n0, sizeof(S)), ldw, nc};
     int64_t blocks = p.blocks;
     if (way == GENERAL) {
-      MDNN_TRY(gemm_mixed_ws(layout, M, nc, K, 1.0f, copy, p.kc, q.w, ldw, t, 0.0f, nullptr, 0, z, p.ldg, MDNN_F32, b,
-                             MDNN_ACT_NONE, nullptr, 0, gw, p.gemm_bytes, st));
+      Logits l;
+      MDNN_TRY(general_logits(layout, M, nc, K, copy, p.kc, q.w, ldw, t, b, z, p.ldg, gw, p.gemm_bytes, l, st));
       hipLaunchKernelGGL((xent_grad_kernel<T>),
-                         dim3((unsigned)ceil_div(p.ldg, 1024), capped(ceil_div(p.rows, 32), 65535)), dim3(256), 0, st, z, M,
+                         dim3((unsigned)ceil_div(p.ldg, 1024), capped(ceil_div(p.rows, GRAD_ROWS), 65535)), dim3(256), 0, st, l, M,
                          p.rows, nc, n0, labels, ignored, N, lse, scale, g, p.ldg, part);
       MDNN_TRY(check_launch("xent_grad_kernel"));
     } else {
@@ -610,6 +680,12 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(nc, 64)), dim3(256), 0, st, part + n0, blocks, N, nc, alpha,
                          scale, db + n0);
       MDNN_TRY(check_launch("xent_db_kernel"));
+    }
+    if (p.is_few && (dx || dw)) {
+      XentFew a = {};
+      a.x = copy, a.g = g, a.w = q.w, a.dw = dw, a.part = (float*)(ws + p.few), a.alpha = alpha;
+      a.M = M, a.N = N, a.K = K, a.ldx = p.kc, a.ldg = p.ldg, a.ldw = q.ldw, a.lddw = lddw, a.by_class = layout == MDNN_NT;
+      return xent_few<T>(a, dw ? dw_type : MDNN_F32, dx, lddx, st);
     }
     if (dx) {
       const mdnn_layout_t back = layout == MDNN_NN ? MDNN_NT : MDNN_NN;

@@ -38,6 +38,7 @@ __device__ __forceinline__ void xent_end(const XentTile& x, const XentNumbers<TL
   __syncthreads();                    // (the mainloop's last fragment reads are done)
 
   if constexpr (!BWD) {
+    if (tm == 0 && tn == 0 && tid == 0) *x.done = 0;
     Pair* red = (Pair*)room;  // [WN][BM]
     static_assert(TL::WN * TL::BM * sizeof(Pair) <= TL::A_BYTES && TL::WM * TL::BN * 4 <= TL::A_BYTES, "room for the sums");
 #pragma unroll

@@ -143,7 +143,9 @@ class Problem:
 
 SIZES = [(1, 1, 1), (1, 2, 3), (2, 5, 8), (1, 1000, 64), (3, 4097, 40), (5, 300, 333), (16, 2048, 256), (17, 1001, 129),
          (33, 515, 64), (64, 1024, 128), (65, 1030, 72), (100, 3001, 200), (128, 256, 512), (200, 777, 1000),
-         (257, 2000, 96), (300, 1536, 320), (512, 512, 64)]
+         (257, 2000, 96), (300, 1536, 320), (512, 512, 64),
+         (40, 1500, 1100), (5, 300, 2100), (1, 999, 520), (70, 513, 777), (600, 130, 600),
+         (7, 3000, 1000), (8, 515, 4100), (3, 9000, 65), (2, 70, 2100), (4, 8, 8), (8, 2049, 17)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
