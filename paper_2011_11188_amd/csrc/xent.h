@@ -48,7 +48,7 @@ struct XentProduct {
   bool w_kc, backward;
 };
 // 256, 128 or 64: the side of the tiles, by the sizes.
-int xent_tile(int64_t M, int64_t N);
+int xent_tile(int64_t M, int64_t N, int64_t K, bool backward);
 template <class T>
 mdnn_status_t xent_tiles(const XentProduct& p, const XentTile& x, hipStream_t st);
 

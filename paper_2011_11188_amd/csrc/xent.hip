@@ -31,9 +31,15 @@
 
 namespace mdnn {
 
-int xent_tile(int64_t M, int64_t N) {
+// 256 from one tile a CU on, but for so few steps that a tile is mostly its end,
+// which two workgroups a CU of 128 run beside each other's (backward 8192 x 16384 x
+// 128 bf16 371 us, 256 403; x 256, 4096 x 32768, 509 and 490; forward 9024 x 4416 x
+// 64 35.5 and 37.0, 8192 x 16384 x 128 95 and 88).  Then 128 from one a CU on (64:
+// 2000 x 3000 x 512 25.8 us, 128 18.7; 300 x 20000 x 640 33.8 and 24.5; 100 x 32768 x
+// 4096 93 and 80), for rows that fill them.
+int xent_tile(int64_t M, int64_t N, int64_t K, bool backward) {
   auto tiles = [&](int64_t side) { return ceil_div(M, side) * ceil_div(N, side); };
-  if (M > 128 && tiles(256) >= 256) return 256;
+  if (M > 128 && tiles(256) >= 256 && K > (backward ? 128 : 64)) return 256;
   return M > 64 && tiles(128) >= 256 ? 128 : 64;
 }
 
@@ -48,21 +54,33 @@ struct Logits {
   int64_t ldz, part;  // part: elements between parts
   int32_t splits;
   const float* bias;  // with parts: the piece's, or null
-  // element c of a row, the parts added in their order
-  __device__ __forceinline__ float at(int64_t row, int64_t c) const {
-    const float* p = z + row * ldz + c;
-    float v = *p;
-    for (int k = 1; k < splits; ++k) v += p[k * part];
-    return splits > 1 && bias ? v + bias[c] : v;
-  }
+  // four elements of a row from c on, the parts added in their order, four of
+  // them in flight (past the piece: its last element again)
   __device__ __forceinline__ void quad(int64_t row, int64_t c, int64_t nc, float (&e)[4]) const {
     if (splits == 1) {
       const float4_t q = *(const float4_t*)(z + row * ldz + c);  // (rows of whole quads)
 #pragma unroll
       for (int k = 0; k < 4; ++k) e[k] = q[k];
-    } else {
+      return;
+    }
+    const float* p = z + row * ldz;
+    int64_t at[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) e[k] = at(row, c + k < nc ? c + k : nc - 1);
+    for (int k = 0; k < 4; ++k) at[k] = c + k < nc ? c + k : nc - 1, e[k] = 0.0f;
+    for (int s = 0; s < splits; s += 4) {
+      float v[4][4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[u][k] = p[(s + u < splits ? s + u : s) * part + at[k]];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[k] += s + u < splits ? v[u][k] : 0.0f;
+    }
+    if (bias) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) e[k] += bias[at[k]];
     }
   }
 };
@@ -93,7 +111,11 @@ xent_stats_kernel(Logits z, int64_t M, int64_t nc, int64_t n0, const int32_t* la
     __syncthreads();
     if (threadIdx.x == 0) {
       pairs[row] = join(join(buf[0], buf[1]), join(buf[2], buf[3]));
-      if (at >= 0 && at < nc) zlab[row] = z.at(row, at);
+      if (at >= 0 && at < nc) {
+        float e[4];
+        z.quad(row, at & ~(int64_t)3, nc, e);
+        zlab[row] = at & 2 ? (at & 1 ? e[3] : e[2]) : (at & 1 ? e[1] : e[0]);
+      }
     }
     __syncthreads();
   }
@@ -254,10 +276,10 @@ xent_prepare_kernel(const typename T::storage* x, int64_t ldx, int64_t M, int64_
   }
 }
 
-// Logits of a piece to G (type T, rows of ldg elements): GRAD_ROWS rows a block, four columns a thread, four rows
-// in flight.  Rows past M and columns past nc become zeros.  part: the block's
+// Logits of a piece to G (type T, rows of ldg elements): GRAD_ROWS rows a block, both in flight, four columns
+// a thread.  Rows past M and columns past nc become zeros.  part: the block's
 // column sums, or null.
-constexpr int GRAD_ROWS = 8;
+constexpr int GRAD_ROWS = 2;
 template <class T>
 __global__ void __launch_bounds__(256)
 xent_grad_kernel(Logits z, int64_t M, int64_t rows, int64_t nc, int64_t n0, const int32_t* labels, int32_t ignored,
@@ -268,18 +290,18 @@ xent_grad_kernel(Logits z, int64_t M, int64_t rows, int64_t nc, int64_t n0, cons
   for (int64_t b = blockIdx.y; b * GRAD_ROWS < rows; b += gridDim.y) {
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     const int64_t r1 = b * GRAD_ROWS + GRAD_ROWS < rows ? b * GRAD_ROWS + GRAD_ROWS : rows;
-    for (int64_t r0 = b * GRAD_ROWS; r0 < r1; r0 += 4) {
-      float q[4][4];
-      int32_t label[4];
-      float l[4];
+    for (int64_t r0 = b * GRAD_ROWS; r0 < r1; r0 += GRAD_ROWS) {
+      float q[GRAD_ROWS][4];
+      int32_t label[GRAD_ROWS];
+      float l[GRAD_ROWS];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < GRAD_ROWS; ++k) {
         const int64_t r = r0 + k < M ? r0 + k : M - 1;
         z.quad(r, c, nc, q[k]);
         label[k] = labels[r], l[k] = lse[r];
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < GRAD_ROWS; ++k) {
         if (r0 + k >= r1) break;
         const bool live = r0 + k < M && label[k] != ignored;
         const float at_l = label[k] >= 0 && label[k] < N ? l[k] : __builtin_nanf("");
@@ -371,7 +393,9 @@ Way way_by_size(int64_t M, int64_t N, int64_t K, mdnn_dtype_t t, bool backward) 
 Way way_below(Way w) { return w == TILED ? STAGED : GENERAL; }
 
 // The tile that a way's products take.
-int way_tile(Way w, int64_t M, int64_t N) { return w == STAGED ? xent_reg_tile(M, N) : xent_tile(M, N); }
+int way_tile(Way w, int64_t M, int64_t N, int64_t K, bool backward) {
+  return w == STAGED ? xent_reg_tile(M, N) : xent_tile(M, N, up(K, 64), backward);
+}
 
 struct Space {
   size_t at = 0;
@@ -440,7 +464,7 @@ FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   int64_t tiles = 1;
   if (way != GENERAL)
     for (int64_t n : {p.nc, last}) {
-      const int64_t k = ceil_div(n, way_tile(way, M, n));
+      const int64_t k = ceil_div(n, way_tile(way, M, n, K, false));
       tiles = k > tiles ? k : tiles;
     }
   p.pairs = s.take((size_t)tiles * M * sizeof(Pair));
@@ -489,7 +513,7 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   if (way != GENERAL) {
     p.blocks = 1;
     for (int64_t n : {p.nc, last}) {
-      const int64_t b = ceil_div(M, way_tile(way, M, n));
+      const int64_t b = ceil_div(M, way_tile(way, M, n, K, true));
       p.blocks = b > p.blocks ? b : p.blocks;
     }
   }
@@ -625,7 +649,7 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       XentTile e = {};
       e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.pairs = pairs, e.zlab = zlab, e.done = done;
       MDNN_TRY(tiles<T>(way, a, e, st));
-      n = ceil_div(nc, way_tile(way, M, nc));
+      n = ceil_div(nc, way_tile(way, M, nc, K, false));
     }
     hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)p.blocks), dim3(1024), 0, st, pairs, n, i > 0 ? run : nullptr,
                        i + 1 < p.pieces ? run : nullptr, M, N, zlab, labels, ignored, lse, row_loss, loss, tally, done);
@@ -674,7 +698,7 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.lse = lse, e.scale = scale;
       e.g = g, e.ldg = p.ldg, e.rows = p.rows, e.part = part;
       MDNN_TRY(tiles<T>(way, a, e, st));
-      blocks = ceil_div(M, way_tile(way, M, nc));
+      blocks = ceil_div(M, way_tile(way, M, nc, K, true));
     }
     if (db) {
       hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(nc, 64)), dim3(256), 0, st, part + n0, blocks, N, nc, alpha,

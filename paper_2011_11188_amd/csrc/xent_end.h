@@ -2,22 +2,31 @@
 // logits' gradient (backward), from the accumulators.
 #pragma once
 
+#include <type_traits>
+
 #include "xent.h"
 
 namespace mdnn {
 namespace {
 
-// The bias of a tile's columns, the labels and lse of its rows.
+// The bias of a tile's columns (-Inf past the piece: no probability), the labels
+// and lse of its rows (+Inf where G is zero: ignored rows and those past M).
 template <class TL, bool BWD>
 struct XentNumbers {
   float bias[TL::BN];
   int32_t label[TL::BM];
   float lse[BWD ? TL::BM : 1];
   __device__ __forceinline__ void load(const XentTile& x, int64_t M, int64_t N, int64_t m0, int64_t n0, int tid) {
-    for (int i = tid; i < TL::BN; i += TL::NT) bias[i] = x.bias && n0 + i < N ? x.bias[n0 + i] : 0.0f;
+    for (int i = tid; i < TL::BN; i += TL::NT) bias[i] = n0 + i >= N ? -INFINITY : x.bias ? x.bias[n0 + i] : 0.0f;
     for (int i = tid; i < TL::BM; i += TL::NT) {
-      label[i] = m0 + i < M ? x.labels[m0 + i] : x.ignored;
-      if constexpr (BWD) lse[i] = m0 + i < M ? x.lse[m0 + i] : 0.0f;
+      const int32_t c = m0 + i < M ? x.labels[m0 + i] : x.ignored;
+      if constexpr (BWD) {
+        const bool live = m0 + i < M && c != x.ignored;
+        label[i] = live ? c : -1;
+        lse[i] = !live ? INFINITY : c >= 0 && c < x.classes ? x.lse[m0 + i] : __builtin_nanf("");
+      } else {
+        label[i] = c;
+      }
     }
   }
 };
@@ -34,8 +43,15 @@ __device__ __forceinline__ void xent_end(const XentTile& x, const XentNumbers<TL
   float4_t bq[FN];
 #pragma unroll
   for (int j = 0; j < FN; ++j) bq[j] = *(const float4_t*)&rn.bias[nw + j * 16];
-  const bool edge = n0 + TL::BN > N;  // columns past the piece: no logits
-  __syncthreads();                    // (the mainloop's last fragment reads are done)
+  if (n0 + TL::BN > N) {  // (columns past the piece: whatever they were multiplied from)
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = n0 + nw + j * 16 + e < N ? acc[i][j][e] : 0.0f;
+  }
+  __syncthreads();  // (the mainloop's last fragment reads are done)
 
   if constexpr (!BWD) {
     if (tm == 0 && tn == 0 && tid == 0) *x.done = 0;
@@ -48,10 +64,8 @@ __device__ __forceinline__ void xent_end(const XentTile& x, const XentNumbers<TL
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float z = acc[i][j][e] + bq[j][e];
-          if (edge) z = n0 + nw + j * 16 + e < N ? z : -INFINITY;
-          acc[i][j][e] = z;
-          v.m = fmaxf(v.m, z);
+          acc[i][j][e] += bq[j][e];
+          v.m = fmaxf(v.m, acc[i][j][e]);
         }
       v.m = fmaxf(v.m, __shfl_xor(v.m, 16, 64));
       v.m = fmaxf(v.m, __shfl_xor(v.m, 32, 64));
@@ -92,28 +106,37 @@ __device__ __forceinline__ void xent_end(const XentTile& x, const XentNumbers<TL
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
       const int row = mw + i * 16;
-      const int32_t label = rn.label[row];
-      const bool live = label != x.ignored && m0 + row < M;
-      const float l = label >= 0 && label < x.classes ? rn.lse[row] : __builtin_nanf("");
-      const int64_t far = (int64_t)label - x.n0 - n0 - nw;
+      const float l = rn.lse[row];
+      const int64_t far = (int64_t)rn.label[row] - x.n0 - n0 - nw;
       const int at = far >= 0 && far < TL::WTN ? (int)far : -1;
+      const bool dead = l == INFINITY, hit = __any(at >= 0), some = __any(dead);  // (few waves hold any)
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
         const int64_t n = n0 + nw + j * 16;
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = __expf(acc[i][j][e] + bq[j][e] - l);
-          v[e] = at == j * 16 + e ? v[e] - 1.0f : v[e];
-          v[e] = live && (!edge || n + e < N) ? v[e] : 0.0f;
-          sum[j][e] += v[e];
+        for (int e = 0; e < 4; ++e) v[e] = __expf(acc[i][j][e] + bq[j][e] - l);
+        if (hit) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = at == j * 16 + e ? v[e] - 1.0f : v[e];
         }
+        if (some) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = dead ? 0.0f : v[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[j][e] += v[e];
         if (m0 + row < x.rows && n < x.ldg) {
           S* d = (S*)x.g + (m0 + row) * x.ldg + n;
           if constexpr (sizeof(S) == 2) {
+            // (a vector conversion is one instruction for two elements)
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            typedef std::conditional_t<T::id == MDNN_F16, _Float16, __bf16> E;
+            typedef E e2 __attribute__((ext_vector_type(2)));
+            const float c = T::id == MDNN_F16 ? x.scale : 1.0f;
             uint2 q;
-            q.x = (uint32_t)from_f<T>(v[0] * x.scale) | ((uint32_t)from_f<T>(v[1] * x.scale) << 16);
-            q.y = (uint32_t)from_f<T>(v[2] * x.scale) | ((uint32_t)from_f<T>(v[3] * x.scale) << 16);
+            q.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[0] * c, v[1] * c}, e2));
+            q.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){v[2] * c, v[3] * c}, e2));
             *(uint2*)d = q;
           } else {
             *(float4_t*)d = (float4_t){v[0], v[1], v[2], v[3]};

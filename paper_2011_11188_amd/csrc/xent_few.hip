@@ -220,8 +220,8 @@ void launch_rows(const XentFew& a, const FewPlan& p, hipStream_t st) {
 }  // namespace
 
 // Strips of W's contiguous dimension, and splits of the other one: two blocks a
-// CU where each leaves its own sums for dx (by class), else four; at least 16 rows
-// of W to a thread group, so that the sums stay small beside W.
+// CU where each leaves its own sums for dx (by class), else four; at least 16 (4)
+// rows of W to a thread group, so that the sums stay small beside W.
 FewPlan few_plan(bool by_class, int64_t N, int64_t K) {
   FewPlan p;
   const int64_t across = by_class ? K : N, along = by_class ? N : K, chunks = ceil_div(across, 8);
@@ -230,7 +230,7 @@ FewPlan few_plan(bool by_class, int64_t N, int64_t K) {
     while (p.tx > 16 && p.tx / 2 >= chunks) p.tx /= 2;
   p.strips = ceil_div(chunks, p.tx);
   const int groups = 256 / p.tx;
-  int64_t n = ceil_div(by_class ? 512 : 1024, p.strips), most = ceil_div(along, 16 * groups);
+  int64_t n = ceil_div(by_class ? 512 : 1024, p.strips), most = ceil_div(along, by_class ? 16 * groups : 4);
   n = n < most ? n : most;
   p.per = ceil_div(along, n);
   p.splits = ceil_div(along, p.per);

@@ -100,7 +100,7 @@ void launch_xent_tile(const XentProduct& p, const XentTile& x, hipStream_t st) {
 
 template <class T>
 mdnn_status_t xent_tiles(const XentProduct& p, const XentTile& x, hipStream_t st) {
-  switch (xent_tile(p.M, p.N)) {
+  switch (xent_tile(p.M, p.N, p.K, p.backward)) {
     case 256: launch_xent_tile<T, lds::Tile256, 2>(p, x, st); break;
     case 128: launch_xent_tile<T, lds::Tile128, 2>(p, x, st); break;
     default: launch_xent_tile<T, lds::Tile<64, 64, 2, 2, 2>, 4>(p, x, st); break;
