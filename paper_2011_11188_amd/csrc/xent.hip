@@ -363,10 +363,12 @@ xent_round_kernel(const float* src, int64_t rows, int64_t cols, typename T::stor
 int64_t up(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
 
 // Classes of a piece: as many as `elems` elements of `rows` a class hold, in
-// whole multiples of 256, at least one.
+// whole multiples of 256, at least one, at most 2^26 (a launch holds fewer than
+// 2^32 threads).
 int64_t piece_classes(int64_t N, int64_t rows, int64_t elems) {
-  const int64_t nc = elems / rows / 256 * 256;
-  return nc < 256 ? (N < 256 ? N : 256) : nc < N ? nc : N;
+  int64_t nc = elems / rows / 256 * 256;
+  nc = nc < 256 ? 256 : nc < (1 << 26) ? nc : 1 << 26;
+  return nc < N ? nc : N;
 }
 
 // How a call runs: the tiles read the operands as they are (TILED) or copies in
@@ -733,7 +735,7 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
     }
   }
   if (dx && joined) {
-    hipLaunchKernelGGL((xent_round_kernel<T>), dim3(capped(ceil_div(K, 256), 1024), capped(M, 65535)), dim3(256), 0, st,
+    hipLaunchKernelGGL((xent_round_kernel<T>), dim3(capped(ceil_div(K, 256), 1024), capped(M, 4096)), dim3(256), 0, st,
                        acc, M, K, (S*)dx, lddx);
     MDNN_TRY(check_launch("xent_round_kernel"));
   }

@@ -242,7 +242,7 @@ FewPlan few_plan(bool by_class, int64_t N, int64_t K) {
 // fp16 474 us, as two products 408; 4 x 17020 x 3136 bf16 99 and 149)
 bool xent_few_ok(bool by_class, mdnn_dtype_t t, int64_t M, int64_t N, int64_t K) {
   const int64_t most = by_class || t == MDNN_F32 ? 8 : 4;
-  return M <= most && (by_class ? K : N) >= 8 && N <= 1 << 28 && K <= 1 << 28;
+  return M <= most && (by_class ? K : N) >= 8 && N <= 1 << 26 && K <= 1 << 20;
 }
 
 template <class T>

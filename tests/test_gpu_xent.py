@@ -166,7 +166,9 @@ def test_gradients(mdnn, size, by_class, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("m,n,k,by_class", [(4100, 9000, 64, False), (4096, 8192, 128, True), (9000, 20011, 32, True),
-                                            (1000, 70001, 40, False), (20000, 4100, 72, False), (70, 131072, 520, True)])
+                                            (1000, 70001, 40, False), (20000, 4100, 72, False), (70, 131072, 520, True),
+                                            (1 << 20, 2305, 64, False), (1 << 20, 2368, 64, True), (4, 70001, 264, True),
+                                            (3, 70001, 264, False)])
 def test_large(mdnn, m, n, k, by_class, dtype):
     """Several pieces, row blocks and tiles; against 64 bits on the GPU, by the module's bounds."""
     import torch
@@ -184,8 +186,9 @@ def test_large(mdnn, m, n, k, by_class, dtype):
     a = 1.0 / int(counted.sum())
     dw_want, db_want, total = torch.zeros_like(wd), torch.zeros(n, dtype=torch.float64, device="cuda"), 0.0
     dw_tol, db_tol = torch.zeros_like(wd), torch.zeros_like(db_want)
-    for lo in range(0, m, 2000):
-        rows = slice(lo, min(m, lo + 2000))
+    step = 2000 if m < 1 << 20 else 1 << 14
+    for lo in range(0, m, step):
+        rows = slice(lo, min(m, lo + step))
         xd, c = x[rows].double(), counted[rows, None]
         z = xd @ wd + bias.double()
         want = torch.logsumexp(z, 1)
