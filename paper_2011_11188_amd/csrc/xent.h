@@ -36,6 +36,10 @@ struct XentTile {
   void* g;
   int64_t ldg, rows;
   float* part;
+  // where one tile row holds all rows: db itself in place of part (or null), and a = S / counted rows over `scale` to alpha
+  bool alone;
+  const float* loss_scale;
+  float *alpha, *db;
 };
 
 // The products whose tiles end so (16-bit operands, x K-contiguous, W
@@ -61,7 +65,9 @@ mdnn_status_t xent_reg(const XentProduct& p, const XentTile& x, hipStream_t st);
 
 // dW and dx of up to eight rows in one pass over W (xent_few.hip).
 struct XentFew {
-  const void *x, *g, *w;  // x: ignored rows zero
+  const void *x, *g, *w;
+  const int32_t* labels;  // rows of x whose label is ignored count as zeros; null: they are
+  int32_t ignored;
   void* dw;               // or null
   float* part;            // few_plan's parts [parts][M][K], or null
   const float* alpha;

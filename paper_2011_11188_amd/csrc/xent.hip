@@ -283,8 +283,14 @@ constexpr int GRAD_ROWS = 2;
 template <class T>
 __global__ void __launch_bounds__(256)
 xent_grad_kernel(Logits z, int64_t M, int64_t rows, int64_t nc, int64_t n0, const int32_t* labels, int32_t ignored,
-                 int64_t N, const float* lse, float scale, typename T::storage* g, int64_t ldg, float* part) {
+                 int64_t N, const float* lse, float scale, typename T::storage* g, int64_t ldg, float* part,
+                 const float* loss_scale, float* alpha) {
   typedef typename T::storage S;
+  if (alpha && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {  // (few rows)
+    int n = 0;
+    for (int64_t r = 0; r < M; ++r) n += labels[r] != ignored;
+    *alpha = (loss_scale ? *loss_scale : 1.0f) / (float)(n > 0 ? n : 1) * (1.0f / scale);
+  }
   const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= ldg) return;
   for (int64_t b = blockIdx.y; b * GRAD_ROWS < rows; b += gridDim.y) {
@@ -678,9 +684,19 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
   void* gw = ws + p.gemm;
   const bool joined = H && p.pieces > 1;
   float* acc = joined ? (float*)(ws + p.acc) : nullptr;
-  hipLaunchKernelGGL((xent_prepare_kernel<T>), dim3(capped(p.rows, 1 << 16) + 1), dim3(256), 0, st, (const S*)x, ldx, M,
-                     K, labels, ignored, loss_scale, 1.0f / scale, alpha, copy, p.rows, p.kc);
-  MDNN_TRY(check_launch("xent_prepare_kernel"));
+  // Few rows are read where they are: their kernels leave out the ignored ones.
+  const bool few = p.is_few && (dx || dw);
+  const bool here = few && (way == GENERAL || (way == STAGED && xent_reg_ok(t, XentProduct{x, w, ldx, ldw, M, p.nc, K, p.nc,
+                                                                                           layout == MDNN_NT, true})) ||
+                            (way == TILED && aligned(x, 16) && ldx % 8 == 0 && (M + 255) * ldx < (int64_t)1 << 31));
+  if (here) {
+    copy = (S*)x;
+  } else {
+    hipLaunchKernelGGL((xent_prepare_kernel<T>), dim3(capped(p.rows, 1 << 16) + 1), dim3(256), 0, st, (const S*)x, ldx, M,
+                       K, labels, ignored, loss_scale, 1.0f / scale, alpha, copy, p.rows, p.kc);
+    MDNN_TRY(check_launch("xent_prepare_kernel"));
+  }
+  const int64_t ldc = here ? ldx : p.kc;
   for (int64_t n0 = 0; n0 < N; n0 += p.nc) {
     const int64_t nc = n0 + p.nc < N ? p.nc : N - n0;
     const float* b = bias ? bias + n0 : nullptr;
@@ -688,29 +704,31 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
     int64_t blocks = p.blocks;
     if (way == GENERAL) {
       Logits l;
-      MDNN_TRY(general_logits(layout, M, nc, K, copy, p.kc, q.w, ldw, t, b, z, p.ldg, gw, p.gemm_bytes, l, st));
+      MDNN_TRY(general_logits(layout, M, nc, K, copy, ldc, q.w, ldw, t, b, z, p.ldg, gw, p.gemm_bytes, l, st));
       hipLaunchKernelGGL((xent_grad_kernel<T>),
                          dim3((unsigned)ceil_div(p.ldg, 1024), capped(ceil_div(p.rows, GRAD_ROWS), 65535)), dim3(256), 0, st, l, M,
-                         p.rows, nc, n0, labels, ignored, N, lse, scale, g, p.ldg, part);
+                         p.rows, nc, n0, labels, ignored, N, lse, scale, g, p.ldg, part, loss_scale, here ? alpha : nullptr);
       MDNN_TRY(check_launch("xent_grad_kernel"));
     } else {
       MDNN_TRY(take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
-      XentProduct a = {copy, q.w, p.kc, q.ldw, M, nc, way == STAGED ? K : p.kc, q.ext, layout == MDNN_NT, true};
+      XentProduct a = {copy, q.w, ldc, q.ldw, M, nc, way == STAGED ? K : p.kc, q.ext, layout == MDNN_NT, true};
       XentTile e = {};
       e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.lse = lse, e.scale = scale;
-      e.g = g, e.ldg = p.ldg, e.rows = p.rows, e.part = part;
-      MDNN_TRY(tiles<T>(way, a, e, st));
       blocks = ceil_div(M, way_tile(way, M, nc, K, true));
+      e.alone = blocks == 1, e.loss_scale = loss_scale, e.alpha = alpha, e.db = e.alone ? db : nullptr;
+      e.g = g, e.ldg = p.ldg, e.rows = p.rows, e.part = e.alone ? nullptr : part;
+      MDNN_TRY(tiles<T>(way, a, e, st));
     }
-    if (db) {
+    if (db && (way == GENERAL || blocks > 1)) {
       hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(nc, 64)), dim3(256), 0, st, part + n0, blocks, N, nc, alpha,
                          scale, db + n0);
       MDNN_TRY(check_launch("xent_db_kernel"));
     }
-    if (p.is_few && (dx || dw)) {
+    if (few) {
       XentFew a = {};
       a.x = copy, a.g = g, a.w = q.w, a.dw = dw, a.part = (float*)(ws + p.few), a.alpha = alpha;
-      a.M = M, a.N = N, a.K = K, a.ldx = p.kc, a.ldg = p.ldg, a.ldw = q.ldw, a.lddw = lddw, a.by_class = layout == MDNN_NT;
+      a.labels = here ? labels : nullptr, a.ignored = ignored;
+      a.M = M, a.N = N, a.K = K, a.ldx = ldc, a.ldg = p.ldg, a.ldw = q.ldw, a.lddw = lddw, a.by_class = layout == MDNN_NT;
       return xent_few<T>(a, dw ? dw_type : MDNN_F32, dx, lddx, st);
     }
     if (dx) {

@@ -23,7 +23,8 @@ struct XentNumbers {
       if constexpr (BWD) {
         const bool live = m0 + i < M && c != x.ignored;
         label[i] = live ? c : -1;
-        lse[i] = !live ? INFINITY : c >= 0 && c < x.classes ? x.lse[m0 + i] : __builtin_nanf("");
+        const float l = live ? x.lse[m0 + i] : 0.0f;
+        lse[i] = !live ? INFINITY : c >= 0 && c < x.classes ? (l == INFINITY ? 3.4e38f : l) : __builtin_nanf("");
       } else {
         label[i] = c;
       }
@@ -144,7 +145,13 @@ __device__ __forceinline__ void xent_end(const XentTile& x, const XentNumbers<TL
         }
       }
     }
-    if (x.part) {
+    float alpha = 0.0f;
+    if (x.alone) {
+      const int n = __syncthreads_count(tid < TL::BM && rn.lse[tid < TL::BM ? tid : 0] != INFINITY);
+      alpha = (x.loss_scale ? *x.loss_scale : 1.0f) / (float)(n > 0 ? n : 1) * (1.0f / x.scale);
+      if (tn == 0 && tid == 0) *x.alpha = alpha;
+    }
+    if (x.part || x.db) {
       // over the 16 rows of the lanes, then the tile's wave rows in order
       float* red = (float*)room;  // [WM][BN]
 #pragma unroll
@@ -165,7 +172,10 @@ __device__ __forceinline__ void xent_end(const XentTile& x, const XentNumbers<TL
         float s = red[c];
 #pragma unroll
         for (int w = 1; w < TL::WM; ++w) s += red[w * TL::BN + c];
-        x.part[tm * x.classes + x.n0 + n0 + c] = s;
+        if (x.db)
+          x.db[x.n0 + n0 + c] = s * (alpha * x.scale);
+        else
+          x.part[tm * x.classes + x.n0 + n0 + c] = s;
       }
     }
   }

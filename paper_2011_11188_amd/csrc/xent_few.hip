@@ -17,6 +17,11 @@
 namespace mdnn {
 namespace {
 
+// Whether row m of x counts (as zeros where it does not).
+__device__ __forceinline__ bool counts(const XentFew& a, int m) {
+  return m < a.M && (!a.labels || a.labels[m] != a.ignored);
+}
+
 constexpr int FEW_TILE = 64;  // rows of W whose numbers a block holds in LDS at a time
 
 // W [N][K]: a thread's columns k of x in registers, the classes' G through LDS.
@@ -33,9 +38,10 @@ __global__ void __launch_bounds__(256) xent_few_by_class_kernel(XentFew a) {
 #pragma unroll
   for (int m = 0; m < MR; ++m) {
     Chunk<T> c;
-    if (m < a.M) c.load((const S*)a.x + m * a.ldx + pos.start);
+    const bool on = counts(a, m);
+    if (on) c.load((const S*)a.x + m * a.ldx + pos.start);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[m][e] = m < a.M ? c.get(e) : 0.0f, acc[m][e] = 0.0f;
+    for (int e = 0; e < 8; ++e) x[m][e] = on ? c.get(e) : 0.0f, acc[m][e] = 0.0f;
   }
   const int64_t n1 = (int64_t)(blockIdx.y + 1) * a.per < a.N ? (int64_t)(blockIdx.y + 1) * a.per : a.N;
   for (int64_t t0 = (int64_t)blockIdx.y * a.per; t0 < n1; t0 += FEW_TILE) {
@@ -129,7 +135,7 @@ __global__ void __launch_bounds__(256) xent_few_by_row_kernel(XentFew a) {
     __syncthreads();
     for (int i = threadIdx.x; i < FEW_TILE * MR; i += 256) {
       const int m = i / FEW_TILE, k = i % FEW_TILE;
-      xs[k][m] = m < a.M && k < left ? load_f<T>((const S*)a.x + m * a.ldx + t0 + k) : 0.0f;
+      xs[k][m] = k < left && counts(a, m) ? load_f<T>((const S*)a.x + m * a.ldx + t0 + k) : 0.0f;
     }
     __syncthreads();
     for (int i0 = 0; i0 < left; i0 += 4) {
