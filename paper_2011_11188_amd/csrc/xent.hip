@@ -127,33 +127,56 @@ struct Tally {
 };
 
 // The pairs of a piece's tiles, and those of the pieces before it (`before`, or
-// null), joined: 64 rows a block, 16 groups of tiles, joined in their order.  To
-// `after` (which may be `before`) where more pieces follow, else to lse and the
-// rows' losses: a block leaves its losses' sum and the number of its rows that
-// count, and the last one to do so (counted in `done`, which a kernel before
-// this one has cleared) adds all blocks' in their order for the mean.
+// null), joined: RPB rows a block, 1024 / RPB groups that take the tiles in turn,
+// eight in flight, joined in a fixed order.  To `after` (which may be `before`)
+// where more pieces follow, else to lse and the rows' losses: a block leaves its
+// losses' sum and the number of its rows that count, and the last one to do so
+// (counted in `done`, which a kernel before this one has cleared) adds all blocks'
+// in their order for the mean.  Up to 1024 rows, 16 a block: one row of 512 tiles
+// takes one round of loads (5.3 us, 64 rows a block 9.0).
+int rows_per_block(int64_t M) { return M <= 1024 ? 16 : 64; }
+
+template <int RPB>
 __global__ void __launch_bounds__(1024)
-xent_rows_kernel(const Pair* pairs, int64_t pieces, const Pair* before, Pair* after, int64_t M, int64_t N, const float* zlab, const int32_t* labels,
-                 int32_t ignored, float* lse, float* row_loss, float* loss, Tally* tally, uint32_t* done) {
-  __shared__ Pair buf[16][64];
-  const int r = threadIdx.x & 63, g = threadIdx.x >> 6;
-  const int64_t row = (int64_t)blockIdx.x * 64 + r, at = row < M ? row : M - 1;
-  const int64_t per = ceil_div(pieces, 16), p0 = g * per, p1 = p0 + per < pieces ? p0 + per : pieces;
+xent_rows_kernel(const Pair* pairs, int64_t pieces, const Pair* before, Pair* after, int64_t M, int64_t N,
+                 const float* zlab, const int32_t* labels, int32_t ignored, float* lse, float* row_loss, float* loss,
+                 Tally* tally, uint32_t* done) {
+  constexpr int G = 1024 / RPB;
+  __shared__ Pair buf[G][RPB + (RPB < 64)];  // (odd rows where columns are read)
+  __shared__ Pair rows[RPB];
+  const int g = threadIdx.x / RPB;
+  int r = threadIdx.x % RPB;
+  int64_t row = (int64_t)blockIdx.x * RPB + r;
+  const int64_t at = row < M ? row : M - 1;
   Pair v = {-INFINITY, 0.0f};
   if (before && g == 0) v = before[at];
-  for (int64_t p = p0; p < p1; p += 8) {
+  for (int64_t p = g; p < pieces; p += 8 * G) {
     Pair u[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) u[k] = pairs[(p + k < p1 ? p + k : p) * M + at];
+    for (int k = 0; k < 8; ++k) u[k] = pairs[(p + k * G < pieces ? p + k * G : p) * M + at];
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (p + k < p1) v = join(v, u[k]);
+      if (p + k * G < pieces) v = join(v, u[k]);
   }
   buf[g][r] = v;
   __syncthreads();
-  if (g > 0) return;
+  if constexpr (RPB == 64) {
+    if (g > 0) return;
 #pragma unroll
-  for (int k = 1; k < 16; ++k) v = join(v, buf[k][r]);
+    for (int k = 1; k < G; ++k) v = join(v, buf[k][r]);
+  } else {
+    // a wave joins one row's groups, then wave 0 goes on with the rows
+    static_assert(RPB == 16, "a wave a row");
+    v = buf[threadIdx.x & 63][threadIdx.x >> 6];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = join(v, Pair{__shfl_xor(v.m, o, 64), __shfl_xor(v.s, o, 64)});
+    if ((threadIdx.x & 63) == 0) rows[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    r = threadIdx.x;
+    row = r < RPB ? (int64_t)blockIdx.x * RPB + r : M;
+    if (r < RPB) v = rows[r];
+  }
   if (after) {
     if (row < M) after[row] = v;
     return;
@@ -456,7 +479,7 @@ struct FwdPlan {
 FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
   FwdPlan p = {};
   Space s;
-  p.blocks = ceil_div(M, 64);
+  p.blocks = ceil_div(M, rows_per_block(M));
   p.kc = up(K, 64);
   if (way == GENERAL) {
     p.nc = piece_classes(N, M, (int64_t)16 << 20);
@@ -659,8 +682,14 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       MDNN_TRY(tiles<T>(way, a, e, st));
       n = ceil_div(nc, way_tile(way, M, nc, K, false));
     }
-    hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)p.blocks), dim3(1024), 0, st, pairs, n, i > 0 ? run : nullptr,
-                       i + 1 < p.pieces ? run : nullptr, M, N, zlab, labels, ignored, lse, row_loss, loss, tally, done);
+    const Pair* before = i > 0 ? run : nullptr;
+    Pair* after = i + 1 < p.pieces ? run : nullptr;
+    if (rows_per_block(M) == 16)
+      hipLaunchKernelGGL(xent_rows_kernel<16>, dim3((unsigned)p.blocks), dim3(1024), 0, st, pairs, n, before, after, M, N,
+                         zlab, labels, ignored, lse, row_loss, loss, tally, done);
+    else
+      hipLaunchKernelGGL(xent_rows_kernel<64>, dim3((unsigned)p.blocks), dim3(1024), 0, st, pairs, n, before, after, M, N,
+                         zlab, labels, ignored, lse, row_loss, loss, tally, done);
     MDNN_TRY(check_launch("xent_rows_kernel"));
   }
   return MDNN_SUCCESS;
