@@ -387,6 +387,27 @@ xent_round_kernel(const float* src, int64_t rows, int64_t cols, typename T::stor
       dst[r * ld + c] = from_f<T>(src[r * cols + c]);
 }
 
+// dx from the parts of its product, in their order, times the factor.
+template <class T>
+__global__ void __launch_bounds__(256)
+xent_parts_kernel(const float* part, int parts, int64_t rows, int64_t cols, const float* alpha, typename T::storage* dst,
+                  int64_t ld) {
+  const float a = *alpha;
+  for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < cols; c += (int64_t)gridDim.x * 256) {
+      const float* p = part + r * cols + c;
+      float s = 0.0f;
+      for (int k0 = 0; k0 < parts; k0 += 8) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = p[(k0 + k < parts ? k0 + k : k0) * rows * cols];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += k0 + k < parts ? v[k] : 0.0f;
+      }
+      dst[r * ld + c] = from_f<T>(s * a);
+    }
+}
+
 // ------------------------------------------------------------------- plans
 
 int64_t up(int64_t n, int64_t to) { return ceil_div(n, to) * to; }
@@ -518,9 +539,24 @@ FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   return p;
 }
 
+// Depth split of dx on the register-staged kernel, whose classes are the depth:
+// two rounds of two workgroups a CU (500 x 777 over 10007 fp32 198 us on its 104
+// tiles), at least 512 deep, parts of at most 64 MB.
+SplitPlan dx_splits(int64_t M, int64_t K, int64_t depth) {
+  SplitPlan p{1, depth};
+  int64_t n = 1024 / (ceil_div(M, 64) * ceil_div(K, 64));
+  n = n < depth / 512 ? n : depth / 512;
+  const int64_t most = ((int64_t)16 << 20) / (M * K);
+  n = n < most ? n : most;
+  if (n < 2) return p;
+  p.k_per_split = up(ceil_div(depth, n), 64);
+  p.splits = (int)ceil_div(depth, p.k_per_split);
+  return p;
+}
+
 struct BwdPlan {
   int64_t nc, pieces, rows, kc, ldg, blocks, ldw;
-  size_t alpha, copy, z, g, part, acc, pack, few, gemm, gemm_bytes, bytes;
+  size_t alpha, copy, z, g, part, acc, pack, few, parts, gemm, gemm_bytes, bytes;
   bool is_few;
 };
 BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, mdnn_dtype_t t) {
@@ -531,7 +567,7 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   // (fp32: a depth below 8 of dW's product would take a kernel for narrow operands: 4 rows, 30912 x 134, 35 us)
   p.rows = h ? up(M, 64) : M < 8 ? 8 : M;
   p.kc = h ? up(K, 64) : up(K, 4);
-  p.nc = piece_classes(N, way == GENERAL ? M : p.rows, (way == GENERAL ? (int64_t)32 : h ? (int64_t)128 : (int64_t)64) << 20);
+  p.nc = piece_classes(N, way == GENERAL ? M : p.rows, (way == GENERAL ? (int64_t)32 : (int64_t)128) << 20);
   if (way == PACKED) {
     const int64_t most = piece_classes(N, p.kc, (int64_t)128 << 20);
     p.nc = p.nc < most ? p.nc : most;
@@ -565,6 +601,8 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
       p.gemm_bytes = b > p.gemm_bytes ? b : p.gemm_bytes;
   p.is_few = p.pieces == 1 && xent_few_ok(layout == MDNN_NT, t, M, N, K);
   p.few = s.take(p.is_few ? (size_t)few_plan(layout == MDNN_NT, N, K).parts * M * K * 4 : 0);
+  const int splits = dx_splits(M, K, N).splits;
+  p.parts = s.take((way == STAGED || way == GENERAL) && p.pieces == 1 && splits > 1 ? (size_t)splits * M * K * 4 : 0);
   p.gemm = s.take(p.gemm_bytes);
   p.bytes = s.at;
   return p;
@@ -695,6 +733,14 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
   return MDNN_SUCCESS;
 }
 
+// Whether a gradient's product of 16-bit operands may split its depth.  From 128
+// tiles of 64 x 64 on, one launch of them is no slower up to this depth than parts
+// and their sum (704 x 1140 x 827 bf16 47.9 -> 31.4 us, 1000 x 5003 x 1000 fp16 76.6 ->
+// 71.7; limits of 2048 and 6000 differ only above).
+bool product_splits(int64_t M, int64_t N, int64_t K) {
+  return ceil_div(M, 64) * ceil_div(N, 64) < 128 || K > 6000;
+}
+
 template <class T>
 mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx,
                       const void* w, int64_t ldw, const float* bias, const int32_t* labels, int32_t ignored,
@@ -760,25 +806,36 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       a.M = M, a.N = N, a.K = K, a.ldx = ldc, a.ldg = p.ldg, a.ldw = q.ldw, a.lddw = lddw, a.by_class = layout == MDNN_NT;
       return xent_few<T>(a, dw ? dw_type : MDNN_F32, dx, lddx, st);
     }
-    if (dx) {
-      const mdnn_layout_t back = layout == MDNN_NN ? MDNN_NT : MDNN_NN;
+    const mdnn_layout_t back = layout == MDNN_NN ? MDNN_NT : MDNN_NN;
+    const SplitPlan sp = dx_splits(M, K, nc);
+    if (dx && (way == STAGED || way == GENERAL) && p.pieces == 1 && sp.splits > 1 &&
+        gemm_reg_ok(t, back, M, K, nc, p.ldg, q.ldw, sp.splits)) {
+      Epilogue ep{};
+      ep.alpha = 1.0f, ep.partial = (float*)(ws + p.parts), ep.k_per_split = sp.k_per_split;
+      MDNN_TRY(gemm_reg(t, MDNN_F32, back, M, K, nc, g, p.ldg, q.w, q.ldw, ep, sp.splits, st));
+      hipLaunchKernelGGL((xent_parts_kernel<T>), dim3(capped(ceil_div(K, 256), 1024), capped(M, 4096)), dim3(256), 0, st,
+                         ep.partial, sp.splits, M, K, alpha, (S*)dx, lddx);
+      MDNN_TRY(check_launch("xent_parts_kernel"));
+    } else if (dx) {
       void* d = joined ? (void*)acc : dx;
       const int64_t ldd = joined ? K : lddx;
+      const size_t gb = product_splits(M, K, nc) ? p.gemm_bytes : 0;
       // (a copied piece's padding is zeros on both sides: whole steps)
       MDNN_TRY(gemm_mixed_ws(back, M, K, way == PACKED ? up(nc, 64) : nc, 1.0f, g, p.ldg, q.w, q.ldw, t,
                              n0 > 0 ? 1.0f : 0.0f, d, ldd, d, ldd, joined ? MDNN_F32 : t, nullptr, MDNN_ACT_NONE, nullptr,
-                             0, gw, p.gemm_bytes, st, nullptr, alpha, 0, way == PACKED ? p.kc : 0));
+                             0, gb ? gw : nullptr, gb, st, nullptr, alpha, 0, way == PACKED ? p.kc : 0));
     }
     if (dw) {
-      const size_t ds = dtype_size(dw_type);
+      const size_t ds = dtype_size(dw_type), gb = product_splits(nc, K, p.rows) ? p.gemm_bytes : 0;
+      void* gv = gb ? gw : nullptr;
       if (layout == MDNN_NN)
         MDNN_TRY(gemm_mixed_ws(MDNN_TN, K, nc, p.rows, 1.0f, copy, p.kc, g, p.ldg, t, 0.0f, nullptr, 0,
-                               (char*)dw + n0 * ds, lddw, dw_type, nullptr, MDNN_ACT_NONE, nullptr, 0, gw, p.gemm_bytes,
-                               st, nullptr, alpha, p.kc, up(nc, 8)));
+                               (char*)dw + n0 * ds, lddw, dw_type, nullptr, MDNN_ACT_NONE, nullptr, 0, gv, gb, st,
+                               nullptr, alpha, p.kc, up(nc, 8)));
       else
         MDNN_TRY(gemm_mixed_ws(MDNN_TN, nc, K, p.rows, 1.0f, g, p.ldg, copy, p.kc, t, 0.0f, nullptr, 0,
-                               (char*)dw + n0 * lddw * ds, lddw, dw_type, nullptr, MDNN_ACT_NONE, nullptr, 0, gw,
-                               p.gemm_bytes, st, nullptr, alpha, up(nc, 8), p.kc));
+                               (char*)dw + n0 * lddw * ds, lddw, dw_type, nullptr, MDNN_ACT_NONE, nullptr, 0, gv,
+                               gb, st, nullptr, alpha, up(nc, 8), p.kc));
     }
   }
   if (dx && joined) {
