@@ -30,11 +30,11 @@ struct XentTile {
   float* zlab;
   uint32_t* done;  // cleared
   // backward: G times `scale` in the operands' type, rows of ldg elements (a multiple of 64), zeros in rows M .. rows - 1
-  // and columns past the piece; part: column sums of tile row t at part[t * classes + n0 + column], or null
+  // and columns past the piece; part: column sums of tile row t at part[t * ldp + column of the piece], or null
   const float* lse;
   float scale;
   void* g;
-  int64_t ldg, rows;
+  int64_t ldg, rows, ldp;
   float* part;
   // where one tile row holds all rows: db itself in place of part (or null), and a = S / counted rows over `scale` to alpha
   bool alone;

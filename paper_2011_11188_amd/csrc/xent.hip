@@ -307,7 +307,7 @@ template <class T>
 __global__ void __launch_bounds__(256)
 xent_grad_kernel(Logits z, int64_t M, int64_t rows, int64_t nc, int64_t n0, const int32_t* labels, int32_t ignored,
                  int64_t N, const float* lse, float scale, typename T::storage* g, int64_t ldg, float* part,
-                 const float* loss_scale, float* alpha) {
+                 int64_t ldp, const float* loss_scale, float* alpha) {
   typedef typename T::storage S;
   if (alpha && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {  // (few rows)
     int n = 0;
@@ -353,7 +353,7 @@ xent_grad_kernel(Logits z, int64_t M, int64_t rows, int64_t nc, int64_t n0, cons
     if (part) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (c + e < nc) part[b * N + n0 + c + e] = sum[e];
+        if (c + e < nc) part[b * ldp + c + e] = sum[e];
     }
   }
 }
@@ -591,7 +591,7 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
     p.z = s.take(za > zb ? za : zb);
   }
   p.g = s.take((size_t)p.rows * p.ldg * es);
-  p.part = s.take((size_t)p.blocks * N * 4);
+  p.part = s.take((size_t)p.blocks * p.nc * 4);
   p.acc = s.take(h && p.pieces > 1 ? (size_t)M * K * 4 : 0);
   p.ldw = layout == MDNN_NN ? p.ldg : p.kc;
   p.pack = s.take(way == PACKED ? (size_t)(layout == MDNN_NN ? p.kc : p.ldg) * p.ldw * 2 : 0);
@@ -782,7 +782,8 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       MDNN_TRY(general_logits(layout, M, nc, K, copy, ldc, q.w, ldw, t, b, z, p.ldg, gw, p.gemm_bytes, l, st));
       hipLaunchKernelGGL((xent_grad_kernel<T>),
                          dim3((unsigned)ceil_div(p.ldg, 1024), capped(ceil_div(p.rows, GRAD_ROWS), 65535)), dim3(256), 0, st, l, M,
-                         p.rows, nc, n0, labels, ignored, N, lse, scale, g, p.ldg, part, loss_scale, here ? alpha : nullptr);
+                         p.rows, nc, n0, labels, ignored, N, lse, scale, g, p.ldg, part, p.nc, loss_scale,
+                         here ? alpha : nullptr);
       MDNN_TRY(check_launch("xent_grad_kernel"));
     } else {
       MDNN_TRY(take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
@@ -791,11 +792,11 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.lse = lse, e.scale = scale;
       blocks = ceil_div(M, way_tile(way, M, nc, K, true));
       e.alone = blocks == 1, e.loss_scale = loss_scale, e.alpha = alpha, e.db = e.alone ? db : nullptr;
-      e.g = g, e.ldg = p.ldg, e.rows = p.rows, e.part = e.alone ? nullptr : part;
+      e.g = g, e.ldg = p.ldg, e.rows = p.rows, e.ldp = p.nc, e.part = e.alone ? nullptr : part;
       MDNN_TRY(tiles<T>(way, a, e, st));
     }
     if (db && (way == GENERAL || blocks > 1)) {
-      hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(nc, 64)), dim3(256), 0, st, part + n0, blocks, N, nc, alpha,
+      hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(nc, 64)), dim3(256), 0, st, part, blocks, p.nc, nc, alpha,
                          scale, db + n0);
       MDNN_TRY(check_launch("xent_db_kernel"));
     }

@@ -175,7 +175,7 @@ __device__ __forceinline__ void xent_end(const XentTile& x, const XentNumbers<TL
         if (x.db)
           x.db[x.n0 + n0 + c] = s * (alpha * x.scale);
         else
-          x.part[tm * x.classes + x.n0 + n0 + c] = s;
+          x.part[tm * x.ldp + n0 + c] = s;
       }
     }
   }
