@@ -829,6 +829,15 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
     if (dw) {
       const size_t ds = dtype_size(dw_type), gb = product_splits(nc, K, p.rows) ? p.gemm_bytes : 0;
       void* gv = gb ? gw : nullptr;
+      if constexpr (H) {
+        if (p.rows == 64 && (layout == MDNN_NN ? xent_outer_ok(K, nc) : xent_outer_ok(nc, K))) {
+          if (layout == MDNN_NN)
+            MDNN_TRY(xent_outer<T>(copy, p.kc, K, g, p.ldg, nc, alpha, (char*)dw + n0 * ds, lddw, dw_type, st));
+          else
+            MDNN_TRY(xent_outer<T>(g, p.ldg, nc, copy, p.kc, K, alpha, (char*)dw + n0 * lddw * ds, lddw, dw_type, st));
+          continue;
+        }
+      }
       if (layout == MDNN_NN)
         MDNN_TRY(gemm_mixed_ws(MDNN_TN, K, nc, p.rows, 1.0f, copy, p.kc, g, p.ldg, t, 0.0f, nullptr, 0,
                                (char*)dw + n0 * ds, lddw, dw_type, nullptr, MDNN_ACT_NONE, nullptr, 0, gv, gb, st,

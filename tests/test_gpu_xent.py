@@ -164,6 +164,15 @@ def test_gradients(mdnn, size, by_class, dtype):
         Problem(*size, dtype, by_class, bias, pad, offset).check_backward(mdnn, scale, dw)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (8, 8), (3, 1)])
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("by_class", [False, True])
+@pytest.mark.parametrize("m,n,k", [(9, 5003, 1000), (33, 1031, 1100), (64, 4097, 520)])
+def test_gradients_of_a_few_dozen_rows(mdnn, m, n, k, by_class, wide, pad, offset, dtype):
+    Problem(m, n, k, dtype, by_class, pad=pad, offset=offset).check_backward(mdnn, dw_type="f32" if wide else dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("m,n,k,by_class", [(4100, 9000, 64, False), (4096, 8192, 128, True), (9000, 20011, 32, True),
                                             (1000, 70001, 40, False), (20000, 4100, 72, False), (70, 131072, 520, True),
