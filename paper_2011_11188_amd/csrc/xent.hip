@@ -33,10 +33,10 @@ namespace mdnn {
 
 // 256 from one tile a CU on, but for so few steps that a tile is mostly its end,
 // which two workgroups a CU of 128 run beside each other's (backward 8192 x 16384 x
-// 128 bf16 371 us, 256 403; x 256, 4096 x 32768, 509 and 490; forward 9024 x 4416 x
-// 64 35.5 and 37.0, 8192 x 16384 x 128 95 and 88).  Then 128 from one a CU on (64:
-// 2000 x 3000 x 512 25.8 us, 128 18.7; 300 x 20000 x 640 33.8 and 24.5; 100 x 32768 x
-// 4096 93 and 80), for rows that fill them.
+// 128 bf16 312 us, 256 325; 4096 x 32768 x 256 440 and 430; forward 9024 x 4416 x 64
+// 32.0 and 33.1, 8192 x 16384 x 128 87 and 81).  Then 128 from one a CU on (64: 2000 x
+// 3008 x 512 fp16 23.6 us, 128 17.8; 300 x 20032 x 640 bf16 31.5 and 22.9; 100 x 32768
+// x 4096 fp16 89 and 76), for rows that fill them.
 int xent_tile(int64_t M, int64_t N, int64_t K, bool backward) {
   auto tiles = [&](int64_t side) { return ceil_div(M, side) * ceil_div(N, side); };
   if (M > 128 && tiles(256) >= 256 && K > (backward ? 128 : 64)) return 256;
