@@ -244,30 +244,52 @@ __device__ __forceinline__ uint4 chunk16(const S* row, int64_t c, int64_t cols) 
 }
 
 // [rows][cols] of 16-bit elements at any address to rows of ldc (a multiple of
-// 8), zeros past cols and in rows .. all - 1.
-__global__ void __launch_bounds__(256)
-xent_pack_kernel(const uint16_t* src, int64_t ld, int64_t rows, int64_t cols, uint16_t* dst, int64_t all, int64_t ldc) {
-  const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
-  if (c >= ldc) return;
-  for (int64_t r0 = ((int64_t)blockIdx.y * 4 + (threadIdx.x >> 6)) * 4; r0 < all; r0 += (int64_t)gridDim.y * 16) {
+// 8), zeros past cols and in rows .. all - 1; gx by gy blocks.
+struct Pack {
+  const uint16_t* src;
+  int64_t ld, rows, cols;
+  uint16_t* dst;
+  int64_t all, ldc;
+  uint32_t gx, gy;
+};
+
+__device__ __forceinline__ void pack_block(const Pack& p, uint32_t block) {
+  const int64_t c = ((int64_t)(block % p.gx) * 64 + (threadIdx.x & 63)) * 8;
+  if (c >= p.ldc) return;
+  for (int64_t r0 = ((int64_t)(block / p.gx) * 4 + (threadIdx.x >> 6)) * 4; r0 < p.all; r0 += (int64_t)p.gy * 16) {
     uint4 v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = r0 + k < rows ? chunk16(src + (r0 + k) * ld, c, cols) : make_uint4(0, 0, 0, 0);
+    for (int k = 0; k < 4; ++k)
+      v[k] = r0 + k < p.rows ? chunk16(p.src + (r0 + k) * p.ld, c, p.cols) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (r0 + k < all) *(uint4*)(dst + (r0 + k) * ldc + c) = v[k];
+      if (r0 + k < p.all) *(uint4*)(p.dst + (r0 + k) * p.ldc + c) = v[k];
   }
+}
+
+// One copy, or two beside each other.
+__global__ void __launch_bounds__(256) xent_pack_kernel(Pack a, Pack b) {
+  const uint32_t first = a.gx * a.gy;
+  if (blockIdx.x < first)
+    pack_block(a, blockIdx.x);
+  else
+    pack_block(b, blockIdx.x - first);
 }
 
 // Block 0 counts the rows with a label that is not ignored and leaves
 // a = S / count, times `scale`; the others copy x to rows of ldc elements,
 // ignored rows, rows past M and columns past K as zeros (what an ignored row
-// holds, Inf and NaN among it, must not reach dW as 0 * Inf).
+// holds, Inf and NaN among it, must not reach dW as 0 * Inf).  Blocks from `own` on
+// copy W's first piece, where that is packed.
 template <class T>
 __global__ void __launch_bounds__(256)
 xent_prepare_kernel(const typename T::storage* x, int64_t ldx, int64_t M, int64_t K, const int32_t* labels,
                     int32_t ignored, const float* loss_scale, float scale, float* alpha, typename T::storage* copy,
-                    int64_t rows, int64_t ldc) {
+                    int64_t rows, int64_t ldc, uint32_t own, Pack w) {
+  if (blockIdx.x >= own) {
+    pack_block(w, blockIdx.x - own);
+    return;
+  }
   if (blockIdx.x == 0) {
     __shared__ int64_t buf[4];
     int64_t n = 0;
@@ -290,7 +312,7 @@ xent_prepare_kernel(const typename T::storage* x, int64_t ldx, int64_t M, int64_
   }
   constexpr int E = 16 / sizeof(typename T::storage);  // elements of a 16-byte chunk
   const int64_t per = ldc / E;
-  for (int64_t row = blockIdx.x - 1; row < rows; row += gridDim.x - 1) {
+  for (int64_t row = blockIdx.x - 1; row < rows; row += own - 1) {
     const bool live = row < M && labels[row < M ? row : 0] != ignored;
     const typename T::storage* p = x + row * ldx;
     for (int64_t c = threadIdx.x; c < per; c += 256) {
@@ -459,7 +481,8 @@ struct Space {
 };
 
 // K split of a general piece's logits where their tiles are few (1: the
-// product's own ways), at least 256 deep, parts of at most 32 MB.
+// product's own ways), at least 256 deep (8 x 3619 over 1216 fp32 23 us a call, 128
+// deep 27), parts of at most 32 MB.
 SplitPlan logit_splits(int64_t M, int64_t nc, int64_t K) {
   SplitPlan p{1, K};
   const int64_t tiles = ceil_div(M, 64) * ceil_div(nc, 64);
@@ -541,11 +564,14 @@ FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
 
 // Depth split of dx on the register-staged kernel, whose classes are the depth:
 // two rounds of two workgroups a CU (500 x 777 over 10007 fp32 198 us on its 104
-// tiles), at least 512 deep, parts of at most 64 MB.
-SplitPlan dx_splits(int64_t M, int64_t K, int64_t depth) {
+// tiles), parts of at most 64 MB and, as a step of fp32 takes several times one of
+// 16 bits, at least 128 deep (14 x 514 over 1392 33.5 us a call, 512 deep 43.2) or
+// 512 (128 x 1664 over 2176 fp16 39.3, 128 deep 43.0).
+SplitPlan dx_splits(int64_t M, int64_t K, int64_t depth, mdnn_dtype_t t) {
+  const int64_t least = t == MDNN_F32 ? 128 : 512;
   SplitPlan p{1, depth};
   int64_t n = 1024 / (ceil_div(M, 64) * ceil_div(K, 64));
-  n = n < depth / 512 ? n : depth / 512;
+  n = n < depth / least ? n : depth / least;
   const int64_t most = ((int64_t)16 << 20) / (M * K);
   n = n < most ? n : most;
   if (n < 2) return p;
@@ -601,7 +627,7 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
       p.gemm_bytes = b > p.gemm_bytes ? b : p.gemm_bytes;
   p.is_few = p.pieces == 1 && xent_few_ok(layout == MDNN_NT, t, M, N, K);
   p.few = s.take(p.is_few ? (size_t)few_plan(layout == MDNN_NT, N, K).parts * M * K * 4 : 0);
-  const int splits = dx_splits(M, K, N).splits;
+  const int splits = dx_splits(M, K, N, t).splits;
   p.parts = s.take((way == STAGED || way == GENERAL) && p.pieces == 1 && splits > 1 ? (size_t)splits * M * K * 4 : 0);
   p.gemm = s.take(p.gemm_bytes);
   p.bytes = s.at;
@@ -652,29 +678,33 @@ const void* w_piece(mdnn_layout_t layout, const void* w, int64_t ldw, int64_t n0
 
 unsigned capped(int64_t n, int64_t most) { return (unsigned)(n < most ? n : most); }
 
-mdnn_status_t pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t all, int64_t ldc,
-                   hipStream_t st) {
-  hipLaunchKernelGGL(xent_pack_kernel, dim3((unsigned)ceil_div(ldc, 512), capped(ceil_div(all, 16), 65535)), dim3(256), 0,
-                     st, (const uint16_t*)src, ld, rows, cols, (uint16_t*)dst, all, ldc);
+Pack pack_of(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t all, int64_t ldc) {
+  const int64_t gx = ceil_div(ldc, 512), most = ((int64_t)1 << 22) / gx;
+  return {(const uint16_t*)src, ld, rows, cols, (uint16_t*)dst, all, ldc, (uint32_t)gx,
+          capped(ceil_div(all, 16), most < 1 ? 1 : most)};
+}
+// (either may be empty)
+mdnn_status_t pack(const Pack& a, const Pack& b, hipStream_t st) {
+  const uint32_t blocks = a.gx * a.gy + b.gx * b.gy;
+  if (blocks == 0) return MDNN_SUCCESS;
+  hipLaunchKernelGGL(xent_pack_kernel, dim3(blocks), dim3(256), 0, st, a, b);
   return check_launch("xent_pack_kernel");
 }
 
 // Classes n0 .. n0 + nc - 1 of W as the tiles read them: in place, or copied to
-// rows of ldc, zeros past the sizes (the depth to kc, classes to a multiple of 64).
+// rows of ldc by `copy`, zeros past the sizes (the depth to kc, classes to a multiple of 64).
 struct Piece {
   const void* w;
   int64_t ldw, ext;  // ext: classes that class-contiguous rows have memory for
 };
-mdnn_status_t take_piece(Way way, mdnn_layout_t layout, const void* w, int64_t ldw, size_t es, int64_t n0, int64_t nc,
-                         int64_t K, int64_t kc, void* room, int64_t ldc, Piece& out, hipStream_t st) {
+Piece take_piece(Way way, mdnn_layout_t layout, const void* w, int64_t ldw, size_t es, int64_t n0, int64_t nc, int64_t K,
+                 int64_t kc, void* room, int64_t ldc, Pack& copy) {
   const void* p = w_piece(layout, w, ldw, n0, es);
-  if (way != PACKED) {
-    out = {p, ldw, nc};
-    return MDNN_SUCCESS;
-  }
+  copy = {};
+  if (way != PACKED) return {p, ldw, nc};
   const int64_t all = up(nc, 64);
-  out = {room, ldc, all};
-  return layout == MDNN_NN ? pack(p, ldw, K, nc, room, kc, ldc, st) : pack(p, ldw, nc, K, room, all, ldc, st);
+  copy = layout == MDNN_NN ? pack_of(p, ldw, K, nc, room, kc, ldc) : pack_of(p, ldw, nc, K, room, all, ldc);
+  return {room, ldc, all};
 }
 
 template <class T>
@@ -695,8 +725,9 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
   float *zlab = (float*)(ws + p.zlab), *z = (float*)(ws + p.z);
   Tally* tally = (Tally*)(ws + p.tally);
   uint32_t* done = (uint32_t*)(ws + p.done);
+  Pack x_copy = {};
   if (way < STAGED && !(aligned(x, 16) && ldx % 8 == 0 && K % 64 == 0 && (M + 255) * ldx < (int64_t)1 << 31)) {
-    MDNN_TRY(pack(x, ldx, M, K, ws + p.copy, M, p.kc, st));
+    x_copy = pack_of(x, ldx, M, K, ws + p.copy, M, p.kc);
     x = ws + p.copy, ldx = p.kc;
   }
   for (int64_t i = 0; i < p.pieces; ++i) {
@@ -712,8 +743,10 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
                          done);
       MDNN_TRY(check_launch("xent_stats_kernel"));
     } else {
-      Piece q;
-      MDNN_TRY(take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
+      Pack copy;
+      const Piece q = take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, copy);
+      MDNN_TRY(pack(x_copy, copy, st));
+      x_copy = {};
       XentProduct a = {x, q.w, ldx, q.ldw, M, nc, way == STAGED ? K : p.kc, q.ext, layout == MDNN_NT, false};
       XentTile e = {};
       e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.pairs = pairs, e.zlab = zlab, e.done = done;
@@ -767,8 +800,11 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
   if (here) {
     copy = (S*)x;
   } else {
-    hipLaunchKernelGGL((xent_prepare_kernel<T>), dim3(capped(p.rows, 1 << 16) + 1), dim3(256), 0, st, (const S*)x, ldx, M,
-                       K, labels, ignored, loss_scale, 1.0f / scale, alpha, copy, p.rows, p.kc);
+    const uint32_t own = capped(p.rows, 1 << 16) + 1;
+    Pack first;
+    take_piece(way, layout, w, ldw, dtype_size(t), 0, p.nc < N ? p.nc : N, K, p.kc, ws + p.pack, p.ldw, first);
+    hipLaunchKernelGGL((xent_prepare_kernel<T>), dim3(own + first.gx * first.gy), dim3(256), 0, st, (const S*)x, ldx, M, K,
+                       labels, ignored, loss_scale, 1.0f / scale, alpha, copy, p.rows, p.kc, own, first);
     MDNN_TRY(check_launch("xent_prepare_kernel"));
   }
   const int64_t ldc = here ? ldx : p.kc;
@@ -786,7 +822,9 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
                          here ? alpha : nullptr);
       MDNN_TRY(check_launch("xent_grad_kernel"));
     } else {
-      MDNN_TRY(take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, q, st));
+      Pack next;
+      q = take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, next);
+      if (n0 > 0) MDNN_TRY(pack(next, {}, st));  // (the first is copied beside x)
       XentProduct a = {copy, q.w, ldc, q.ldw, M, nc, way == STAGED ? K : p.kc, q.ext, layout == MDNN_NT, true};
       XentTile e = {};
       e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.lse = lse, e.scale = scale;
@@ -808,7 +846,7 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       return xent_few<T>(a, dw ? dw_type : MDNN_F32, dx, lddx, st);
     }
     const mdnn_layout_t back = layout == MDNN_NN ? MDNN_NT : MDNN_NN;
-    const SplitPlan sp = dx_splits(M, K, nc);
+    const SplitPlan sp = dx_splits(M, K, nc, t);
     if (dx && (way == STAGED || way == GENERAL) && p.pieces == 1 && sp.splits > 1 &&
         gemm_reg_ok(t, back, M, K, nc, p.ldg, q.ldw, sp.splits)) {
       Epilogue ep{};

@@ -25,7 +25,8 @@ __device__ __forceinline__ bool counts(const XentFew& a, int m) {
 constexpr int FEW_TILE = 64;  // rows of W whose numbers a block holds in LDS at a time
 
 // W [N][K]: a thread's columns k of x in registers, the classes' G through LDS.
-// Sums over a block's classes go to part[split * groups + group][m][K].
+// Sums over a block's classes go to part[split][m][K], its groups of threads joined by
+// shuffles and through LDS.
 template <class T, class OutT, int MR>
 __global__ void __launch_bounds__(256) xent_few_by_class_kernel(XentFew a) {
   typedef typename T::storage S;
@@ -82,13 +83,32 @@ __global__ void __launch_bounds__(256) xent_few_by_class_kernel(XentFew a) {
       }
     }
   }
-  if (!a.part || pos.lo == 8) return;
+  if (!a.part) return;
+  __shared__ float4_t sums[256][2];
+  const int own = tx < 64 ? 64 : tx;  // threads with sums of their own, once a wave's are joined
 #pragma unroll
   for (int m = 0; m < MR; ++m) {
-    if (m >= a.M) break;
-    Chunk<F32> o;
-    o.set(acc[m]);
-    o.store(a.part + (((int64_t)blockIdx.y * groups + grp) * a.M + m) * a.K + pos.start, pos.lo);
+    if (m >= a.M) break;  // (uniform)
+    for (int o = tx; o < 64; o <<= 1) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[m][e] += __shfl_xor(acc[m][e], o, 64);
+    }
+    if (own < 256) {
+      __syncthreads();
+      sums[threadIdx.x][0] = (float4_t){acc[m][0], acc[m][1], acc[m][2], acc[m][3]};
+      sums[threadIdx.x][1] = (float4_t){acc[m][4], acc[m][5], acc[m][6], acc[m][7]};
+      __syncthreads();
+      if ((int)threadIdx.x < tx)
+        for (int t = (int)threadIdx.x + own; t < 256; t += own) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[m][e] += sums[t][e >> 2][e & 3];
+        }
+    }
+    if ((int)threadIdx.x < tx && pos.lo < 8) {
+      Chunk<F32> o;
+      o.set(acc[m]);
+      o.store(a.part + ((int64_t)blockIdx.y * a.M + m) * a.K + pos.start, pos.lo);
+    }
   }
 }
 
@@ -226,8 +246,8 @@ void launch_rows(const XentFew& a, const FewPlan& p, hipStream_t st) {
 }  // namespace
 
 // Strips of W's contiguous dimension, and splits of the other one: two blocks a
-// CU where each leaves its own sums for dx (by class), else four; at least 16 (4)
-// rows of W to a thread group, so that the sums stay small beside W.
+// CU where each leaves its own sums for dx (by class), else four; at least 4 rows
+// of W to a thread group (by class 8 x 3000 x 64 fp32 18.9 us, 16 rows 25.7).
 FewPlan few_plan(bool by_class, int64_t N, int64_t K) {
   FewPlan p;
   const int64_t across = by_class ? K : N, along = by_class ? N : K, chunks = ceil_div(across, 8);
@@ -236,11 +256,11 @@ FewPlan few_plan(bool by_class, int64_t N, int64_t K) {
     while (p.tx > 16 && p.tx / 2 >= chunks) p.tx /= 2;
   p.strips = ceil_div(chunks, p.tx);
   const int groups = 256 / p.tx;
-  int64_t n = ceil_div(by_class ? 512 : 1024, p.strips), most = ceil_div(along, by_class ? 16 * groups : 4);
+  int64_t n = ceil_div(by_class ? 512 : 1024, p.strips), most = ceil_div(along, by_class ? 4 * groups : 4);
   n = n < most ? n : most;
   p.per = ceil_div(along, n);
   p.splits = ceil_div(along, p.per);
-  p.parts = by_class ? p.splits * groups : p.strips;
+  p.parts = by_class ? p.splits : p.strips;
   return p;
 }
 
