@@ -450,16 +450,22 @@ int64_t piece_classes(int64_t N, int64_t rows, int64_t elems) {
 // the caller's workspace holds every way that its sizes allow.
 enum Way { TILED, PACKED, STAGED, GENERAL };
 
-// Rows from which copying W pays (two passes over it at memory speed against
-// products at about twice the register-staged kernel's rate).
-bool pack_pays(int64_t M, bool backward) { return M >= (backward ? 256 : 512); }
+// Where copying W pays (two passes over it at memory speed and a launch, against
+// products at about twice the register-staged kernel's rate): by the rows and by the
+// whole product.  Forward, copied and not: 1000 x 5003 x 1000 fp16 30.5 and 36.9 us,
+// 400 x 14787 x 6490 bf16 190 and 238, but 320 x 40805 x 955 94 and 64, 1000 x 3001 x
+// 301 22.6 and 17.5; backward: 320 x 14787 x 6490 439 and 510, 1000 x 2049 x 650 40 and
+// 49, but 192 x 40805 x 955 173 and 161, 1000 x 3001 x 301 46.4 and 39.6.
+bool pack_pays(int64_t M, int64_t N, int64_t K, bool backward) {
+  return M >= (backward ? 256 : 384) && (double)M * N * K >= (backward ? 0x1p30 : 0x1p32);
+}
 
 Way way_by_size(int64_t M, int64_t N, int64_t K, mdnn_dtype_t t, bool backward) {
   // (a grid of less than half the chip's CUs over a long K: split in the general product)
   if (ceil_div(M, 64) * ceil_div(N, 64) < 128 && K > 512) return GENERAL;
   if (t != MDNN_F32 && M * up(K, 64) < (int64_t)1 << 31) {  // (32-bit offsets reach every row of x)
     if ((N % 64 == 0 || (!backward && N % 8 == 0)) && K % 64 == 0) return TILED;
-    if (pack_pays(M, backward)) return PACKED;
+    if (pack_pays(M, N, K, backward)) return PACKED;
   }
   const int64_t e = 16 / (int64_t)dtype_size(t);
   return K >= e && N >= e ? STAGED : GENERAL;

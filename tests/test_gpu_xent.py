@@ -173,6 +173,16 @@ def test_gradients_of_a_few_dozen_rows(mdnn, m, n, k, by_class, wide, pad, offse
     Problem(m, n, k, dtype, by_class, pad=pad, offset=offset).check_backward(mdnn, dw_type="f32" if wide else dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (3, 1)])
+@pytest.mark.parametrize("by_class", [False, True])
+@pytest.mark.parametrize("m,n,k", [(700, 5003, 1301), (401, 12008, 901), (385, 9024, 1300)])
+def test_odd_sizes_of_large_products(mdnn, m, n, k, by_class, pad, offset, dtype):
+    p = Problem(m, n, k, dtype, by_class, pad=pad, offset=offset)
+    p.check_forward(mdnn)
+    p.check_backward(mdnn, dw_type=dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("m,n,k,by_class", [(4100, 9000, 64, False), (4096, 8192, 128, True), (9000, 20011, 32, True),
                                             (1000, 70001, 40, False), (20000, 4100, 72, False), (70, 131072, 520, True),
