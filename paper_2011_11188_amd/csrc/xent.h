@@ -85,11 +85,11 @@ bool xent_few_ok(bool by_class, mdnn_dtype_t t, int64_t M, int64_t N, int64_t K)
 template <class T>
 mdnn_status_t xent_few(XentFew a, mdnn_dtype_t dw_type, void* dx, int64_t lddx, hipStream_t st);
 
-// D [R][ldd] of d_type = *alpha * P^T Q for 64 rows of 16-bit P [64][ldp >= R] and Q [64][ldq >= C] on 16 bytes, leading
-// dimensions up(R, 64) and up(C, 64) (xent_outer.hip).
-bool xent_outer_ok(int64_t R, int64_t C);
+// D [R][ldd] of d_type = *alpha * P^T Q for `rows` rows, a multiple of 64, of 16-bit P [rows][ldp >= R] and Q [rows][ldq
+// >= C] on 16 bytes, leading dimensions up(R, 64) and up(C, 64) (xent_outer.hip).
+bool xent_outer_ok(int64_t R, int64_t C, int64_t rows);
 template <class T>
-mdnn_status_t xent_outer(const void* p, int64_t ldp, int64_t R, const void* q, int64_t ldq, int64_t C, const float* alpha,
-                         void* d, int64_t ldd, mdnn_dtype_t d_type, hipStream_t st);
+mdnn_status_t xent_outer(const void* p, int64_t ldp, int64_t R, const void* q, int64_t ldq, int64_t C, int64_t rows,
+                         const float* alpha, void* d, int64_t ldd, mdnn_dtype_t d_type, hipStream_t st);
 
 }  // namespace mdnn

@@ -874,11 +874,11 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
       const size_t ds = dtype_size(dw_type), gb = product_splits(nc, K, p.rows) ? p.gemm_bytes : 0;
       void* gv = gb ? gw : nullptr;
       if constexpr (H) {
-        if (p.rows == 64 && (layout == MDNN_NN ? xent_outer_ok(K, nc) : xent_outer_ok(nc, K))) {
+        if (layout == MDNN_NN ? xent_outer_ok(K, nc, p.rows) : xent_outer_ok(nc, K, p.rows)) {
           if (layout == MDNN_NN)
-            MDNN_TRY(xent_outer<T>(copy, p.kc, K, g, p.ldg, nc, alpha, (char*)dw + n0 * ds, lddw, dw_type, st));
+            MDNN_TRY(xent_outer<T>(copy, p.kc, K, g, p.ldg, nc, p.rows, alpha, (char*)dw + n0 * ds, lddw, dw_type, st));
           else
-            MDNN_TRY(xent_outer<T>(g, p.ldg, nc, copy, p.kc, K, alpha, (char*)dw + n0 * lddw * ds, lddw, dw_type, st));
+            MDNN_TRY(xent_outer<T>(g, p.ldg, nc, copy, p.kc, K, p.rows, alpha, (char*)dw + n0 * lddw * ds, lddw, dw_type, st));
           continue;
         }
       }

@@ -1,12 +1,14 @@
-// dW of up to 64 rows of 16-bit operands: D[r][c] = a * sum over m of P[m][r] Q[m][c],
-// m < 64, P and Q rows on 16 bytes in the workspace (x's copy and G).
+// dW of up to 512 rows of 16-bit operands: D[r][c] = a * sum over m of P[m][r] Q[m][c],
+// P and Q rows on 16 bytes in the workspace (x's copy and G).
 //
-// Bound: D's writes.  The product is one 64-deep step; the GEMM's tiles store it as
+// Bound: D's writes.  The product is few 64-deep steps; the GEMM's tiles store it as
 // the matrix instruction leaves it, 16 rows by 8 bytes of every lane, at 3.3
 // TB/s on 16-byte rows and 1.1 on others (6912 x 27552 fp16 117-133 us, x 27551 358).
 // Here a tile turns in LDS and leaves in whole rows, 16 bytes a lane, at any
 // element address: a call's time, 64 x 32768 x 4096 bf16 by feature 475 -> 240 us, by
 // class fp16 257 -> 212, 32 x 27551 x 6912 fp16 397 -> 300, 16 x 32768 x 1024 bf16 74 -> 56.
+// A step's loads are waited for at once: three workgroups a CU run beside each
+// other (256 x 32768 x 4096 bf16 443 -> 382 us, 512 x 20000 x 2048 245 -> 222).
 #include "gemm_lds.h"
 #include "internal.h"
 #include "row_chunk.h"
@@ -19,7 +21,8 @@ typedef lds::Tile<64, 256, 1, 4, 3> TileOuter;
 
 template <class T, class OutT>
 __global__ void __launch_bounds__(TileOuter::NT, TileOuter::OCC)
-xent_outer_kernel(lds::MatArgs pa, lds::MatArgs qa, int64_t R, int64_t C, const float* alpha, void* d, int64_t ldd) {
+xent_outer_kernel(lds::MatArgs pa, lds::MatArgs qa, int64_t R, int64_t C, int steps, const float* alpha, void* d,
+                  int64_t ldd) {
   typedef TileOuter TL;
   typedef lds::MatLoader<false, TL::BM, TL::LA> LA;
   typedef lds::MatLoader<false, TL::BN, TL::LB> LB;
@@ -40,28 +43,31 @@ xent_outer_kernel(lds::MatArgs pa, lds::MatArgs qa, int64_t R, int64_t C, const 
   LB lb;
   la.init(pa, r0, 0, wave, lane);
   lb.init(qa, c0, 0, wave, lane);
-  la.issue(0, lds::lds_address(sa) + (uint32_t)(wave * TL::LA) * 1024u);
-  lb.issue(0, lds::lds_address(sb) + (uint32_t)(wave * TL::LB) * 1024u);
   const float a = *alpha;
-  lds::wait_vm_lgkm0<0>();
-  __syncthreads();
   const lds::LaneFrag fa = lds::lane_frag<false, TL::BM>(lane), fb = lds::lane_frag<false, TL::BN>(lane);
   float4_t acc[TL::FM][TL::FN];
 #pragma unroll
   for (int i = 0; i < TL::FM; ++i)
 #pragma unroll
     for (int j = 0; j < TL::FN; ++j) acc[i][j] = (float4_t){0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < steps; ++s) {
+    if (s > 0) __syncthreads();  // (the last step's reads are done)
+    la.issue(s, lds::lds_address(sa) + (uint32_t)(wave * TL::LA) * 1024u);
+    lb.issue(s, lds::lds_address(sb) + (uint32_t)(wave * TL::LB) * 1024u);
+    lds::wait_vm_lgkm0<0>();
+    __syncthreads();
 #pragma unroll
-  for (int kk = 0; kk < 2; ++kk) {
-    uint4 fragA[TL::FM], fragB[TL::FN];
+    for (int kk = 0; kk < 2; ++kk) {
+      uint4 fragA[TL::FM], fragB[TL::FN];
 #pragma unroll
-    for (int i = 0; i < TL::FM; ++i) fragA[i] = lds::fragment<false, TL::BM>(sa, i * 16, kk, fa);
+      for (int i = 0; i < TL::FM; ++i) fragA[i] = lds::fragment<false, TL::BM>(sa, i * 16, kk, fa);
 #pragma unroll
-    for (int j = 0; j < TL::FN; ++j) fragB[j] = lds::fragment<false, TL::BN>(sb, wave * TL::WTN + j * 16, kk, fb);
+      for (int j = 0; j < TL::FN; ++j) fragB[j] = lds::fragment<false, TL::BN>(sb, wave * TL::WTN + j * 16, kk, fb);
 #pragma unroll
-    for (int i = 0; i < TL::FM; ++i)
+      for (int i = 0; i < TL::FM; ++i)
 #pragma unroll
-      for (int j = 0; j < TL::FN; ++j) acc[i][j] = Mfma<T>::run(fragB[j], fragA[i], acc[i][j]);
+        for (int j = 0; j < TL::FN; ++j) acc[i][j] = Mfma<T>::run(fragB[j], fragA[i], acc[i][j]);
+    }
   }
   constexpr int PER = TL::BN / E;  // threads of a row
 #pragma unroll
@@ -110,30 +116,32 @@ xent_outer_kernel(lds::MatArgs pa, lds::MatArgs qa, int64_t R, int64_t C, const 
 
 }  // namespace
 
-// More tiles than 64 (64 x 1000 x 777 bf16, 64 tiles either way round: 30.0 us against the
-// GEMM's 29.4; 9 x 5003 x 1000 fp16, 320: 32.5 against 36.0), and the loaders' 32-bit
-// offsets reach 64 rows.
-bool xent_outer_ok(int64_t R, int64_t C) {
+// Up to 512 rows (512 x 60001 x 577 bf16 256 us against the GEMM's 245, 384 237 and 237,
+// 1000 443 and 384; 1000 x 32768 x 4096 831 and 847), more tiles than 64 (64 x 1000 x 777
+// bf16, 64 either way round: 30.0 against 29.4; 9 x 5003 x 1000 fp16, 320: 32.5 against
+// 36.0), and the loaders' 32-bit offsets reach a step's 64 rows.
+bool xent_outer_ok(int64_t R, int64_t C, int64_t rows) {
   const int64_t tiles = ceil_div(R, TileOuter::BM) * ceil_div(C, TileOuter::BN);
-  return R < (int64_t)1 << 24 && C < (int64_t)1 << 24 && tiles > 64 && tiles < (int64_t)1 << 24;
+  return rows <= 512 && R < (int64_t)1 << 24 && C < (int64_t)1 << 24 && tiles > 64 && tiles < (int64_t)1 << 24;
 }
 
 template <class T>
-mdnn_status_t xent_outer(const void* p, int64_t ldp, int64_t R, const void* q, int64_t ldq, int64_t C, const float* alpha,
-                         void* d, int64_t ldd, mdnn_dtype_t d_type, hipStream_t st) {
+mdnn_status_t xent_outer(const void* p, int64_t ldp, int64_t R, const void* q, int64_t ldq, int64_t C, int64_t rows,
+                         const float* alpha, void* d, int64_t ldd, mdnn_dtype_t d_type, hipStream_t st) {
+  const int steps = (int)(rows / 64);
   const lds::MatArgs a{p, ldp, ceil_div(R, 8) * 8}, b{q, ldq, ceil_div(C, 8) * 8};
   const int64_t tiles = ceil_div(R, TileOuter::BM) * ceil_div(C, TileOuter::BN);
   if (d_type == MDNN_F32)
-    hipLaunchKernelGGL((xent_outer_kernel<T, F32>), dim3((unsigned)tiles), dim3(TileOuter::NT), 0, st, a, b, R, C, alpha, d,
-                       ldd);
+    hipLaunchKernelGGL((xent_outer_kernel<T, F32>), dim3((unsigned)tiles), dim3(TileOuter::NT), 0, st, a, b, R, C, steps,
+                       alpha, d, ldd);
   else
-    hipLaunchKernelGGL((xent_outer_kernel<T, T>), dim3((unsigned)tiles), dim3(TileOuter::NT), 0, st, a, b, R, C, alpha, d,
-                       ldd);
+    hipLaunchKernelGGL((xent_outer_kernel<T, T>), dim3((unsigned)tiles), dim3(TileOuter::NT), 0, st, a, b, R, C, steps,
+                       alpha, d, ldd);
   return check_launch("xent_outer_kernel");
 }
-template mdnn_status_t xent_outer<F16>(const void*, int64_t, int64_t, const void*, int64_t, int64_t, const float*, void*,
-                                       int64_t, mdnn_dtype_t, hipStream_t);
-template mdnn_status_t xent_outer<BF16>(const void*, int64_t, int64_t, const void*, int64_t, int64_t, const float*, void*,
-                                        int64_t, mdnn_dtype_t, hipStream_t);
+template mdnn_status_t xent_outer<F16>(const void*, int64_t, int64_t, const void*, int64_t, int64_t, int64_t, const float*,
+                                       void*, int64_t, mdnn_dtype_t, hipStream_t);
+template mdnn_status_t xent_outer<BF16>(const void*, int64_t, int64_t, const void*, int64_t, int64_t, int64_t, const float*,
+                                        void*, int64_t, mdnn_dtype_t, hipStream_t);
 
 }  // namespace mdnn

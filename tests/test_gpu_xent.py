@@ -168,7 +168,7 @@ def test_gradients(mdnn, size, by_class, dtype):
 @pytest.mark.parametrize("pad,offset", [(0, 0), (8, 8), (3, 1)])
 @pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("by_class", [False, True])
-@pytest.mark.parametrize("m,n,k", [(9, 5003, 1000), (33, 1031, 1100), (64, 4097, 520)])
+@pytest.mark.parametrize("m,n,k", [(9, 5003, 1000), (33, 1031, 1100), (64, 4097, 520), (130, 4097, 520)])
 def test_gradients_of_a_few_dozen_rows(mdnn, m, n, k, by_class, wide, pad, offset, dtype):
     Problem(m, n, k, dtype, by_class, pad=pad, offset=offset).check_backward(mdnn, dw_type="f32" if wide else dtype)
 
