@@ -454,7 +454,7 @@ struct LnBwdArgs {
 // Sums of dgamma and dbeta stay in the registers of their columns' threads over a
 // block's rows, are added over its row groups in their order and written once;
 // sums_kernel adds the blocks' in order.  Bound: memory (4096 x 4096 bf16 with
-// residual and dropout 41 us, 4.1 TB/s, and 5 for the sums; without 38.5 together),
+// residual and dropout 42 us, 4.4 TB/s, and 5 for the sums; without 38.5 together),
 // and two launches where that is little (20 x 900 fp32 9.5).
 template <class T, bool DROP, int TPR, int NCH>
 __global__ void __launch_bounds__(512, NCH <= 2 && !(DROP && !Chunk<T>::H) ? 4 : 2) layernorm_bwd_kernel(LnBwdArgs a) {
