@@ -291,7 +291,7 @@ template <class T>
 __global__ void __launch_bounds__(256)
 conv_small_filter_mfma_kernel(const typename T::storage* __restrict__ x, const typename T::storage* __restrict__ dy,
                               ConvGeom g, int64_t P, float* __restrict__ partial) {
-  __shared__ float red[3][4][64][4];  // waves 1..3: [wave][fragment][lane][4]
+  __shared__ __attribute__((aligned(16))) float red[3][4][64][4];  // waves 1..3: [wave][fragment][lane][4]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int K = g.r * g.s * g.c, N = g.k;
   float4_t acc[2][2];

@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(512, NCH <= 2 && !(DROP && !Chunk<T>::H) ? 4 :
   typedef typename T::storage S;
   constexpr int NT = 512, RPB = NT / TPR, WIDE = TPR * NCH * 8;
   __shared__ RowSums<3, TPR, RPB> buf;
-  __shared__ float part[RPB > 1 ? RPB * WIDE : 1];
+  __shared__ __attribute__((aligned(16))) float part[RPB > 1 ? RPB * WIDE : 1];
   __shared__ float4_t gamma[WIDE / 4];
   const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
   DropKey key = {};

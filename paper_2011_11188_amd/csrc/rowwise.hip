@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(BWD_NT(TPR)) norm_bwd_kernel(BwdArgs a) {
   typedef typename T::storage S;
   constexpr int NT = BWD_NT(TPR), RPB = NT / TPR, WIDE = TPR * NCH * 8;
   __shared__ Sum2 buf[2][RPB][TPR / 64 + 1];
-  __shared__ float part[RPB > 1 ? RPB * WIDE : 1];
+  __shared__ __attribute__((aligned(16))) float part[RPB > 1 ? RPB * WIDE : 1];
   const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
   ChunkPos pos[NCH];
   float dg[NCH][8];

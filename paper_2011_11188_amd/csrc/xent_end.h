@@ -13,7 +13,7 @@ namespace {
 // and lse of its rows (+Inf where G is zero: ignored rows and those past M).
 template <class TL, bool BWD>
 struct XentNumbers {
-  float bias[TL::BN];
+  alignas(16) float bias[TL::BN];  // (read four at a time)
   int32_t label[TL::BM];
   float lse[BWD ? TL::BM : 1];
   __device__ __forceinline__ void load(const XentTile& x, int64_t M, int64_t N, int64_t m0, int64_t n0, int tid) {
