@@ -205,6 +205,20 @@ def _call(name: str, *args) -> int:
     return st
 
 
+def _site(v) -> int:
+    """Dropout's site, which its C argument has to hold (ctypes cuts a number off without a word)."""
+    if not 0 <= v < 1 << 32:
+        raise ValueError("site must lie in [0, 2^32 - 1]")
+    return v
+
+
+def _label(v) -> int:
+    """The ignored label, likewise."""
+    if not -1 << 31 <= v < 1 << 31:
+        raise ValueError("ignored must lie in [-2^31, 2^31 - 1]")
+    return v
+
+
 def dtype_of(t) -> int:
     import torch
     return {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}[t.dtype]
@@ -426,18 +440,18 @@ def mdnn_rmsnorm_bwd(rows, cols, dy, lddy, h, ldh, gamma, eps, dres, lddr, dx, l
 
 
 def mdnn_dropout_fwd(rows, cols, x, ldx, residual, ldr, p, rng, site, y, ldy, dtype, stream=None):
-    return _call("mdnn_dropout_fwd", rows, cols, _p(x), ldx, _p(residual), ldr, p, _p(rng), site, _p(y), ldy, dtype,
-                 _s(stream))
+    return _call("mdnn_dropout_fwd", rows, cols, _p(x), ldx, _p(residual), ldr, p, _p(rng), _site(site), _p(y), ldy,
+                 dtype, _s(stream))
 
 
 def mdnn_dropout_bwd(rows, cols, dy, lddy, p, rng, site, dx, lddx, dtype, stream=None):
-    return _call("mdnn_dropout_bwd", rows, cols, _p(dy), lddy, p, _p(rng), site, _p(dx), lddx, dtype, _s(stream))
+    return _call("mdnn_dropout_bwd", rows, cols, _p(dy), lddy, p, _p(rng), _site(site), _p(dx), lddx, dtype, _s(stream))
 
 
 def mdnn_layernorm_fwd(rows, cols, x, ldx, residual, ldr, p, rng, site, gamma, beta, eps, h_out, ldh, y, ldy, dtype,
                        stream=None):
-    return _call("mdnn_layernorm_fwd", rows, cols, _p(x), ldx, _p(residual), ldr, p, _p(rng), site, _p(gamma), _p(beta),
-                 eps, _p(h_out), ldh, _p(y), ldy, dtype, _s(stream))
+    return _call("mdnn_layernorm_fwd", rows, cols, _p(x), ldx, _p(residual), ldr, p, _p(rng), _site(site), _p(gamma),
+                 _p(beta), eps, _p(h_out), ldh, _p(y), ldy, dtype, _s(stream))
 
 
 def mdnn_layernorm_bwd_workspace(rows, cols) -> int:
@@ -447,7 +461,8 @@ def mdnn_layernorm_bwd_workspace(rows, cols) -> int:
 def mdnn_layernorm_bwd(rows, cols, dy, lddy, h, ldh, gamma, eps, dres, lddr, p, rng, site, dx, lddx, dh, lddh, dgamma,
                        dbeta, dtype, workspace=None, ws_bytes=0, stream=None):
     return _call("mdnn_layernorm_bwd", rows, cols, _p(dy), lddy, _p(h), ldh, _p(gamma), eps, _p(dres), lddr, p, _p(rng),
-                 site, _p(dx), lddx, _p(dh), lddh, _p(dgamma), _p(dbeta), dtype, _p(workspace), ws_bytes, _s(stream))
+                 _site(site), _p(dx), lddx, _p(dh), lddh, _p(dgamma), _p(dbeta), dtype, _p(workspace), ws_bytes,
+                 _s(stream))
 
 
 def mdnn_linear_xent_fwd_workspace(layout, M, N, K, dtype) -> int:
@@ -456,8 +471,8 @@ def mdnn_linear_xent_fwd_workspace(layout, M, N, K, dtype) -> int:
 
 def mdnn_linear_xent_fwd(layout, M, N, K, x, ldx, w, ldw, dtype, bias, labels, ignored, loss, row_loss, lse,
                          workspace=None, ws_bytes=0, stream=None):
-    return _call("mdnn_linear_xent_fwd", layout, M, N, K, _p(x), ldx, _p(w), ldw, dtype, _p(bias), _p(labels), ignored,
-                 _p(loss), _p(row_loss), _p(lse), _p(workspace), ws_bytes, _s(stream))
+    return _call("mdnn_linear_xent_fwd", layout, M, N, K, _p(x), ldx, _p(w), ldw, dtype, _p(bias), _p(labels),
+                 _label(ignored), _p(loss), _p(row_loss), _p(lse), _p(workspace), ws_bytes, _s(stream))
 
 
 def mdnn_linear_xent_bwd_workspace(layout, M, N, K, dtype) -> int:
@@ -466,9 +481,9 @@ def mdnn_linear_xent_bwd_workspace(layout, M, N, K, dtype) -> int:
 
 def mdnn_linear_xent_bwd(layout, M, N, K, x, ldx, w, ldw, dtype, bias, labels, ignored, lse, loss_scale, dx, lddx, dw,
                          lddw, dw_type, db, workspace=None, ws_bytes=0, stream=None):
-    return _call("mdnn_linear_xent_bwd", layout, M, N, K, _p(x), ldx, _p(w), ldw, dtype, _p(bias), _p(labels), ignored,
-                 _p(lse), _p(loss_scale), _p(dx), lddx, _p(dw), lddw, dw_type, _p(db), _p(workspace), ws_bytes,
-                 _s(stream))
+    return _call("mdnn_linear_xent_bwd", layout, M, N, K, _p(x), ldx, _p(w), ldw, dtype, _p(bias), _p(labels),
+                 _label(ignored), _p(lse), _p(loss_scale), _p(dx), lddx, _p(dw), lddw, dw_type, _p(db), _p(workspace),
+                 ws_bytes, _s(stream))
 
 
 def mdnn_net_create(layers, batch: int, cfg: TrainCfg) -> int:
