@@ -25,6 +25,9 @@ __device__ __forceinline__ float fetch_sel(const Src& src, int64_t mn, int64_t k
   return o >= 0 ? v : 0.0f;
 }
 
+// Columns whose 64-wide tiles a grid's second dimension counts.
+constexpr int64_t F32_GRID_COLS = (int64_t)65535 * 64;
+
 template <class SrcA, class SrcB, int KG>
 __global__ void __launch_bounds__(256 * KG)
 gemm_f32_kernel(SrcA a, SrcB b, int64_t M, int64_t N, int64_t K, Epilogue ep) {
@@ -35,7 +38,12 @@ gemm_f32_kernel(SrcA a, SrcB b, int64_t M, int64_t N, int64_t K, Epilogue ep) {
   float(*As)[68] = (float(*)[68])(smem + grp * STAGE);
   float(*Bs)[68] = (float(*)[68])(smem + grp * STAGE + 16 * 68);
   const int tx = tid & 15, ty = tid >> 4;
-  const int64_t m0 = (int64_t)blockIdx.x * 64, n0 = (int64_t)blockIdx.y * 64;
+  uint32_t tm = blockIdx.x, tn = blockIdx.y;
+  if (N > F32_GRID_COLS) {  // (the columns' tiles lie along x too)
+    const uint32_t tiles_m = (uint32_t)ceil_div(M, 64);
+    tn = tm / tiles_m, tm -= tn * tiles_m;
+  }
+  const int64_t m0 = (int64_t)tm * 64, n0 = (int64_t)tn * 64;
   int64_t kbeg = 0, kend = K;
   if (ep.partial) {
     kbeg = (int64_t)blockIdx.z * ep.k_per_split;
@@ -297,9 +305,11 @@ inline mdnn_status_t run_pipe(const typename LA::Args& a, const typename LB::Arg
 template <class SrcA, class SrcB>
 inline mdnn_status_t run_gemm32(const SrcA& a, const SrcB& b, int64_t M, int64_t N, int64_t K,
                                 const Epilogue& ep, int splits, hipStream_t stream) {
-  if (ceil_div(M, 64) > 0x7fffffffLL || ceil_div(N, 64) > 65535 || splits > 65535)
+  const bool wide = N > F32_GRID_COLS;  // (columns by x: gradients of 16 rows of millions of classes)
+  const int64_t gx = ceil_div(M, 64) * (wide ? ceil_div(N, 64) : 1);
+  if (ceil_div(M, 64) > 0x7fffffffLL || gx > (wide ? 0x3fffffLL : 0x7fffffffLL) || splits > 65535)
     return fail(MDNN_ERR_SHAPE, "gemm: problem too large for the fp32 launch grid");
-  dim3 grid((unsigned)ceil_div(M, 64), (unsigned)ceil_div(N, 64), (unsigned)splits);
+  dim3 grid((unsigned)gx, wide ? 1u : (unsigned)ceil_div(N, 64), (unsigned)splits);
   // few workgroups over a long K: four K groups per tile
   const int64_t blocks = (int64_t)grid.x * grid.y * grid.z;
   const int64_t k_each = splits > 1 ? ep.k_per_split : K;
