@@ -30,11 +30,12 @@ struct XentTile {
   float* zlab;
   uint32_t* done;  // cleared
   // backward: G times `scale` in the operands' type, rows of ldg elements (a multiple of 64), zeros in rows M .. rows - 1
-  // and columns past the piece; part: column sums of tile row t at part[t * ldp + column of the piece], or null
+  // and columns past the product's up to `width` (memory of a row from g on); part: column sums of tile row t at
+  // part[t * ldp + column], or null
   const float* lse;
   float scale;
   void* g;
-  int64_t ldg, rows, ldp;
+  int64_t ldg, width, rows, ldp;
   float* part;
   // where one tile row holds all rows: db itself in place of part (or null), and a = S / counted rows over `scale` to alpha
   bool alone;
@@ -55,6 +56,15 @@ struct XentProduct {
 int xent_tile(int64_t M, int64_t N, int64_t K, bool backward);
 template <class T>
 mdnn_status_t xent_tiles(const XentProduct& p, const XentTile& x, hipStream_t st);
+
+// How a call runs (host code, for the calls and their tests): 0 tiles read W as it is, 1 copied, 2 the register-staged
+// tiles do, 3 logits through the workspace; the classes of one tile product.
+struct XentWay {
+  int32_t way;
+  int64_t classes;
+};
+XentWay xent_way(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, int64_t ldx, const void* w, int64_t ldw,
+                 mdnn_dtype_t t, bool backward);
 
 // The same by the register-staged kernel: any type, element address and
 // leading dimension that xent_reg_ok takes (ext is not used); tiles of 128 or 64.

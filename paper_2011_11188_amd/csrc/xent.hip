@@ -45,6 +45,8 @@ int xent_tile(int64_t M, int64_t N, int64_t K, bool backward) {
 
 namespace {
 
+constexpr int64_t MAX_ROWS = (int64_t)1 << 24, MAX_N = 0x7fffffff;
+
 // ---------------------------------------------------------------- forward
 
 // A row's piece of logits in the workspace: rows of ldz, or the parts of a split
@@ -472,6 +474,19 @@ Way way_by_size(int64_t M, int64_t N, int64_t K, mdnn_dtype_t t, bool backward) 
 }
 Way way_below(Way w) { return w == TILED ? STAGED : GENERAL; }
 
+// Classes of a table [N][K] that one tile product takes: as many, in whole
+// multiples of 256, as 32-bit offsets reach in rows up to a sixteenth (64 elements)
+// wider than K; wider ones go through stored logits, as all such tables did (64 x
+// 250880 x 14336 bf16 forward 1739 us, in four products 1412; 512 rows 3423 and 3471;
+// 2 x 4300000 x 256 fp32 4300 and 1891).  Class-contiguous rows are addressed step by
+// step, all their classes at once.
+int64_t reach_classes(mdnn_layout_t layout, int64_t K, mdnn_dtype_t t) {
+  if (layout == MDNN_NN) return MAX_N;
+  const int64_t wide = K + (K > 1024 ? K / 16 : 64), most = (int64_t)1 << (t == MDNN_F32 ? 30 : 31);
+  const int64_t n = most / wide / 256 * 256 - 256;
+  return n < 256 ? 256 : n;
+}
+
 // The tile that a way's products take.
 int way_tile(Way w, int64_t M, int64_t N, int64_t K, bool backward) {
   return w == STAGED ? xent_reg_tile(M, N) : xent_tile(M, N, up(K, 64), backward);
@@ -535,10 +550,8 @@ FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
     p.nc = piece_classes(N, M, (int64_t)16 << 20);
   } else {
     p.nc = piece_classes(N, ceil_div(M, 64), (int64_t)32 << 20);  // pairs of 64 columns at least
-    if (way == PACKED) {
-      const int64_t most = piece_classes(N, p.kc, (int64_t)128 << 20);
-      p.nc = p.nc < most ? p.nc : most;
-    }
+    const int64_t most = way == PACKED ? piece_classes(N, p.kc, (int64_t)128 << 20) : reach_classes(layout, K, t);
+    p.nc = p.nc < most ? p.nc : most;
   }
   p.pieces = ceil_div(N, p.nc);
   const int64_t last = N - (p.pieces - 1) * p.nc;
@@ -588,6 +601,7 @@ SplitPlan dx_splits(int64_t M, int64_t K, int64_t depth, mdnn_dtype_t t) {
 
 struct BwdPlan {
   int64_t nc, pieces, rows, kc, ldg, blocks, ldw;
+  int64_t span;  // classes of a tile product: the piece's, or as many as its loaders reach
   size_t alpha, copy, z, g, part, acc, pack, few, parts, gemm, gemm_bytes, bytes;
   bool is_few;
 };
@@ -604,6 +618,11 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
     const int64_t most = piece_classes(N, p.kc, (int64_t)128 << 20);
     p.nc = p.nc < most ? p.nc : most;
   }
+  p.span = p.nc;
+  if (way == TILED || way == STAGED) {
+    const int64_t most = reach_classes(layout, K, t);
+    p.span = p.nc < most ? p.nc : most;
+  }
   p.pieces = ceil_div(N, p.nc);
   p.ldg = up(p.nc, h ? 64 : 4);
   const int64_t last = N - (p.pieces - 1) * p.nc;
@@ -611,10 +630,11 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   p.blocks = ceil_div(p.rows, GRAD_ROWS);
   if (way != GENERAL) {
     p.blocks = 1;
-    for (int64_t n : {p.nc, last}) {
-      const int64_t b = ceil_div(M, way_tile(way, M, n, K, true));
-      p.blocks = b > p.blocks ? b : p.blocks;
-    }
+    for (int64_t n : {p.nc, last})
+      for (int64_t s : {n < p.span ? n : p.span, n - (n - 1) / p.span * p.span}) {  // (the widths of its tile products)
+        const int64_t b = ceil_div(M, way_tile(way, M, s, K, true));
+        p.blocks = b > p.blocks ? b : p.blocks;
+      }
   }
   p.alpha = s.take(4);
   p.copy = s.take((size_t)p.rows * p.kc * es);
@@ -641,20 +661,18 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
 }
 
 // Whether W's rows are as the tiles read them: on 16 bytes, 32-bit offsets over
-// a piece's rows; or as the register-staged tiles do.
-bool w_fits(Way way, mdnn_layout_t layout, int64_t M, int64_t K, const void* x, int64_t ldx, const void* w, int64_t ldw,
-            int64_t N, int64_t nc, mdnn_dtype_t t) {
+// a tile product's rows; or as the register-staged tiles do.
+bool w_fits(Way way, mdnn_layout_t layout, int64_t M, int64_t K, int64_t ldx, const void* w, int64_t ldw, int64_t N,
+            int64_t nc, mdnn_dtype_t t) {
   if (way == TILED)
     return aligned(w, 16) && ldw % 8 == 0 && (layout == MDNN_NN ? 64 * ldw + nc : (nc + 255) * ldw) < (int64_t)1 << 31;
   if (way == STAGED) {
     const int64_t last = N - (N - 1) / nc * nc;
-    return xent_reg_ok(t, XentProduct{x, w, ldx, ldw, M, nc, K, nc, layout == MDNN_NT, false}) &&
-           xent_reg_ok(t, XentProduct{x, w, ldx, ldw, M, last, K, last, layout == MDNN_NT, false});
+    return xent_reg_ok(t, XentProduct{nullptr, w, ldx, ldw, M, nc, K, nc, layout == MDNN_NT, false}) &&
+           xent_reg_ok(t, XentProduct{nullptr, w, ldx, ldw, M, last, K, last, layout == MDNN_NT, false});
   }
   return true;
 }
-
-constexpr int64_t MAX_ROWS = (int64_t)1 << 24, MAX_N = 0x7fffffff;
 
 bool sizes_ok(int64_t M, int64_t N, int64_t K) {
   return M >= 0 && M <= MAX_ROWS && N >= 1 && N <= MAX_N && K >= 1 && K <= MAX_N;
@@ -800,8 +818,8 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
   float* acc = joined ? (float*)(ws + p.acc) : nullptr;
   // Few rows are read where they are: their kernels leave out the ignored ones.
   const bool few = p.is_few && (dx || dw);
-  const bool here = few && (way == GENERAL || (way == STAGED && xent_reg_ok(t, XentProduct{x, w, ldx, ldw, M, p.nc, K, p.nc,
-                                                                                           layout == MDNN_NT, true})) ||
+  const XentProduct in_place = {x, w, ldx, ldw, M, p.span, K, p.span, layout == MDNN_NT, true};
+  const bool here = few && (way == GENERAL || (way == STAGED && xent_reg_ok(t, in_place)) ||
                             (way == TILED && aligned(x, 16) && ldx % 8 == 0 && (M + 255) * ldx < (int64_t)1 << 31));
   if (here) {
     copy = (S*)x;
@@ -818,7 +836,12 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
     const int64_t nc = n0 + p.nc < N ? p.nc : N - n0;
     const float* b = bias ? bias + n0 : nullptr;
     Piece q = {w_piece(layout, w, ldw, n0, sizeof(S)), ldw, nc};
-    int64_t blocks = p.blocks;
+    // db of `n` classes from class s of the piece on, from the column sums that `blocks` row blocks left
+    auto sums = [&](int64_t s, int64_t n, int64_t blocks) {
+      hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(n, 64)), dim3(256), 0, st, part + s, blocks, p.nc, n,
+                         alpha, scale, db + n0 + s);
+      return check_launch("xent_db_kernel");
+    };
     if (way == GENERAL) {
       Logits l;
       MDNN_TRY(general_logits(layout, M, nc, K, copy, ldc, q.w, ldw, t, b, z, p.ldg, gw, p.gemm_bytes, l, st));
@@ -827,22 +850,24 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
                          p.rows, nc, n0, labels, ignored, N, lse, scale, g, p.ldg, part, p.nc, loss_scale,
                          here ? alpha : nullptr);
       MDNN_TRY(check_launch("xent_grad_kernel"));
+      if (db) MDNN_TRY(sums(0, nc, p.blocks));
     } else {
       Pack next;
       q = take_piece(way, layout, w, ldw, dtype_size(t), n0, nc, K, p.kc, ws + p.pack, p.ldw, next);
       if (n0 > 0) MDNN_TRY(pack(next, {}, st));  // (the first is copied beside x)
-      XentProduct a = {copy, q.w, ldc, q.ldw, M, nc, way == STAGED ? K : p.kc, q.ext, layout == MDNN_NT, true};
-      XentTile e = {};
-      e.bias = b, e.labels = labels, e.ignored = ignored, e.n0 = n0, e.classes = N, e.lse = lse, e.scale = scale;
-      blocks = ceil_div(M, way_tile(way, M, nc, K, true));
-      e.alone = blocks == 1, e.loss_scale = loss_scale, e.alpha = alpha, e.db = e.alone ? db : nullptr;
-      e.g = g, e.ldg = p.ldg, e.rows = p.rows, e.ldp = p.nc, e.part = e.alone ? nullptr : part;
-      MDNN_TRY(tiles<T>(way, a, e, st));
-    }
-    if (db && (way == GENERAL || blocks > 1)) {
-      hipLaunchKernelGGL(xent_db_kernel, dim3((unsigned)ceil_div(nc, 64)), dim3(256), 0, st, part, blocks, p.nc, nc, alpha,
-                         scale, db + n0);
-      MDNN_TRY(check_launch("xent_db_kernel"));
+      for (int64_t s = 0; s < nc; s += p.span) {
+        const int64_t n = s + p.span < nc ? p.span : nc - s;
+        XentProduct a = {copy, w_piece(layout, q.w, q.ldw, s, sizeof(S)), ldc, q.ldw, M, n, way == STAGED ? K : p.kc,
+                         q.ext - s, layout == MDNN_NT, true};
+        XentTile e = {};
+        e.bias = b ? b + s : nullptr, e.labels = labels, e.ignored = ignored, e.n0 = n0 + s, e.classes = N, e.lse = lse;
+        const int64_t blocks = ceil_div(M, way_tile(way, M, n, K, true));
+        e.alone = blocks == 1, e.loss_scale = loss_scale, e.alpha = alpha, e.db = e.alone ? db : nullptr;
+        e.scale = scale, e.g = g + s, e.ldg = p.ldg, e.width = p.ldg - s, e.rows = p.rows, e.ldp = p.nc;
+        e.part = e.alone || !part ? nullptr : part + s;
+        MDNN_TRY(tiles<T>(way, a, e, st));
+        if (db && blocks > 1) MDNN_TRY(sums(s, n, blocks));
+      }
     }
     if (few) {
       XentFew a = {};
@@ -901,6 +926,21 @@ mdnn_status_t run_bwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
 }
 
 }  // namespace
+
+XentWay xent_way(mdnn_layout_t layout, int64_t M, int64_t N, int64_t K, int64_t ldx, const void* w, int64_t ldw,
+                 mdnn_dtype_t t, bool backward) {
+  for (Way way = way_by_size(M, N, K, t, backward);; way = way_below(way)) {
+    int64_t nc, ld = ldx;
+    if (backward) {
+      const BwdPlan p = bwd_plan(way, layout, M, N, K, t);
+      nc = p.span, ld = p.kc;  // (x's copy)
+    } else {
+      nc = fwd_plan(way, layout, M, N, K, t).nc;
+    }
+    if (w_fits(way, layout, M, K, ld, w, ldw, N, nc, t)) return {(int32_t)way, nc};
+  }
+}
+
 }  // namespace mdnn
 
 using namespace mdnn;
@@ -945,8 +985,7 @@ extern "C" mdnn_status_t mdnn_linear_xent_fwd(mdnn_layout_t layout, int64_t M, i
   const size_t need = fwd_bytes(layout, M, N, K, dtype);
   if (!workspace || ws_bytes < need || !aligned(workspace, 256))
     return fail(MDNN_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) required", who, need);
-  Way way = way_by_size(M, N, K, dtype, false);
-  while (!w_fits(way, layout, M, K, x, ldx, w, ldw, N, fwd_plan(way, layout, M, N, K, dtype).nc, dtype)) way = way_below(way);
+  const Way way = (Way)xent_way(layout, M, N, K, ldx, w, ldw, dtype, false).way;
   char* ws = (char*)workspace;
   switch (dtype) {
     case MDNN_F32:
@@ -996,11 +1035,7 @@ extern "C" mdnn_status_t mdnn_linear_xent_bwd(mdnn_layout_t layout, int64_t M, i
   if (!workspace || ws_bytes < need || !aligned(workspace, 256))
     return fail(MDNN_ERR_WORKSPACE, "%s: workspace of %zu bytes (256-byte aligned) required", who, need);
   clear_error();
-  Way way = way_by_size(M, N, K, dtype, true);
-  for (;; way = way_below(way)) {
-    const BwdPlan p = bwd_plan(way, layout, M, N, K, dtype);
-    if (w_fits(way, layout, M, K, workspace, p.kc, w, ldw, N, p.nc, dtype)) break;
-  }
+  const Way way = (Way)xent_way(layout, M, N, K, ldx, w, ldw, dtype, true).way;
   char* ws = (char*)workspace;
   switch (dtype) {
     case MDNN_F32:

@@ -127,7 +127,7 @@ __device__ __forceinline__ void xent_end(const XentTile& x, const XentNumbers<TL
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[j][e] += v[e];
-        if (m0 + row < x.rows && n < x.ldg) {
+        if (m0 + row < x.rows && n < x.width) {
           S* d = (S*)x.g + (m0 + row) * x.ldg + n;
           if constexpr (sizeof(S) == 2) {
             // (a vector conversion is one instruction for two elements)

@@ -1,0 +1,78 @@
+"""The last layer's cross entropy over tables of classes past what one product's
+32-bit offsets reach, both ways, against 64 bits on the GPU; bounds as in
+test_gpu_xent.py's note."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+HALF = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}
+IGNORED = -7
+
+
+def _check(mdnn, m, n, k, dtype, pad=0, step=1 << 14):
+    import torch
+    t = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+    g = torch.Generator(device="cuda").manual_seed(m + n)
+    x = torch.randn(m, k, generator=g, device="cuda").to(t)
+    w = torch.randn(n, k + pad, generator=g, device="cuda", dtype=t)[:, :k]
+    w *= 2 / k ** 0.5
+    bias = torch.randn(n, generator=g, device="cuda")
+    labels = torch.randint(0, n, (m,), generator=g, device="cuda", dtype=torch.int32)
+    labels[0] = n - 1
+    if m > 3:
+        labels[1], labels[2], labels[3] = 0, IGNORED, n // 2
+    kw = dict(layout=mdnn.NT, ignored=IGNORED)
+    loss, row, lse = mdnn.linear_xent(x, w, labels, bias, **kw)
+    dx, dw, db = mdnn.linear_xent_bwd(x, w, labels, lse, bias, dw_dtype=t, **kw)
+    xd, counted = x.double(), labels != IGNORED
+    a, l, at = 1.0 / int(counted.sum()), lse.double()[:, None], labels.long()
+
+    def pieces():
+        for lo in range(0, n, step):
+            wd = w[lo:lo + step].double()
+            z = xd @ wd.t() + bias[lo:lo + step].double()
+            yield lo, wd, z, (k + 2) * U * (xd.abs() @ wd.abs().t()) + 2 * U * bias[lo:lo + step].double().abs()
+
+    parts = []
+    zl, el, off, most = (torch.zeros(m, dtype=torch.float64, device="cuda") for _ in range(4))
+    for lo, wd, z, e in pieces():
+        parts.append(torch.logsumexp(z, 1))
+        off += ((z - l).exp() * (e + 2 * U * (z - l).abs())).sum(1)
+        most = torch.maximum(most, e.amax(1))
+        here = (at >= lo) & (at < lo + z.shape[1])
+        r = here.nonzero()[:, 0]
+        zl[r], el[r] = z[r, at[r] - lo], e[r, at[r] - lo]
+    want = torch.logsumexp(torch.stack(parts), 0)
+    e_lse = off * 1.01 + (n / 256 + 64) * (4 * U + 2.0 ** -21) + most * 1e-3 + 2 * U * want.abs() + 2.0 ** -21
+    assert bool(((lse.double() - want).abs() <= e_lse).all())
+    r = torch.where(counted, want - zl, 0.0)
+    assert bool(((row.double() - r).abs() <= e_lse + el + 2 * U * r.abs()).all())
+    assert abs(float(loss) - float(row.double().sum()) * a) <= 2 * U * abs(float(loss))
+    xm = torch.where(counted[:, None], xd, 0.0)
+    dx_want, dx_tol = 0.0, 0.0
+    for lo, wd, z, e in pieces():
+        p = torch.where(counted[:, None], (z - l).exp(), 0.0)
+        exact = p * (e + 2.0 ** -21 + 2 * U * (z - l).abs())
+        q = (counted & (at >= lo) & (at < lo + z.shape[1])).nonzero()[:, 0]
+        p[q, at[q] - lo] -= 1.0
+        exact += U * p.abs()
+        stored = exact + HALF[dtype] * (p.abs() + exact) + (2.0 ** -40 if dtype == "f16" else 2.0 ** -134)
+        stored = torch.where(counted[:, None], stored, 0.0)
+        dx_want = dx_want + a * (p @ wd)
+        dx_tol = dx_tol + a * ((stored + (n + 68) * U * p.abs()) @ wd.abs())
+        w_want = a * (p.t() @ xm)
+        tol = a * ((stored + (m + 64) * U * p.abs()).t() @ xm.abs()) + (6 * U + 1.01 * HALF[dtype]) * w_want.abs() + TINY[dtype]
+        assert bool(((dw[lo:lo + step].double() - w_want).abs() <= tol).all()), lo
+        b_want = a * p.sum(0)
+        tol = a * (exact + (m + 8) * U * p.abs()).sum(0) + 4 * U * b_want.abs() + TINY["f32"]
+        assert bool(((db[lo:lo + step].double() - b_want).abs() <= tol).all()), lo
+    assert bool(((dx.double() - dx_want).abs() <= dx_tol + (4 * U + 1.01 * HALF[dtype]) * dx_want.abs() + TINY[dtype]).all())
+
+
+@pytest.mark.parametrize("m,n,k,dtype,pad", [(3, 250880, 8704, "bf16", 0), (70, 250880, 8704, "bf16", 0),
+                                             (200, 250881, 8704, "f16", 8), (5, 250880, 8707, "f16", 0),
+                                             (2, 4300000, 256, "f32", 0), (20, 4300001, 257, "f32", 0)])
+def test_tables_of_2_31_elements(mdnn, m, n, k, dtype, pad):
+    assert n * k >= 2 ** (30 if dtype == "f32" else 31)
+    _check(mdnn, m, n, k, dtype, pad, 1 << (19 if k < 1000 else 14))
