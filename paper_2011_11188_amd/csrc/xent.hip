@@ -487,6 +487,15 @@ int64_t reach_classes(mdnn_layout_t layout, int64_t K, mdnn_dtype_t t) {
   return n < 256 ? 256 : n;
 }
 
+// Pieces of nc classes, or a few fewer so that the last, too, holds a 16-byte chunk,
+// as the register-staged tiles need of class-contiguous rows: a last piece of one to
+// three classes sent all pieces through stored logits (gradients, fp32: 16384 x 8193
+// x 512 3.90 ms, two pieces of at least nine 3.39; 2^20 x 2305 x 64 19.6 and 15.0).
+int64_t whole_chunks(int64_t N, int64_t nc, mdnn_dtype_t t) {
+  while (N % nc > 0 && N % nc < 16 / (int64_t)dtype_size(t)) nc -= 8;
+  return nc;
+}
+
 // The tile that a way's products take.
 int way_tile(Way w, int64_t M, int64_t N, int64_t K, bool backward) {
   return w == STAGED ? xent_reg_tile(M, N) : xent_tile(M, N, up(K, 64), backward);
@@ -552,6 +561,7 @@ FwdPlan fwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
     p.nc = piece_classes(N, ceil_div(M, 64), (int64_t)32 << 20);  // pairs of 64 columns at least
     const int64_t most = way == PACKED ? piece_classes(N, p.kc, (int64_t)128 << 20) : reach_classes(layout, K, t);
     p.nc = p.nc < most ? p.nc : most;
+    if (way == STAGED && layout == MDNN_NN) p.nc = whole_chunks(N, p.nc, t);
   }
   p.pieces = ceil_div(N, p.nc);
   const int64_t last = N - (p.pieces - 1) * p.nc;
@@ -618,6 +628,7 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
     const int64_t most = piece_classes(N, p.kc, (int64_t)128 << 20);
     p.nc = p.nc < most ? p.nc : most;
   }
+  if (way == STAGED && layout == MDNN_NN) p.nc = whole_chunks(N, p.nc, t);
   p.span = p.nc;
   if (way == TILED || way == STAGED) {
     const int64_t most = reach_classes(layout, K, t);

@@ -76,3 +76,54 @@ def _check(mdnn, m, n, k, dtype, pad=0, step=1 << 14):
 def test_tables_of_2_31_elements(mdnn, m, n, k, dtype, pad):
     assert n * k >= 2 ** (30 if dtype == "f32" else 31)
     _check(mdnn, m, n, k, dtype, pad, 1 << (19 if k < 1000 else 14))
+
+
+@pytest.mark.parametrize("m,n,k,dtype", [(16384, 8193, 40, "f32"), (16384, 16387, 24, "f32"), (1 << 19, 515, 64, "f32"),
+                                         (200, (1 << 19) + 3, 65, "f16"), (1 << 20, 2051, 33, "f32")])
+def test_short_last_pieces(mdnn, m, n, k, dtype):
+    """Class-contiguous W whose classes leave less than a 16-byte chunk past whole pieces."""
+    import torch
+    t = {"f32": torch.float32, "f16": torch.float16}[dtype]
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn(m, k, generator=g, device="cuda").to(t)
+    w = (torch.randn(k, n, generator=g, device="cuda") * 2 / k ** 0.5).to(t)
+    bias = torch.randn(n, generator=g, device="cuda")
+    labels = torch.randint(0, n, (m,), generator=g, device="cuda", dtype=torch.int32)
+    labels[::7], labels[1], labels[2] = IGNORED, n - 1, n // 256 * 256
+    loss, row, lse = mdnn.linear_xent(x, w, labels, bias, ignored=IGNORED)
+    dx, dw, db = mdnn.linear_xent_bwd(x, w, labels, lse, bias, ignored=IGNORED)
+    counted = labels != IGNORED
+    a, wd = 1.0 / int(counted.sum()), w.double()
+    dw_want, dw_tol = torch.zeros_like(wd), torch.zeros_like(wd)
+    db_want, db_tol = (torch.zeros(n, dtype=torch.float64, device="cuda") for _ in range(2))
+    wt = wd.t().contiguous()
+    step = max(40, (1 << 25) // n)
+    for lo in range(0, m, step):
+        rows = slice(lo, min(m, lo + step))
+        xd, c = x[rows].double(), counted[rows, None]
+        z, e_z = xd @ wd + bias.double(), (k + 2) * U * (xd.abs() @ wd.abs()) + 2 * U * bias.double().abs()
+        want = torch.logsumexp(z, 1)
+        p = (z - want[:, None]).exp()
+        e = ((p * (e_z + 2 * U * (z - z.amax(1, keepdim=True)).abs())).sum(1) + (n / 256 + 64) * (4 * U + 2.0 ** -21)
+             + e_z.amax(1) * 1e-3 + 2 * U * want.abs() + 2.0 ** -21)
+        assert bool(((lse[rows].double() - want).abs() <= e).all())
+        at = labels[rows].clamp(min=0).long()[:, None]
+        r = torch.where(c[:, 0], want - z.gather(1, at)[:, 0], 0.0)
+        assert bool(((row[rows].double() - r).abs() <= e + e_z.gather(1, at)[:, 0] + 2 * U * r.abs()).all())
+        l = lse[rows].double()[:, None]
+        p = torch.where(c, (z - l).exp(), 0.0)
+        exact = p * (e_z + 2.0 ** -21 + 2 * U * (z - l).abs())
+        p.scatter_add_(1, at, -c.double())
+        exact += U * p.abs()
+        stored = torch.where(c, exact + HALF[dtype] * (p.abs() + exact) + (2.0 ** -40 if dtype == "f16" else 2.0 ** -134), 0.0)
+        dx_want = a * (p @ wt)
+        tol = a * ((stored + (n + 68) * U * p.abs()) @ wt.abs()) + (4 * U + 1.01 * HALF[dtype]) * dx_want.abs() + TINY[dtype]
+        assert bool(((dx[rows].double() - dx_want).abs() <= tol).all())
+        xm = torch.where(c, xd, 0.0).t().contiguous()
+        dw_want += a * (xm @ p)
+        dw_tol += a * (xm.abs() @ (stored + (m + 64) * U * p.abs()))
+        db_want += a * p.sum(0)
+        db_tol += a * (torch.where(c, exact, 0.0) + (m + 8) * U * p.abs()).sum(0)
+    assert bool(((dw.double() - dw_want).abs() <= dw_tol + 6 * U * dw_want.abs()).all())
+    assert bool(((db.double() - db_want).abs() <= db_tol + 4 * U * db_want.abs()).all())
+    assert abs(float(loss) - float(row.double().sum()) * a) <= 2 * U * abs(float(loss))

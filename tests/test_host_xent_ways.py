@@ -53,3 +53,21 @@ def test_smaller_tables_are_whole(way, backward):
             assert way(NT, M, N, K, BF16, backward) == (TILED, N)
             assert way(NN, M, N, K, BF16, backward) == (TILED, N)
     assert way(NT, 8, 250880, 4000, F32, backward) == (STAGED, 250880)
+
+
+def _tile_row_pieces(N, classes):
+    return [min(classes, N - lo) for lo in range(0, N, classes)]
+
+
+@pytest.mark.parametrize("M,N,K,t,backward", [
+    (16384, N, 64, F32, True) for N in (8191, 8192, 8193, 8194, 8195, 8196, 16383, 16385, 16387, 16388)] + [
+    (1 << 20, N, 64, F32, True) for N in (256, 257, 259, 2304, 2305, 2307, 2308, 4609)] + [
+    (200, (1 << 19) + d, 65, F16, True) for d in (-1, 0, 1, 7, 8)] + [
+    (1 << 20, (1 << 11) + d, 33, F32, False) for d in (-1, 0, 1, 3, 4)] + [
+    (1 << 24, N, 40, F32, False) for N in (257, 513, 1027, 2050)])
+def test_a_short_last_piece_does_not_change_the_way(way, M, N, K, t, backward):
+    """Class-contiguous W whose classes leave one to seven (fp32: three) past whole pieces: every piece holds a 16-byte chunk,
+    so that the register-staged tiles take all of them."""
+    got, classes = way(NN, M, N, K, t, backward)
+    assert got == STAGED
+    assert min(_tile_row_pieces(N, classes)) >= (4 if t == F32 else 8)
