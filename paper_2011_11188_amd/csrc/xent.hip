@@ -801,12 +801,18 @@ mdnn_status_t run_fwd(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64
   return MDNN_SUCCESS;
 }
 
-// Whether a gradient's product of 16-bit operands may split its depth.  From 128
-// tiles of 64 x 64 on, one launch of them is no slower up to this depth than parts
-// and their sum (704 x 1140 x 827 bf16 47.9 -> 31.4 us, 1000 x 5003 x 1000 fp16 76.6 ->
-// 71.7; limits of 2048 and 6000 differ only above).
+// Whether a gradient's product of 16-bit operands may split its depth, where its
+// 128 x 128 tiles are below 128 (else none is split).  From 128 tiles of 64 x 64 on,
+// whole depths run on those.  Up to 256 they are one round of workgroups, and parts and
+// their sum win the sooner the fewer they are (bf16, whole and split: 512 x 1024 over
+// 3968 15.4 and 16.3 us, over 6976 23.0 and 21.3; 512 x 1536 over 7040 23.6 and 24.6,
+// over 9984 31.2 and 29.5; 1000 x 1000 NN over 9984 40.2 and 38.1, but NT 32.2 and 36.6);
+// above they are two, and parts win from about 3000 on (448 x 2368 over 2560 26.2 and
+// 19.5; 1408 x 1408 over 2560 22.3 and 23.6, over 4032 31.6 and 29.0; 640 x 3200 over
+// 2944 29.8 and 29.4, over 6016 55 and 46).
 bool product_splits(int64_t M, int64_t N, int64_t K) {
-  return ceil_div(M, 64) * ceil_div(N, 64) < 128 || K > 6000;
+  const int64_t tiles = ceil_div(M, 64) * ceil_div(N, 64);
+  return tiles < 128 || K > (tiles > 256 ? 3000 : 40 * tiles);
 }
 
 template <class T>

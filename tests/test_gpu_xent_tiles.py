@@ -29,6 +29,14 @@ def test_fp32_gradients_of_hundreds_of_rows(mdnn, m, n, k, by_class, pad, offset
     X.Problem(m, n, k, dtype, by_class, pad=pad, offset=offset).check_backward(mdnn, dw_type="f32")
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("by_class", [False, True])
+@pytest.mark.parametrize("m,n,k", [(1100, 2900, 1000), (1100, 3100, 1000), (520, 5600, 1024), (520, 5900, 1024)])
+def test_split_depths(mdnn, m, n, k, by_class, dtype):
+    """dx whole and in parts of its depth (the classes), on both sides of the rule's lines."""
+    X.Problem(m, n, k, dtype, by_class).check_backward(mdnn, dw_type=dtype)
+
+
 @pytest.mark.parametrize("m,n,k,dtype", [(1025, 300, 40, "f32"), (4100, 1001, 64, "f16"), (70001, 515, 24, "bf16"),
                                          (1 << 20, 300, 32, "bf16")])
 def test_the_mean_over_many_blocks(mdnn, m, n, k, dtype):
