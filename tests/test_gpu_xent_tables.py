@@ -10,19 +10,21 @@ TINY = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}
 IGNORED = -7
 
 
-def _check(mdnn, m, n, k, dtype, pad=0, step=1 << 14):
+def _check(mdnn, m, n, k, dtype, pad=0, step=1 << 14, by_class=True):
     import torch
     t = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
     g = torch.Generator(device="cuda").manual_seed(m + n)
     x = torch.randn(m, k, generator=g, device="cuda").to(t)
-    w = torch.randn(n, k + pad, generator=g, device="cuda", dtype=t)[:, :k]
+    rows, cols = (n, k) if by_class else (k, n)
+    w = torch.randn(rows, cols + pad, generator=g, device="cuda", dtype=t)[:, :cols]
     w *= 2 / k ** 0.5
+    table = lambda v, lo: (v[lo:lo + step] if by_class else v[:, lo:lo + step].t()).double()  # noqa: E731
     bias = torch.randn(n, generator=g, device="cuda")
     labels = torch.randint(0, n, (m,), generator=g, device="cuda", dtype=torch.int32)
     labels[0] = n - 1
     if m > 3:
         labels[1], labels[2], labels[3] = 0, IGNORED, n // 2
-    kw = dict(layout=mdnn.NT, ignored=IGNORED)
+    kw = dict(layout=mdnn.NT if by_class else mdnn.NN, ignored=IGNORED)
     loss, row, lse = mdnn.linear_xent(x, w, labels, bias, **kw)
     dx, dw, db = mdnn.linear_xent_bwd(x, w, labels, lse, bias, dw_dtype=t, **kw)
     xd, counted = x.double(), labels != IGNORED
@@ -30,7 +32,7 @@ def _check(mdnn, m, n, k, dtype, pad=0, step=1 << 14):
 
     def pieces():
         for lo in range(0, n, step):
-            wd = w[lo:lo + step].double()
+            wd = table(w, lo).contiguous()
             z = xd @ wd.t() + bias[lo:lo + step].double()
             yield lo, wd, z, (k + 2) * U * (xd.abs() @ wd.abs().t()) + 2 * U * bias[lo:lo + step].double().abs()
 
@@ -63,7 +65,7 @@ def _check(mdnn, m, n, k, dtype, pad=0, step=1 << 14):
         dx_tol = dx_tol + a * ((stored + (n + 68) * U * p.abs()) @ wd.abs())
         w_want = a * (p.t() @ xm)
         tol = a * ((stored + (m + 64) * U * p.abs()).t() @ xm.abs()) + (6 * U + 1.01 * HALF[dtype]) * w_want.abs() + TINY[dtype]
-        assert bool(((dw[lo:lo + step].double() - w_want).abs() <= tol).all()), lo
+        assert bool(((table(dw, lo) - w_want).abs() <= tol).all()), lo
         b_want = a * p.sum(0)
         tol = a * (exact + (m + 8) * U * p.abs()).sum(0) + 4 * U * b_want.abs() + TINY["f32"]
         assert bool(((db[lo:lo + step].double() - b_want).abs() <= tol).all()), lo
@@ -76,6 +78,13 @@ def _check(mdnn, m, n, k, dtype, pad=0, step=1 << 14):
 def test_tables_of_2_31_elements(mdnn, m, n, k, dtype, pad):
     assert n * k >= 2 ** (30 if dtype == "f32" else 31)
     _check(mdnn, m, n, k, dtype, pad, 1 << (19 if k < 1000 else 14))
+
+
+@pytest.mark.parametrize("m,n,k,dtype,pad", [(70, 250880, 8704, "bf16", 0), (20, 250881, 8704, "f16", 0),
+                                             (3, 250880, 8704, "bf16", 8), (20, 262144, 4200, "f32", 4)])
+def test_class_contiguous_weights_of_2_31_elements(mdnn, m, n, k, dtype, pad):
+    assert n * k >= 2 ** (30 if dtype == "f32" else 31)
+    _check(mdnn, m, n, k, dtype, pad, by_class=False)
 
 
 @pytest.mark.parametrize("m,n,k,dtype", [(16384, 8193, 40, "f32"), (16384, 16387, 24, "f32"), (1 << 19, 515, 64, "f32"),
