@@ -15,8 +15,9 @@
 // are no multiples of 64, rows off 16 bytes) are copied to padded rows, W by
 // pieces, where there are rows enough to pay for that; otherwise, and in fp32, the
 // register-staged kernel takes them as they are (xent_reg.hip).  Where neither
-// can (contiguous extents below 16 bytes), or so few tiles over a long K that K
-// has to be split, a piece's fp32 logits go through the workspace.
+// can (contiguous extents below 16 bytes, a table's rows further apart than 32-bit
+// offsets reach over 256 classes), or so few tiles over a long K that K has to be
+// split, a piece's fp32 logits go through the workspace.
 //
 // In 16 bits G is stored as 2^15 G for fp16 (probabilities of 1e-5 are subnormal
 // there, those of 1e-8 nothing; times 2^15 the least normal one is 1.9e-9) and
@@ -631,9 +632,9 @@ BwdPlan bwd_plan(Way way, mdnn_layout_t layout, int64_t M, int64_t N, int64_t K,
   // (fp32: a depth below 8 of dW's product would take a kernel for narrow operands: 4 rows, 30912 x 134, 35 us)
   p.rows = h ? up(M, 64) : M < 8 ? 8 : M;
   p.kc = h ? up(K, 64) : up(K, 4);
-  p.nc = piece_classes(N, way == GENERAL ? M : p.rows, (way == GENERAL ? (int64_t)32 : (int64_t)128) << 20);
-  if (way == PACKED) {
-    const int64_t most = piece_classes(N, p.kc, (int64_t)128 << 20);
+  p.nc = piece_classes(N, p.rows, (int64_t)128 << 20);
+  if (way == GENERAL || way == PACKED) {  // (stored logits; W's copy)
+    const int64_t most = way == GENERAL ? piece_classes(N, M, (int64_t)32 << 20) : piece_classes(N, p.kc, (int64_t)128 << 20);
     p.nc = p.nc < most ? p.nc : most;
   }
   if (way == STAGED && layout == MDNN_NN) p.nc = whole_chunks(N, p.nc, t);
