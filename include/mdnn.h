@@ -596,8 +596,14 @@ mdnn_status_t mdnn_layernorm_bwd(int64_t rows, int64_t cols, const void* dy, int
 
 /* ---------------------------------------------------------------------------
  * A last layer z = x W + bias of many classes and its softmax cross entropy,
- * in pieces of the classes: neither the logits nor their gradients of all
- * classes are kept (mdnn_softmax_xent takes stored logits of up to 1024).
+ * in pieces of the classes (mdnn_softmax_xent takes stored logits of up to
+ * 1024): the workspace does not grow with M x N without end.  A piece's logits
+ * stay in registers; where no tile kernel can take the operands (a few tiles
+ * over a long K, contiguous extents below 16 bytes, rows too far apart for
+ * 32-bit offsets) they are stored as fp32, at most 2^24 of them forward and 2^25
+ * backward.  G below is stored for a piece, at most 2^27 elements.  (Either: or
+ * 256 classes of all rows, where those are more; fewer classes than a piece
+ * are one.)
  *   x [M, K], ldx >= K; W of the same dtype, layout MDNN_NN: W[K, N], ldw >= N
  *   (this library's FC weights), MDNN_NT: W[N, K], ldw >= K (a table by
  *   classes).  bias NULL or fp32 [N] (-Inf masks a class).  labels int32 [M]:
@@ -626,7 +632,9 @@ mdnn_status_t mdnn_layernorm_bwd(int64_t rows, int64_t cols, const void* dy, int
  * 0), 256-byte aligned; scratch, overwritten; calls that share one must be
  * ordered on one stream.  Outputs must not overlap inputs or each other.
  * Products are accumulated in fp32, the exponentials' sums in fp32, the loss
- * over rows in 64 bits; all orders are fixed (deterministic).
+ * over rows in 64 bits; all orders are fixed (deterministic).  An exponential of
+ * a difference d is within 2^-21 + |d| 2^-23 of it, relative, for fp32 operands
+ * too.
  * Errors: MDNN_ERR_SHAPE, _DTYPE, _NULL, _LAYOUT (also layout TN),
  * _MISALIGNED, _WORKSPACE, _LAUNCH.
  * ------------------------------------------------------------------------- */

@@ -474,7 +474,7 @@ def _xent_args(x, w, labels, bias, layout):
 def linear_xent(x, w, labels, bias=None, layout: int = NN, ignored: int = -1, workspace=None, stream=None):
     """(loss, row_loss, lse) of a last layer x w + bias of many classes: the mean cross entropy over the rows whose label
     is not `ignored`, each row's, and the logarithm of each row's sum of exponentials, which the gradients need.  w:
-    [in, classes] (NN) or [classes, in] (NT); the logits of all classes are never stored."""
+    [in, classes] (NN) or [classes, in] (NT), taken in pieces of the classes; no result holds logits."""
     import torch
     M, N, K, ldx, ldw, bias = _xent_args(x, w, labels, bias, layout)
     loss, row_loss, lse = (torch.empty((n,), dtype=torch.float32, device=x.device) for n in (1, M, M))
