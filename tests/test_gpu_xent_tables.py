@@ -64,12 +64,14 @@ def _check(mdnn, m, n, k, dtype, pad=0, step=1 << 14, by_class=True):
         dx_want = dx_want + a * (p @ wd)
         dx_tol = dx_tol + a * ((stored + (n + 68) * U * p.abs()) @ wd.abs())
         w_want = a * (p.t() @ xm)
-        tol = a * ((stored + (m + 64) * U * p.abs()).t() @ xm.abs()) + (6 * U + 1.01 * HALF[dtype]) * w_want.abs() + TINY[dtype]
+        tol = a * ((stored + (m + 64) * U * p.abs()).t() @ xm.abs()) + TINY[dtype]
+        tol = tol + (6 * U + 1.01 * HALF[dtype]) * w_want.abs()
         assert bool(((table(dw, lo) - w_want).abs() <= tol).all()), lo
         b_want = a * p.sum(0)
         tol = a * (exact + (m + 8) * U * p.abs()).sum(0) + 4 * U * b_want.abs() + TINY["f32"]
         assert bool(((db[lo:lo + step].double() - b_want).abs() <= tol).all()), lo
-    assert bool(((dx.double() - dx_want).abs() <= dx_tol + (4 * U + 1.01 * HALF[dtype]) * dx_want.abs() + TINY[dtype]).all())
+    dx_tol = dx_tol + (4 * U + 1.01 * HALF[dtype]) * dx_want.abs() + TINY[dtype]
+    assert bool(((dx.double() - dx_want).abs() <= dx_tol).all())
 
 
 @pytest.mark.parametrize("m,n,k,dtype,pad", [(3, 250880, 8704, "bf16", 0), (70, 250880, 8704, "bf16", 0),
@@ -87,14 +89,12 @@ def test_class_contiguous_weights_of_2_31_elements(mdnn, m, n, k, dtype, pad):
     _check(mdnn, m, n, k, dtype, pad, by_class=False)
 
 
-@pytest.mark.parametrize("m,n,k,dtype", [(16384, 8193, 40, "f32"), (16384, 16387, 24, "f32"), (1 << 19, 515, 64, "f32"),
-                                         (200, (1 << 19) + 3, 65, "f16"), (1 << 20, 2051, 33, "f32")])
-def test_short_last_pieces(mdnn, m, n, k, dtype):
-    """Class-contiguous W whose classes leave less than a 16-byte chunk past whole pieces."""
+def _check_rows(mdnn, m, n, k, dtype):
+    """Class-contiguous W and many rows, a piece of the rows at a time."""
     import torch
-    t = {"f32": torch.float32, "f16": torch.float16}[dtype]
+    t = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
     g = torch.Generator(device="cuda").manual_seed(n)
-    x = torch.randn(m, k, generator=g, device="cuda").to(t)
+    x = torch.empty(m, k, dtype=t, device="cuda").normal_(generator=g)
     w = (torch.randn(k, n, generator=g, device="cuda") * 2 / k ** 0.5).to(t)
     bias = torch.randn(n, generator=g, device="cuda")
     labels = torch.randint(0, n, (m,), generator=g, device="cuda", dtype=torch.int32)
@@ -106,7 +106,7 @@ def test_short_last_pieces(mdnn, m, n, k, dtype):
     dw_want, dw_tol = torch.zeros_like(wd), torch.zeros_like(wd)
     db_want, db_tol = (torch.zeros(n, dtype=torch.float64, device="cuda") for _ in range(2))
     wt = wd.t().contiguous()
-    step = max(40, (1 << 25) // n)
+    step = max(40, (1 << 25) // max(n, k))
     for lo in range(0, m, step):
         rows = slice(lo, min(m, lo + step))
         xd, c = x[rows].double(), counted[rows, None]
@@ -124,9 +124,11 @@ def test_short_last_pieces(mdnn, m, n, k, dtype):
         exact = p * (e_z + 2.0 ** -21 + 2 * U * (z - l).abs())
         p.scatter_add_(1, at, -c.double())
         exact += U * p.abs()
-        stored = torch.where(c, exact + HALF[dtype] * (p.abs() + exact) + (2.0 ** -40 if dtype == "f16" else 2.0 ** -134), 0.0)
+        least = 2.0 ** -40 if dtype == "f16" else 2.0 ** -134
+        stored = torch.where(c, exact + HALF[dtype] * (p.abs() + exact) + least, 0.0)
         dx_want = a * (p @ wt)
-        tol = a * ((stored + (n + 68) * U * p.abs()) @ wt.abs()) + (4 * U + 1.01 * HALF[dtype]) * dx_want.abs() + TINY[dtype]
+        tol = a * ((stored + (n + 68) * U * p.abs()) @ wt.abs()) + TINY[dtype]
+        tol = tol + (4 * U + 1.01 * HALF[dtype]) * dx_want.abs()
         assert bool(((dx[rows].double() - dx_want).abs() <= tol).all())
         xm = torch.where(c, xd, 0.0).t().contiguous()
         dw_want += a * (xm @ p)
@@ -136,3 +138,18 @@ def test_short_last_pieces(mdnn, m, n, k, dtype):
     assert bool(((dw.double() - dw_want).abs() <= dw_tol + 6 * U * dw_want.abs()).all())
     assert bool(((db.double() - db_want).abs() <= db_tol + 4 * U * db_want.abs()).all())
     assert abs(float(loss) - float(row.double().sum()) * a) <= 2 * U * abs(float(loss))
+
+
+@pytest.mark.parametrize("m,n,k,dtype", [(16384, 8193, 40, "f32"), (16384, 16387, 24, "f32"), (1 << 19, 515, 64, "f32"),
+                                         (200, (1 << 19) + 3, 65, "f16"), (1 << 20, 2051, 33, "f32")])
+def test_short_last_pieces(mdnn, m, n, k, dtype):
+    """Classes that leave less than a 16-byte chunk past whole pieces."""
+    _check_rows(mdnn, m, n, k, dtype)
+
+
+@pytest.mark.parametrize("m,n,k,dtype", [(540000, 520, 4096, "bf16"), (530001, 261, 4100, "f16"),
+                                         (270000, 300, 4096, "f32")])
+def test_rows_of_2_31_elements(mdnn, m, n, k, dtype):
+    """x past what 32-bit offsets reach."""
+    assert m * k >= 2 ** (30 if dtype == "f32" else 31)
+    _check_rows(mdnn, m, n, k, dtype)
